@@ -368,6 +368,167 @@ typedef struct {
 omnimem_status omnimem_profile_report(omnimem_ctx* ctx, omnimem_kernel_time* out, int32_t capacity,
                                       int32_t* count);
 
+/* ---------------------------------------------------------------------------
+ * Around the step: what a layer does between its projections and the
+ * compression, and what reads the caches that the compression leaves.
+ *
+ *   omnimem_rotate   normalises and rotates a chunk's projected queries and
+ *                    keys and writes them, with the values, behind the cache;
+ *   omnimem_attend   attention of the chunk over the working set (Eq. 1), with
+ *                    the log-sum-exp that omnimem_score takes, or of prompts
+ *                    and single tokens over a memory and the rows behind it;
+ *   omnimem_pack     holds kept rows in 4 bits (a "memory"), between chunks
+ *                    or for answers; omnimem_unpack brings them back.
+ *
+ * A model runs them layer by layer for several streams at once, so they take
+ * an array of `n` descriptors (HOST memory, copied before the call returns),
+ * one per sequence, of any lengths; 0 rows or queries are allowed and nothing
+ * is done for them.  They share a handle that knows the head layout.  The
+ * conventions above hold: device pointers owned by the caller, host-side
+ * checks before any launch, asynchronous work on `stream`, no allocation
+ * after create, calls on one handle ordered (its workspace is shared by them;
+ * so are graphs captured from it, which must not run at the same time).
+ * Calls can be captured into graphs: descriptors travel as kernel arguments.
+ * The outputs of a call's sequences must not overlap.
+ * ------------------------------------------------------------------------- */
+typedef struct {
+  int32_t n_q_heads;        /* H_q                                            */
+  int32_t n_kv_heads;       /* H_kv; must divide H_q                           */
+  int32_t head_dim;         /* d: 64 or 128                                    */
+  int32_t dtype;            /* omnimem_dtype of every row                      */
+} omnimem_attn_config;
+
+typedef struct omnimem_attn omnimem_attn;
+
+/* Create a handle on the current HIP device, with 32 MiB of workspace (the
+ * partial results of attention rows whose keys are split).  Errors:
+ * INVALID_ARG, UNSUPPORTED (head_dim, dtype), HIP (allocation failed), with
+ * the text in omnimem_attn_last_error(NULL). */
+omnimem_status omnimem_attn_create(const omnimem_attn_config* cfg, omnimem_attn** out);
+
+/* Wait for the device's work, free the workspace and the handle.  NULL is
+ * accepted. */
+omnimem_status omnimem_attn_destroy(omnimem_attn* attn);
+
+/* Text of the handle's last error; NULL -> of the calling thread's last failed
+ * omnimem_attn_create, or call without a handle. */
+const char* omnimem_attn_last_error(const omnimem_attn* attn);
+
+/* Rotary positions with one or several axes (time, height, width, ...):
+ * frequency j turns its pair of channels by pos[axis[j]] * inv_freq[j]
+ * radians. */
+typedef struct {
+  int32_t rotary_dim;       /* leading channels that turn: a multiple of 16, 0 to d */
+  int32_t neighbours;       /* pairs of frequency j: 0: channels j and j + rotary_dim / 2; 1: 2j and 2j + 1 */
+  int32_t n_axes;           /* position axes: 1 to 4                           */
+  const double* inv_freq;   /* HOST [rotary_dim / 2], finite                   */
+  const uint8_t* axis;      /* HOST [rotary_dim / 2], below n_axes; NULL: all 0 */
+  const void* q_weight;     /* device [d], or NULL: queries are not normalised */
+  const void* k_weight;     /* device [d], or NULL: keys are not normalised    */
+  float eps;                /* of the norms, >= 0                              */
+} omnimem_rope;
+
+/* One sequence's projected rows and where they go. */
+typedef struct {
+  const void* q;            /* [H_q][n_rows][d]                                */
+  int64_t q_head_stride, q_row_stride;
+  const void* k;            /* [H_kv][n_rows][d]                               */
+  const void* v;            /* [H_kv][n_rows][d]                               */
+  int64_t kv_head_stride, kv_row_stride;   /* elements, shared by k and v      */
+  const int32_t* pos;       /* [n_axes][n_rows] positions                      */
+  int64_t pos_stride;       /* elements between axes                           */
+  const uint8_t* modality;  /* optional [n_rows]                               */
+  int64_t n_rows;
+  void* q_out;              /* [H_q][n_rows][d]                                */
+  int64_t q_out_head_stride, q_out_row_stride;
+  void* k_out;              /* [H_kv][n_rows][d]: the first row behind the cache */
+  void* v_out;
+  int64_t out_head_stride, out_row_stride; /* elements, shared by k_out and v_out */
+  uint8_t* modality_out;    /* [n_rows], with modality                         */
+} omnimem_projection;
+
+/* For each row x of a query or key head: x' = x * w / sqrt(mean(x^2) + eps)
+ * where a weight is given, else x; then its pairs turn:
+ * (x'_a cos - x'_b sin, x'_a sin + x'_b cos).  Values (and modality, when
+ * given) are copied.  Angles are formed and reduced in 64 bits, norms and
+ * rotations computed in fp32 and rounded once.  Each output is its own input
+ * (same pointer and strides: in place) or overlaps no input.
+ * Errors: INVALID_ARG, UNSUPPORTED (rotary_dim not a multiple of 16). */
+omnimem_status omnimem_rotate(omnimem_attn* attn, const omnimem_rope* rope, const omnimem_projection* seqs,
+                              int32_t n, hipStream_t stream);
+
+/* A memory holds the K and V rows of each KV head in 4 bits, in blocks of 32
+ * rows and 34 d bytes.  32 values share a scale 2^e: of K, 32 consecutive
+ * channels of a row; of V, a channel's 32 rows (the axis that each is summed
+ * along).  With m the group's largest magnitude, e is the smallest exponent
+ * of at least -120 with m <= 7 * 2^e, and a value x is held as the multiple of
+ * 2^e in {0, 0.5, 1, 1.5, 2, 3, 4, 6} nearest to |x| (ties to the even code),
+ * with x's sign: off by at most 2^e.  A group with an infinity or NaN comes
+ * back as NaN.  A block's bytes:
+ *   [0, 16 d)     K codes, row t at (d / 2) t: channels 2i, 2i + 1 in the low
+ *                 and high half of byte i; code = sign << 3 | index above;
+ *   [16 d, 32 d)  V codes, channel c at 16 c: rows 2i, 2i + 1 in byte i;
+ *   [32 d, 33 d)  K scales (e + 127): channels 32 p .. of row t at
+ *                 ((t % 4) (d / 32) + p) 8 + t / 4;
+ *   [33 d, 34 d)  V scales: channel c at (c % 16) (d / 16) + c / 16.
+ * Rows of the last block behind the last row are held as zeros.  A memory's
+ * block b of KV head g is at data + g * data_head_stride + 34 d b. */
+typedef struct {
+  void* k;                  /* [H_kv][n_rows][d] rows to pack, or to write      */
+  void* v;                  /* [H_kv][n_rows][d]                               */
+  int64_t kv_head_stride, kv_row_stride;   /* elements, shared by k and v      */
+  void* data;               /* [H_kv] heads of ceil(n_rows / 32) blocks         */
+  int64_t data_head_stride; /* bytes, a multiple of 16                         */
+  int64_t n_rows;
+} omnimem_held;
+
+/* Bytes of one KV head of a memory of `rows` rows (34 d per started block);
+ * 0 for a head_dim or a number of rows that is not supported. */
+int64_t omnimem_memory_bytes(int32_t head_dim, int64_t rows);
+
+/* Hold rows: writes `data` from k and v.  To add rows to a memory whose last
+ * block is full, give the data behind it; a block is written as a whole.
+ * Errors: INVALID_ARG (null pointers, alignment, strides, overlap). */
+omnimem_status omnimem_pack(omnimem_attn* attn, const omnimem_held* seqs, int32_t n, hipStream_t stream);
+
+/* Bring rows back: writes k and v from `data` (each value as it is held; in
+ * bf16 exact).  Errors as omnimem_pack. */
+omnimem_status omnimem_unpack(omnimem_attn* attn, const omnimem_held* seqs, int32_t n, hipStream_t stream);
+
+/* One sequence's queries and the rows that they attend to: those of an
+ * optional memory, then the tail rows k, v (a working set, a prompt, the
+ * answer's tokens so far, the queries' own rows last). */
+typedef struct {
+  const void* q;            /* [H_q][n_queries][d]                             */
+  int64_t q_head_stride, q_row_stride;
+  int64_t n_queries;
+  const void* memory;       /* or NULL                                         */
+  int64_t memory_head_stride; /* bytes, a multiple of 16                       */
+  int64_t memory_rows;      /* 0 without a memory                              */
+  const void* k;            /* [H_kv][n_tail][d], or NULL without tail rows    */
+  const void* v;
+  int64_t kv_head_stride, kv_row_stride;   /* elements, shared by k and v      */
+  int64_t n_tail;
+  float sm_scale;           /* 0 -> 1/sqrt(d)                                   */
+  void* out;                /* [H_q][n_queries][d]                             */
+  int64_t out_head_stride, out_row_stride;
+  float* lse;               /* optional [H_q][n_queries] fp32                  */
+  int64_t lse_head_stride;  /* elements                                        */
+} omnimem_query;
+
+/* out = softmax(sm_scale q k^T) v over the rows that a query sees, and lse the
+ * natural log of the sum of exp(sm_scale <q, k>) over them.  Query i sees
+ * every memory row, and the tail rows t <= n_tail - n_queries + i (causal) or
+ * all of them.  Rows that it does not see have no part in its result,
+ * whatever they hold.  A query that sees none, or whose products are all -inf,
+ * gets out = 0 and lse = -inf.  Statistics and sums are fp32; with bf16 rows
+ * the weights are rounded to bf16 for the product with v.  Results do not
+ * depend on what else the call holds beyond the order in which a row's keys
+ * are summed (keys are split over workgroups when there are few rows).
+ * Errors: INVALID_ARG (null pointers, alignment, strides, overlap). */
+omnimem_status omnimem_attend(omnimem_attn* attn, const omnimem_query* seqs, int32_t n, int32_t causal,
+                              hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

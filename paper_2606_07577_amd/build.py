@@ -13,7 +13,8 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libomnimem.so")
-SOURCES = ["api.hip", "score.hip", "redundancy.hip", "allocate.hip", "select.hip"]
+SOURCES = ["api.hip", "score.hip", "redundancy.hip", "allocate.hip", "select.hip", "attn_api.hip", "rotate.hip", "hold.hip",
+           "attend.hip"]
 # Throughput probes of the score passes' instruction mix (measurement only,
 # a library of their own: nothing of the product links them).
 PROBE_SOURCES = ["probe.hip"]

@@ -1,0 +1,121 @@
+// Internal declarations of the operators around the compression step
+// (rotation, 4-bit memories, attention): descriptors as they travel to the
+// kernels, and what the translation units share.
+#pragma once
+
+#include "common.h"
+
+namespace omnimem {
+
+// Sequences described by one launch: their descriptors are kernel arguments
+// (of which a kernel may have 4 KiB), so a call needs no table on the device,
+// no copy before it, and can be captured as it is.
+constexpr int kSeqsPerLaunch = 16;
+
+// ---------------------------------------------------------------------------
+// 4-bit memories: blocks of 32 rows and 34 d bytes.
+// ---------------------------------------------------------------------------
+constexpr int kMemRows = 32;
+template <int D>
+struct MemBlock {
+  static constexpr int BYTES = 34 * D;
+  static constexpr int V = 16 * D, KS = 32 * D, VS = 33 * D;   // offsets: V codes, K scales, V scales
+  static constexpr int PARTS = D / 32;                         // K groups of a row
+  __host__ __device__ static inline int k_scale(int t, int p) { return KS + ((t & 3) * PARTS + p) * 8 + (t >> 2); }
+  __host__ __device__ static inline int v_scale(int c) { return VS + (c & 15) * (D / 16) + (c >> 4); }
+};
+constexpr uint32_t kScaleNan = 255;    // the scale byte of a group with an infinity or NaN
+constexpr uint32_t kScaleMin = 7;      // 2^-120
+__device__ inline float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
+
+// The eight values (fp32) of a word of codes; NaN where the scale is kScaleNan.
+__device__ inline void values8(uint32_t w, uint32_t byte, float (&x)[8]) {
+  const float s = scale_of(byte);
+  const floatx2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 1);
+  const floatx2 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 3);
+  x[0] = a[0]; x[1] = a[1]; x[2] = b[0]; x[3] = b[1]; x[4] = c[0]; x[5] = c[1]; x[6] = d[0]; x[7] = d[1];
+  if (byte == kScaleNan) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(0x7FC00000u);
+  }
+}
+// The same as eight bf16 values (each is exact: three significant bits and an
+// exponent of at least -121).
+__device__ inline uint4 values8_bf16(uint32_t w, uint32_t byte) {
+  const float s = scale_of(byte);
+  uint4 r;
+  r.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 0));
+  r.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 1));
+  r.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 2));
+  r.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 3));
+  if (byte == kScaleNan) r.x = r.y = r.z = r.w = 0x7FC07FC0u;
+  return r;
+}
+
+// ---------------------------------------------------------------------------
+// Kernel arguments.
+// ---------------------------------------------------------------------------
+struct RotateSeq {
+  const void* q; const void* k; const void* v;
+  const int32_t* pos;
+  const uint8_t* mod;
+  void* q_out; void* k_out; void* v_out;
+  uint8_t* mod_out;
+  int64_t q_hs, q_rs, kv_hs, kv_rs, pos_s, qo_hs, qo_rs, o_hs, o_rs;
+  int64_t n;
+};
+struct RotateArgs {
+  RotateSeq seq[kSeqsPerLaunch];
+  double turns[64];            // inv_freq / 2 pi
+  uint8_t axis[64];
+  const void* q_w; const void* k_w;
+  float eps;
+  int rot, neighbours, h_q, h_kv;
+};
+
+struct HeldSeq {
+  char* k; char* v; char* data;
+  int64_t kv_hs, kv_rs, data_hs;
+  int64_t n;
+};
+struct HeldArgs {
+  HeldSeq seq[kSeqsPerLaunch];
+};
+
+struct QuerySeq {
+  const void* q; const char* mem; const void* k; const void* v;
+  void* out; float* lse;
+  int64_t q_hs, q_rs, mem_hs, kv_hs, kv_rs, out_hs, out_rs, lse_hs;
+  float scale_log2;            // softmax scale times log2(e)
+  int32_t nq, nm, nt;          // queries, memory rows, tail rows
+  int32_t row_tiles, splits;   // of its work (see AttendPlan)
+  int32_t unit0;               // its first unit of the launch
+  int32_t slot0;               // its first partial
+};
+// A call's work.  A KV head's query rows are numbered query-major (row
+// i * G + h is query i of the head's h-th query head: neighbouring rows see
+// the same keys, and share them), in tiles of R rows.  A row tile's keys
+// come in tiles of kKeyTile rows, the memory's and then the tail's; a unit
+// (one workgroup) is a row tile and `chunk` consecutive key tiles.  With more
+// than one unit to a row tile each writes a partial result (sums against its
+// own maximum) and the join puts them together, in the order of the keys.
+constexpr int kKeyTile = 128;
+struct AttendArgs {
+  QuerySeq seq[kSeqsPerLaunch];
+  int n_seqs, h_kv, group, causal, chunk;
+  float* part_o;               // [slots][R][d] unnormalised sums
+  float2* part_ml;             // [slots][R] (maximum in log2 units, sum of weights)
+};
+static_assert(sizeof(RotateArgs) <= 3968 && sizeof(HeldArgs) <= 3968 && sizeof(AttendArgs) <= 3968,
+              "a kernel's arguments, with what the runtime adds, stay below 4 KiB");
+
+struct AttnDims {
+  int h_q, h_kv, group, d, dtype;
+};
+hipError_t launch_rotate(const AttnDims& dm, const RotateArgs& a, int n, hipStream_t st);
+hipError_t launch_hold(const AttnDims& dm, const HeldArgs& a, int n, bool pack, hipStream_t st);
+constexpr int64_t kPartBytes = (int64_t)32 << 20;   // workspace of a handle
+// Fills the plan fields of `a` for n sequences and launches their attention.
+hipError_t launch_attend(const AttnDims& dm, AttendArgs& a, int n, int compute_units, void* workspace, hipStream_t st);
+
+}  // namespace omnimem

@@ -1,0 +1,200 @@
+// Kept rows in 4 bits: packing rows into a memory's blocks and bringing them
+// back.
+#include "../../include/omnimem.h"
+#include "attn.h"
+
+namespace omnimem {
+namespace {
+
+// The scale byte of a group whose largest magnitude has the bits m: the
+// smallest exponent with m <= 1.75 * 2^(e + 2), from the exponent field of m
+// with anything past 1.75 carried into it.
+__device__ inline uint32_t scale_byte(uint32_t m) {
+  if (m >= 0x7F800000u) return kScaleNan;
+  const int e = (int)((m + 0x1FFFFFu) >> 23) - 2;
+  return (uint32_t)max(e, (int)kScaleMin);
+}
+__device__ inline uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7FFFFFFFu; }
+
+// Eight values over the scale, each the nearest code (ties to even; the
+// conversion takes what lies past 6 to 6), the first in the lowest bits.
+__device__ inline uint32_t codes8(const float (&x)[8], uint32_t byte) {
+  if (byte == kScaleNan) return 0;
+  const float s = scale_of(byte);
+  uint32_t w = 0;
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[0], x[1], s, 0);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], s, 1);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], s, 2);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], s, 3);
+  return w;
+}
+
+__device__ inline float load1(const uint16_t* p) { return __uint_as_float((uint32_t)gload<uint16_t>(p) << 16); }
+__device__ inline float load1(const float* p) { return gload<float>(p); }
+__device__ inline void load8(const uint16_t* p, float (&x)[8]) {
+  const uint4 w = gload16(p);
+  const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(u[i] << 16); x[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u); }
+}
+__device__ inline void load8(const float* p, float (&x)[8]) {
+  const floatx4 a = gload<floatx4>(p), b = gload<floatx4>(p + 4);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { x[i] = a[i]; x[4 + i] = b[i]; }
+}
+// CPL channels (1 or 2) of a row.
+template <int CPL>
+__device__ inline void load_channels(const uint16_t* p, float (&x)[CPL]) {
+  if constexpr (CPL == 1) {
+    x[0] = load1(p);
+  } else {
+    const uint32_t w = gload<uint32_t>(p);
+    x[0] = __uint_as_float(w << 16);
+    x[1] = __uint_as_float(w & 0xFFFF0000u);
+  }
+}
+template <int CPL>
+__device__ inline void load_channels(const float* p, float (&x)[CPL]) {
+#pragma unroll
+  for (int i = 0; i < CPL; ++i) x[i] = load1(p + i);
+}
+
+// One wavefront per block of 32 rows.  K: four lanes to a group of 32
+// channels, 8 channels each.  V: a lane has D/64 channels over the 32 rows.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void pack_rows(HeldArgs a) {
+  using B = MemBlock<D>;
+  constexpr int CPL = D / 64;
+  const HeldSeq& s = a.seq[blockIdx.z];
+  const int lane = threadIdx.x & 63;
+  const int64_t block = (int64_t)blockIdx.x * 4 + wave_id();
+  if (block * kMemRows >= s.n) return;
+  const int valid = (int)min((int64_t)kMemRows, s.n - block * kMemRows);
+  const T* k = reinterpret_cast<const T*>(s.k) + blockIdx.y * s.kv_hs + block * kMemRows * s.kv_rs;
+  const T* v = reinterpret_cast<const T*>(s.v) + blockIdx.y * s.kv_hs + block * kMemRows * s.kv_rs;
+  char* out = s.data + blockIdx.y * s.data_hs + block * B::BYTES;
+  float col[CPL][kMemRows];
+#pragma unroll
+  for (int t = 0; t < kMemRows; ++t) {
+    float x[CPL] = {};
+    if (t < valid) load_channels<CPL>(v + t * s.kv_rs + lane * CPL, x);
+#pragma unroll
+    for (int i = 0; i < CPL; ++i) col[i][t] = x[i];
+  }
+#pragma unroll
+  for (int it = 0; it < D / 16; ++it) {
+    const int slot = it * 64 + lane, t = slot / (D / 8), c8 = slot % (D / 8);
+    float x[8] = {};
+    if (t < valid) load8(k + t * s.kv_rs + c8 * 8, x);
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, magnitude(x[i]));
+    m = max(m, (uint32_t)__shfl_xor((int)m, 1));
+    m = max(m, (uint32_t)__shfl_xor((int)m, 2));
+    const uint32_t byte = scale_byte(m);
+    *reinterpret_cast<uint32_t*>(out + t * (D / 2) + c8 * 4) = codes8(x, byte);
+    if ((c8 & 3) == 0) out[B::k_scale(t, c8 >> 2)] = (char)byte;
+  }
+#pragma unroll
+  for (int i = 0; i < CPL; ++i) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int t = 0; t < kMemRows; ++t) m = max(m, magnitude(col[i][t]));
+    const uint32_t byte = scale_byte(m);
+    uint32_t w[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      float x[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = col[i][8 * j + e];
+      w[j] = codes8(x, byte);
+    }
+    const int c = lane * CPL + i;
+    *reinterpret_cast<uint4*>(out + B::V + c * 16) = make_uint4(w[0], w[1], w[2], w[3]);
+    out[B::v_scale(c)] = (char)byte;
+  }
+}
+
+template <int CPL>
+__device__ inline void store_channels(uint16_t* p, const float (&x)[CPL]) {
+  if constexpr (CPL == 1) *p = (uint16_t)round2(x[0], 0.0f);
+  else *reinterpret_cast<uint32_t*>(p) = round2(x[0], x[1]);
+}
+template <int CPL>
+__device__ inline void store_channels(float* p, const float (&x)[CPL]) {
+#pragma unroll
+  for (int i = 0; i < CPL; ++i) p[i] = x[i];
+}
+__device__ inline void store_values(uint16_t* p, uint32_t w, uint32_t byte) {
+  *reinterpret_cast<uint4*>(p) = values8_bf16(w, byte);
+}
+__device__ inline void store_values(float* p, uint32_t w, uint32_t byte) {
+  float x[8];
+  values8(w, byte, x);
+  *reinterpret_cast<floatx4*>(p) = floatx4{x[0], x[1], x[2], x[3]};
+  *reinterpret_cast<floatx4*>(p + 4) = floatx4{x[4], x[5], x[6], x[7]};
+}
+
+// The same the other way.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void unpack_rows(HeldArgs a) {
+  using B = MemBlock<D>;
+  constexpr int CPL = D / 64;
+  const HeldSeq& s = a.seq[blockIdx.z];
+  const int lane = threadIdx.x & 63;
+  const int64_t block = (int64_t)blockIdx.x * 4 + wave_id();
+  if (block * kMemRows >= s.n) return;
+  const int valid = (int)min((int64_t)kMemRows, s.n - block * kMemRows);
+  T* k = reinterpret_cast<T*>(s.k) + blockIdx.y * s.kv_hs + block * kMemRows * s.kv_rs;
+  T* v = reinterpret_cast<T*>(s.v) + blockIdx.y * s.kv_hs + block * kMemRows * s.kv_rs;
+  const char* in = s.data + blockIdx.y * s.data_hs + block * B::BYTES;
+  uint4 codes[CPL];
+  uint32_t byte[CPL];
+#pragma unroll
+  for (int i = 0; i < CPL; ++i) {
+    codes[i] = gload16(in + B::V + (lane * CPL + i) * 16);
+    byte[i] = gload<uint8_t>(in + B::v_scale(lane * CPL + i));
+  }
+#pragma unroll
+  for (int it = 0; it < D / 16; ++it) {
+    const int slot = it * 64 + lane, t = slot / (D / 8), c8 = slot % (D / 8);
+    const uint32_t w = gload<uint32_t>(in + t * (D / 2) + c8 * 4);
+    const uint32_t b = gload<uint8_t>(in + B::k_scale(t, c8 >> 2));
+    if (t < valid) store_values(k + t * s.kv_rs + c8 * 8, w, b);
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    float x[CPL][8];
+#pragma unroll
+    for (int i = 0; i < CPL; ++i) values8(j == 0 ? codes[i].x : j == 1 ? codes[i].y : j == 2 ? codes[i].z : codes[i].w, byte[i], x[i]);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      float y[CPL];
+#pragma unroll
+      for (int i = 0; i < CPL; ++i) y[i] = x[i][e];
+      if (8 * j + e < valid) store_channels<CPL>(v + (8 * j + e) * s.kv_rs + lane * CPL, y);
+    }
+  }
+}
+
+template <typename T, int D>
+void launch(const HeldArgs& a, dim3 grid, bool pack, hipStream_t st) {
+  if (pack) pack_rows<T, D><<<grid, 256, 0, st>>>(a); else unpack_rows<T, D><<<grid, 256, 0, st>>>(a);
+}
+
+}  // namespace
+
+hipError_t launch_hold(const AttnDims& dm, const HeldArgs& a, int n, bool pack, hipStream_t st) {
+  int64_t rows = 0;
+  for (int i = 0; i < n; ++i) rows = std::max(rows, a.seq[i].n);
+  if (rows == 0) return hipSuccess;
+  const dim3 grid((unsigned)((rows + 4 * kMemRows - 1) / (4 * kMemRows)), dm.h_kv, n);
+  if (dm.dtype == OMNIMEM_BF16) {
+    if (dm.d == 128) launch<uint16_t, 128>(a, grid, pack, st); else launch<uint16_t, 64>(a, grid, pack, st);
+  } else {
+    if (dm.d == 128) launch<float, 128>(a, grid, pack, st); else launch<float, 64>(a, grid, pack, st);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace omnimem

@@ -28,6 +28,8 @@ EXPORTED = [
     "omnimem_calibrate", "omnimem_calibration_reset", "omnimem_calibration_budgets",
     "omnimem_allocate_fixed", "omnimem_profile", "omnimem_profile_report", "omnimem_inplace_status",
     "omnimem_append", "omnimem_allocate_noalloc", "omnimem_set_topk_path",
+    "omnimem_attn_create", "omnimem_attn_destroy", "omnimem_attn_last_error", "omnimem_rotate", "omnimem_pack",
+    "omnimem_unpack", "omnimem_memory_bytes", "omnimem_attend",
 ]
 
 
@@ -65,6 +67,50 @@ class Chunk(ctypes.Structure):
     _fields_ = [
         ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("head_stride", ctypes.c_int64),
         ("row_stride", ctypes.c_int64), ("modality", ctypes.c_void_p), ("n_rows", ctypes.c_int64),
+    ]
+
+
+class AttnConfig(ctypes.Structure):
+    _fields_ = [("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("dtype", ctypes.c_int32)]
+
+
+class Rope(ctypes.Structure):
+    _fields_ = [
+        ("rotary_dim", ctypes.c_int32), ("neighbours", ctypes.c_int32), ("n_axes", ctypes.c_int32),
+        ("inv_freq", ctypes.POINTER(ctypes.c_double)), ("axis", ctypes.POINTER(ctypes.c_uint8)),
+        ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("eps", ctypes.c_float),
+    ]
+
+
+class Projection(ctypes.Structure):
+    _fields_ = [
+        ("q", ctypes.c_void_p), ("q_head_stride", ctypes.c_int64), ("q_row_stride", ctypes.c_int64),
+        ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("kv_head_stride", ctypes.c_int64),
+        ("kv_row_stride", ctypes.c_int64), ("pos", ctypes.c_void_p), ("pos_stride", ctypes.c_int64),
+        ("modality", ctypes.c_void_p), ("n_rows", ctypes.c_int64), ("q_out", ctypes.c_void_p),
+        ("q_out_head_stride", ctypes.c_int64), ("q_out_row_stride", ctypes.c_int64), ("k_out", ctypes.c_void_p),
+        ("v_out", ctypes.c_void_p), ("out_head_stride", ctypes.c_int64), ("out_row_stride", ctypes.c_int64),
+        ("modality_out", ctypes.c_void_p),
+    ]
+
+
+class Held(ctypes.Structure):
+    _fields_ = [
+        ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("kv_head_stride", ctypes.c_int64),
+        ("kv_row_stride", ctypes.c_int64), ("data", ctypes.c_void_p), ("data_head_stride", ctypes.c_int64),
+        ("n_rows", ctypes.c_int64),
+    ]
+
+
+class Query(ctypes.Structure):
+    _fields_ = [
+        ("q", ctypes.c_void_p), ("q_head_stride", ctypes.c_int64), ("q_row_stride", ctypes.c_int64),
+        ("n_queries", ctypes.c_int64), ("memory", ctypes.c_void_p), ("memory_head_stride", ctypes.c_int64),
+        ("memory_rows", ctypes.c_int64), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+        ("kv_head_stride", ctypes.c_int64), ("kv_row_stride", ctypes.c_int64), ("n_tail", ctypes.c_int64),
+        ("sm_scale", ctypes.c_float), ("out", ctypes.c_void_p), ("out_head_stride", ctypes.c_int64),
+        ("out_row_stride", ctypes.c_int64), ("lse", ctypes.c_void_p), ("lse_head_stride", ctypes.c_int64),
     ]
 
 
@@ -121,6 +167,22 @@ def load_library(path=LIB_PATH):
     lib.omnimem_profile_report.argtypes = [vp, ctypes.POINTER(KernelTime), ctypes.c_int32,
                                            ctypes.POINTER(ctypes.c_int32)]
     lib.omnimem_profile_report.restype = i32
+    lib.omnimem_attn_create.argtypes = [ctypes.POINTER(AttnConfig), ctypes.POINTER(vp)]
+    lib.omnimem_attn_create.restype = i32
+    lib.omnimem_attn_destroy.argtypes = [vp]
+    lib.omnimem_attn_destroy.restype = i32
+    lib.omnimem_attn_last_error.argtypes = [vp]
+    lib.omnimem_attn_last_error.restype = ctypes.c_char_p
+    lib.omnimem_rotate.argtypes = [vp, ctypes.POINTER(Rope), ctypes.POINTER(Projection), ctypes.c_int32, vp]
+    lib.omnimem_rotate.restype = i32
+    lib.omnimem_pack.argtypes = [vp, ctypes.POINTER(Held), ctypes.c_int32, vp]
+    lib.omnimem_pack.restype = i32
+    lib.omnimem_unpack.argtypes = [vp, ctypes.POINTER(Held), ctypes.c_int32, vp]
+    lib.omnimem_unpack.restype = i32
+    lib.omnimem_memory_bytes.argtypes = [ctypes.c_int32, i64]
+    lib.omnimem_memory_bytes.restype = ctypes.c_int64
+    lib.omnimem_attend.argtypes = [vp, ctypes.POINTER(Query), ctypes.c_int32, ctypes.c_int32, vp]
+    lib.omnimem_attend.restype = i32
     _lib = lib
     return lib
 
@@ -317,6 +379,184 @@ def make_chunk(k, v, modality):
     ch.modality = _ptr(modality)
     ch.n_rows = k.shape[1]
     return ch
+
+
+MEMORY_ROWS = 32   # rows of a memory block
+
+
+def array_of(descriptors):
+    """A ctypes array of descriptors of one type: built once, passed to any number of calls."""
+    return (type(descriptors[0]) * len(descriptors))(*descriptors)
+
+
+def memory_shape(n_kv_heads, head_dim, rows):
+    """Shape of the uint8 tensor that holds `rows` rows of every KV head in 4 bits."""
+    return n_kv_heads, -(-int(rows) // MEMORY_ROWS), 34 * head_dim
+
+
+def _rows(what, *tensors):
+    """Tensors [heads, rows, d] of one type with their channels next to each other (k and v of one shape and strides)."""
+    first = tensors[0]
+    for t in tensors:
+        if t.dim() != 3 or t.stride(2) != 1 or t.dtype not in (torch.bfloat16, torch.float32):
+            raise ValueError(f"{what} must be [heads, rows, d], bf16 or fp32, its channels contiguous")
+        if t.shape != first.shape or t.stride() != first.stride() or t.dtype != first.dtype:
+            raise ValueError(f"{what} must share shape, strides and type")
+
+
+def _memory(data, rows, k_like=None):
+    if data.dtype != torch.uint8 or data.dim() != 3 or data.stride(2) != 1 or data.stride(1) != data.shape[2]:
+        raise ValueError("a memory is a uint8 tensor [H_kv, blocks, 34 d], its blocks contiguous")
+    if not 0 <= rows <= data.shape[1] * MEMORY_ROWS:
+        raise ValueError(f"{rows} rows do not fit {data.shape[1]} blocks of {MEMORY_ROWS}")
+    if k_like is not None and (data.shape[0] != k_like.shape[0] or data.shape[2] != 34 * k_like.shape[2]):
+        raise ValueError("the memory's heads or width differ from the rows'")
+
+
+def make_rope(head_dim, inv_freq, axis=None, n_axes=None, rotary_dim=None, neighbours=False, q_weight=None,
+              k_weight=None, eps=1e-6):
+    """Descriptor of a model's rotary positions: inv_freq (radians per position, one per pair of channels), axis (the
+    position axis of each; default all 0), the leading rotary_dim channels of a head (default: two per frequency) paired
+    j with j + rotary_dim/2, or 2j with 2j + 1 (neighbours), and optional norm weights [d] (device) for queries and keys."""
+    freq = [float(f) for f in inv_freq]
+    rot = 2 * len(freq) if rotary_dim is None else int(rotary_dim)
+    if rot != 2 * len(freq) or rot > head_dim:
+        raise ValueError(f"rotary_dim {rot} of {head_dim} channels takes {rot // 2} frequencies, got {len(freq)}")
+    axis = [0] * len(freq) if axis is None else [int(a) for a in axis]
+    if len(axis) != len(freq) or any(not 0 <= a < 4 for a in axis):
+        raise ValueError("one axis in 0 .. 3 per frequency")
+    weights = [w for w in (q_weight, k_weight) if w is not None]
+    if any(w.shape != (head_dim,) or w.stride(0) != 1 for w in weights):
+        raise ValueError(f"norm weights must be contiguous [{head_dim}]")
+    r = Rope()
+    r.rotary_dim, r.neighbours = rot, int(bool(neighbours))
+    r.n_axes = int(n_axes) if n_axes is not None else max(axis, default=0) + 1
+    r._freq, r._axis = (ctypes.c_double * max(1, len(freq)))(*freq), (ctypes.c_uint8 * max(1, len(freq)))(*axis)
+    r.inv_freq, r.axis = r._freq, r._axis
+    r.q_weight, r.k_weight, r.eps = _ptr(q_weight), _ptr(k_weight), float(eps)
+    r._weights = weights    # (kept alive with the descriptor)
+    r._dtypes = {w.dtype for w in weights}
+    return r
+
+
+def make_projection(q, k, v, pos, q_out, k_out, v_out, modality=None, modality_out=None):
+    """Descriptor of a sequence's projected rows q [H_q, n, d], k, v [H_kv, n, d] at positions pos int32 [axes, n], and
+    of where they go: q_out [H_q, n, d]; k_out, v_out [H_kv, >= n, d] from the first row behind the cache."""
+    n = k.shape[1]
+    k_out, v_out = k_out[:, :n], v_out[:, :n]
+    for what, group in (("q", (q,)), ("k and v", (k, v)), ("q_out", (q_out,)), ("k_out and v_out", (k_out, v_out))):
+        _rows(what, *group)
+    if q_out.shape != q.shape or k_out.shape != k.shape or q.shape[1:] != k.shape[1:]:
+        raise ValueError("outputs must have their inputs' heads, rows and width")
+    if len({t.dtype for t in (q, k, q_out, k_out)}) != 1:
+        raise TypeError("rows must have one type")
+    if pos.dtype != torch.int32 or pos.dim() != 2 or pos.shape[1] != n or pos.stride(1) != 1:
+        raise ValueError("pos must be int32 [axes, n], its positions contiguous")
+    for m in (modality, modality_out):
+        if m is not None and (m.dtype != torch.uint8 or m.dim() != 1 or m.shape[0] < n or m.stride(0) != 1):
+            raise TypeError("modality must be contiguous uint8 [>= n]")
+    p = Projection()
+    p.q, p.q_head_stride, p.q_row_stride = _ptr(q), q.stride(0), q.stride(1)
+    p.k, p.v, p.kv_head_stride, p.kv_row_stride = _ptr(k), _ptr(v), k.stride(0), k.stride(1)
+    p.pos, p.pos_stride, p.n_rows = _ptr(pos), pos.stride(0), n
+    p.q_out, p.q_out_head_stride, p.q_out_row_stride = _ptr(q_out), q_out.stride(0), q_out.stride(1)
+    p.k_out, p.v_out, p.out_head_stride, p.out_row_stride = _ptr(k_out), _ptr(v_out), k_out.stride(0), k_out.stride(1)
+    p.modality, p.modality_out = _ptr(modality), _ptr(modality_out)
+    p._axes, p._dtype = pos.shape[0], q.dtype
+    return p
+
+
+def make_held(k, v, data):
+    """Descriptor of rows k, v [H_kv, n, d] and the memory that holds them: uint8 of memory_shape (or with more blocks)."""
+    _rows("k and v", k, v)
+    _memory(data, k.shape[1], k)
+    h = Held()
+    h.k, h.v, h.kv_head_stride, h.kv_row_stride = _ptr(k), _ptr(v), k.stride(0), k.stride(1)
+    h.data, h.data_head_stride, h.n_rows = _ptr(data), data.stride(0), k.shape[1]
+    return h
+
+
+def make_query(q, out, k=None, v=None, memory=None, memory_rows=0, sm_scale=0.0, lse=None):
+    """Descriptor of a sequence's queries q [H_q, n, d], their results out [H_q, n, d] (lse fp32 [H_q, n]) and the rows
+    they attend to: memory_rows rows of an optional memory, then the tail rows k, v [H_kv, n_tail, d]."""
+    _rows("q", q)
+    _rows("out", out)
+    if out.shape != q.shape or out.dtype != q.dtype:
+        raise ValueError("out must have q's shape and type")
+    x = Query()
+    x.q, x.q_head_stride, x.q_row_stride, x.n_queries = _ptr(q), q.stride(0), q.stride(1), q.shape[1]
+    x.out, x.out_head_stride, x.out_row_stride = _ptr(out), out.stride(0), out.stride(1)
+    x.sm_scale = float(sm_scale)
+    if (k is None) != (v is None):
+        raise ValueError("k and v must both be given")
+    if k is not None:
+        _rows("k and v", k, v)
+        if k.dtype != q.dtype or k.shape[2] != q.shape[2]:
+            raise ValueError("k and v must have q's type and width")
+        x.k, x.v, x.kv_head_stride, x.kv_row_stride, x.n_tail = _ptr(k), _ptr(v), k.stride(0), k.stride(1), k.shape[1]
+    if memory is not None:
+        _memory(memory, int(memory_rows), k)
+        if memory.shape[2] != 34 * q.shape[2]:
+            raise ValueError("the memory's width differs from the queries'")
+        x.memory, x.memory_head_stride, x.memory_rows = _ptr(memory), memory.stride(0), int(memory_rows)
+    elif memory_rows:
+        raise ValueError("memory_rows without a memory")
+    if lse is not None:
+        if lse.dtype != torch.float32 or lse.shape != q.shape[:2] or lse.stride(1) != 1:
+            raise ValueError("lse must be fp32 [H_q, n], its queries contiguous")
+        x.lse, x.lse_head_stride = _ptr(lse), lse.stride(0)
+    return x
+
+
+class Attention:
+    """An omnimem_attn: the operators around the compression step for one head layout, on the current device.  Calls
+    take lists of descriptors or arrays from array_of, one entry per sequence, of tensors on that device."""
+
+    def __init__(self, n_q_heads, n_kv_heads, head_dim, dtype=BF16):
+        lib = load_library()
+        self.handle = None
+        self.cfg = AttnConfig(n_q_heads, n_kv_heads, head_dim, dtype)
+        self._lib = lib
+        handle = ctypes.c_void_p()
+        st = lib.omnimem_attn_create(ctypes.byref(self.cfg), ctypes.byref(handle))
+        if st != OK:
+            raise OmnimemError(st, lib.omnimem_attn_last_error(None).decode())
+        self.handle = handle
+        self.device = torch.cuda.current_device()
+
+    def _call(self, function, descriptors, kind, *more, stream=None):
+        if len(descriptors) and not (isinstance(descriptors, ctypes.Array) and descriptors._type_ is kind):
+            descriptors = (kind * len(descriptors))(*descriptors)
+        s = stream if stream is not None else torch.cuda.current_stream(self.device)
+        before, after = (more[:1], more[1:]) if kind is Projection else ((), more)
+        st = function(self.handle, *before, descriptors if len(descriptors) else None, len(descriptors), *after,
+                      ctypes.c_void_p(s.cuda_stream))
+        if st != OK:
+            raise OmnimemError(st, self._lib.omnimem_attn_last_error(self.handle).decode())
+
+    # Same names as the C ABI.
+    def omnimem_rotate(self, rope, projections, stream=None):
+        self._call(self._lib.omnimem_rotate, projections, Projection, ctypes.byref(rope), stream=stream)
+
+    def omnimem_pack(self, held, stream=None):
+        self._call(self._lib.omnimem_pack, held, Held, stream=stream)
+
+    def omnimem_unpack(self, held, stream=None):
+        self._call(self._lib.omnimem_unpack, held, Held, stream=stream)
+
+    def omnimem_attend(self, queries, causal=True, stream=None):
+        self._call(self._lib.omnimem_attend, queries, Query, int(bool(causal)), stream=stream)
+
+    def close(self):
+        if self.handle:
+            self._lib.omnimem_attn_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
 
 
 def default_scale(head_dim):

@@ -1,0 +1,138 @@
+"""omnimem_attend against its definition in 64 bits.
+
+With S the largest sum of |q||k| scale of a row's products, u = 2^-24 and N keys: a product of d terms in fp32, scaled
+and turned to a power of 2, is off by at most (d + 6) u S, and so is its share of the weights, relative to them; the
+maximum cancels.  Sums of N weights and of N products with v are off by at most (N + 8) u of their sizes (exp2 and the
+join's factors among the 8 steps).  With A the weighted mean of |v|, out is off by at most A (2 (d + 6) u S + 2 (N + 8) u),
+and with bf16 by A eps / 2 more (each weight rounded, not their sum) and eps / 2 of the value (the result rounded).
+lse is off by (d + 6) u S + (N + 8) u and 2 u of its value.  A weight below 2^-126 of the largest is not an fp32 number
+(the definition's 64 bits hold it): N of them times the largest |v| may be missing."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import operators_oracle as orc
+from paper_2606_07577_amd import omnimem as om
+
+pytestmark = pytest.mark.gpu
+TORCH = {"bf16": torch.bfloat16, "f32": torch.float32}
+U = 2.0 ** -24
+
+
+def host(t):
+    return t.double().cpu().numpy()
+
+
+class Case:
+    """One sequence: random rows, a memory of them packed by the library, an output with a border that stays."""
+
+    def __init__(self, attn, g, h_q, h_kv, d, dtype, nq, nm, nt, scale=None, lse=True):
+        self.sizes, self.scale, td = (nq, nm, nt), scale or d ** -0.5, TORCH[dtype]
+        rnd = lambda *s: torch.randn(*s, generator=g, device="cuda")
+        self.q = rnd(nq, h_q, d).to(td).transpose(0, 1)              # query-major, as a projection leaves it
+        self.k, self.v = (rnd(h_kv, nt + 3, d).to(td) for _ in range(2))
+        self.data, held = None, (np.zeros((h_kv, 0, d)),) * 2
+        if nm:
+            km, vm = (rnd(h_kv, nm, d).to(td) for _ in range(2))
+            self.data = torch.zeros(om.memory_shape(h_kv, d, nm), dtype=torch.uint8, device="cuda")
+            attn.omnimem_pack([om.make_held(km, vm, self.data)])
+            torch.cuda.synchronize()
+            held = orc.unpack(self.data.cpu().numpy(), nm)
+        self.held = held
+        self.k[:, nt:] = float("nan")                                # rows behind the tail
+        self.v[:, nt:] = float("nan")
+        self.out = torch.full((h_q, nq + 1, d), 7.0, device="cuda", dtype=td)
+        self.lse = torch.full((h_q, nq + 1), 7.0, device="cuda") if lse else None
+
+    def query(self):
+        nq, nm, nt = self.sizes
+        return om.make_query(self.q, self.out[:, :nq], self.k[:, :nt] if nt else None, self.v[:, :nt] if nt else None,
+                             self.data, nm, self.scale, None if self.lse is None else self.lse[:, :nq])
+
+    def check(self, causal):
+        nq, nm, nt = self.sizes
+        d, dt = self.q.shape[2], self.q.dtype
+        k, v = (np.concatenate([m, host(t[:, :nt])], 1) for m, t in zip(self.held, (self.k, self.v)))
+        out, lse, size, reach = orc.attend(host(self.q), k, v, nm, self.scale, causal)
+        n, half = k.shape[1], torch.finfo(dt).eps / 2 if dt == torch.bfloat16 else 0.0
+        near = 2 * (d + 6) * U * reach[..., None] + 2 * (n + 8) * U + half
+        tol = size * near + (half or U) * np.abs(out) + n * 2.0 ** -126 * np.abs(v).max(initial=0.0)
+        got = host(self.out[:, :nq])
+        assert np.array_equal(np.isnan(got), np.isnan(out))
+        fine = bool((np.abs(got - out) <= tol)[~np.isnan(out)].all())
+        assert fine, (self.sizes, float(np.nanmax(np.abs(got - out) / tol)))
+        assert (self.out[:, nq:] == 7).all()
+        if self.lse is not None:
+            got = host(self.lse[:, :nq])
+            assert np.array_equal(np.isneginf(got), np.isneginf(lse)) and np.array_equal(np.isnan(got), np.isnan(lse))
+            f = np.isfinite(lse)
+            assert (np.abs(got[f] - lse[f]) <= (d + 6) * U * reach[f] + (n + 8) * U + 2 * U * np.abs(lse[f])).all()
+            assert (self.lse[:, nq:] == 7).all()
+
+
+def handle(h_q, h_kv, d, dtype):
+    return om.Attention(h_q, h_kv, d, om.BF16 if dtype == "bf16" else om.F32)
+
+
+SIZES = [(1, 0, 1), (1, 1, 0), (1, 219, 5), (1, 128, 128), (2, 33, 0), (3, 0, 300), (5, 700, 9), (9, 0, 4), (17, 0, 4), (40, 31, 77),
+         (130, 0, 130), (70, 257, 129), (300, 100, 411)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("h_q,h_kv,d", [(7, 1, 128), (4, 2, 64), (2, 2, 128), (20, 1, 64)])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("sizes", SIZES)
+def test_sequences_alone(dtype, h_q, h_kv, d, causal, sizes):
+    attn = handle(h_q, h_kv, d, dtype)
+    c = Case(attn, torch.Generator(device="cuda").manual_seed(sum(sizes)), h_q, h_kv, d, dtype, *sizes)
+    attn.omnimem_attend([c.query()], causal)
+    torch.cuda.synchronize()
+    c.check(causal)
+    attn.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_ragged_batches(dtype, d):
+    """More sequences than a launch describes, of all forms, empty ones among them."""
+    h_q, h_kv = 6, 2
+    attn = handle(h_q, h_kv, d, dtype)
+    g = torch.Generator(device="cuda").manual_seed(d)
+    sizes = [(1 + (5 * i) % 23, (37 * i) % 300, (11 * i) % 90) for i in range(18)] + [(0, 5, 5), (4, 0, 0)]
+    cases = [Case(attn, g, h_q, h_kv, d, dtype, *s, lse=i % 2 == 0) for i, s in enumerate(sizes)]
+    attn.omnimem_attend([c.query() for c in cases])
+    torch.cuda.synchronize()
+    for c in cases:
+        c.check(True)
+    attn.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("nq,nm,nt", [(1, 9000, 70), (3, 0, 5000), (50, 2000, 1500)])
+def test_keys_split_over_workgroups(dtype, nq, nm, nt):
+    attn = handle(2, 1, 128, dtype)
+    g = torch.Generator(device="cuda").manual_seed(nq)
+    c = Case(attn, g, 2, 1, 128, dtype, nq, nm, nt)
+    attn.omnimem_attend([c.query()])
+    torch.cuda.synchronize()
+    c.check(True)
+    first = c.out.clone()
+    for _ in range(3):                       # the sums' order is fixed: the same bits every time
+        c.out.fill_(7.0)
+        attn.omnimem_attend([c.query()])
+        torch.cuda.synchronize()
+        assert torch.equal(c.out, first)
+    attn.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("scale", [1e-6, 30.0])
+@pytest.mark.parametrize("nq", [2, 90])
+def test_flat_and_sharp_weights(dtype, scale, nq):
+    """Products near 0, and of several hundreds with weights that are 0 but for a few."""
+    attn = handle(4, 1, 64, dtype)
+    c = Case(attn, torch.Generator(device="cuda").manual_seed(5), 4, 1, 64, dtype, nq, 200, 150, scale=scale)
+    attn.omnimem_attend([c.query()])
+    torch.cuda.synchronize()
+    c.check(True)
+    attn.close()
