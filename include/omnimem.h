@@ -400,7 +400,7 @@ typedef struct {
 
 typedef struct omnimem_attn omnimem_attn;
 
-/* Create a handle on the current HIP device, with 32 MiB of workspace (the
+/* Create a handle on the current HIP device, with 128 MiB of workspace (the
  * partial results of attention rows whose keys are split).  Errors:
  * INVALID_ARG, UNSUPPORTED (head_dim, dtype), HIP (allocation failed), with
  * the text in omnimem_attn_last_error(NULL). */

@@ -1,89 +1,129 @@
 // Attention over a 4-bit memory and the tail rows behind it.
+//
+// Every kernel makes one pass over the keys with a running maximum and sum:
+// scores are formed transposed, S^T = K Q^T, so that a lane holds one query's
+// scores, its maximum and its sum, and the weights leave the score's registers
+// as they enter the second product, O^T = V^T P^T: an MFMA's sum runs over its
+// keys in any order, so K and V are read in the order that the accumulator
+// registers have.
 #include "../../include/omnimem.h"
 #include "attn.h"
 
 namespace omnimem {
 namespace {
 
-// Where a unit's work lies.
-struct Unit {
-  int s, g, rt, split;       // sequence, KV head, row tile, split
-  int rows;                  // query rows of the head (G * n_q)
-  int k0, k1;                // key tiles
-  int mem_tiles;             // of the sequence
-  int slot;                  // partial, or -1: the result is final
-};
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+using frag = bf16x8;
+
+__device__ inline float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ inline int64_t elems(uint32_t units, int esz) { return (int64_t)units * (16 / esz); }
 
 // Tail rows that query i sees.
 __device__ inline int tail_seen(const QuerySeq& s, int causal, int i) {
   return causal ? min(max(s.nt - s.nq + i + 1, 0), s.nt) : s.nt;
 }
-__host__ __device__ inline int tiles_of(int64_t rows) { return (int)((rows + kKeyTile - 1) / kKeyTile); }
+template <int KT>
+__host__ __device__ inline int tiles_of(int rows) { return (int)(((int64_t)rows + KT - 1) / KT); }
 
-template <int R>
+// ---------------------------------------------------------------------------
+// Work of a unit.
+// ---------------------------------------------------------------------------
+struct Unit {
+  int s, g, rt;              // sequence, KV head, row tile
+  int rows;                  // query rows of the head (G * n_q)
+  int k0, k1;                // key tiles
+  int mem_tiles;             // of the sequence
+  int slot;                  // partial, or -1: the result is final
+};
+// The last sequence whose entry of `first` is at most u (lane-parallel).
+__device__ inline int seq_of(const int32_t* first, int n, int u) {
+  const int lane = threadIdx.x & 63;
+  const int v = lane < n ? first[lane] : INT32_MAX;
+  return uniform(__popcll(__ballot(v <= u)) - 1);
+}
+template <int R, int KT>
 __device__ inline Unit unit_of(const AttendArgs& a, int u) {
   Unit x;
-  x.s = 0;
-  while (x.s + 1 < a.n_seqs && u >= a.seq[x.s + 1].unit0) ++x.s;
+  int split = 0, splits = 1, tile;
+  x.slot = -1;
+  if (a.whole > 0) {
+    tile = u;
+    if (u >= a.whole) {
+      splits = a.seq[0].splits;
+      x.slot = u - a.whole;
+      tile = a.whole + x.slot / splits;
+      split = x.slot % splits;
+    }
+    x.s = seq_of(a.unit0, a.n_seqs, tile);
+    tile -= a.unit0[x.s];
+  } else {
+    x.s = seq_of(a.unit0, a.n_seqs, u);
+    u -= a.unit0[x.s];
+    splits = a.seq[x.s].splits;
+    if (splits > 1) x.slot = a.seq[x.s].slot0 + u;
+    tile = u / splits;
+    split = u % splits;
+  }
   const QuerySeq& s = a.seq[x.s];
-  u -= s.unit0;
-  x.slot = s.splits > 1 ? s.slot0 + u : -1;
-  x.split = u % s.splits;
-  u /= s.splits;
-  x.rt = u % s.row_tiles;
-  x.g = u / s.row_tiles;
+  x.g = tile / s.row_tiles;
+  x.rt = s.row_tiles - 1 - tile % s.row_tiles;   // (the last rows see the most: they begin first)
   x.rows = a.group * s.nq;
-  x.mem_tiles = tiles_of(s.nm);
-  const int last = (min((x.rt + 1) * R, x.rows) - 1) / a.group;   // the tile's last query sees the most
-  const int tiles = x.mem_tiles + tiles_of(tail_seen(s, a.causal, last));
-  x.k0 = min(x.split * a.chunk, tiles);
-  x.k1 = min(x.k0 + a.chunk, tiles);
+  x.mem_tiles = tiles_of<KT>(s.nm);
+  const int last = (min((x.rt + 1) * R, x.rows) - 1) / a.group;
+  const int tiles = x.mem_tiles + tiles_of<KT>(tail_seen(s, a.causal, last));
+  x.k0 = (int)((int64_t)tiles * split / splits);
+  x.k1 = (int)((int64_t)tiles * (split + 1) / splits);
   return x;
 }
 
-template <typename T> __device__ inline float to_f32(T x);
-template <> __device__ inline float to_f32(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
-template <> __device__ inline float to_f32(float x) { return x; }
-__device__ inline void put(uint16_t* p, float x) { *p = (uint16_t)round2(x, 0.0f); }
-__device__ inline void put(float* p, float x) { *p = x; }
-template <typename T> __device__ inline T as(float x);
-template <> __device__ inline uint16_t as<uint16_t>(float x) { return (uint16_t)round2(x, 0.0f); }
-template <> __device__ inline float as<float>(float x) { return x; }
+// One query row of a tile: where its query is, and the tail rows that it sees.
+struct Row {
+  bool live;
+  int i, h, seen;
+};
+__device__ inline Row row_of(const AttendArgs& a, const QuerySeq& s, const Unit& x, int row) {
+  Row r;
+  r.live = row < x.rows;
+  r.i = r.live ? row / a.group : 0;
+  r.h = x.g * a.group + (r.live ? row - r.i * a.group : 0);
+  r.seen = r.live ? tail_seen(s, a.causal, r.i) : 0;
+  return r;
+}
 
-__device__ inline float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ inline void put4(uint16_t* p, floatx4 x) { *reinterpret_cast<uint2*>(p) = make_uint2(round2(x[0], x[1]), round2(x[2], x[3])); }
+__device__ inline void put4(float* p, floatx4 x) { *reinterpret_cast<floatx4*>(p) = x; }
+__device__ inline float log_of(float m, float l) { return l == 0.0f ? -INFINITY : (m + log2f(l)) * kLn2; }
 
-// The simple form: 32 query rows to a unit; the four wavefronts take 32 keys
-// each of a tile of 128 in LDS, and join their sums at the end.
-template <typename T, int D>
-struct Simple {
-  static constexpr int R = 32;
-  static constexpr int ROW = D + 16 / (int)sizeof(T);      // padded LDS row
-  static constexpr int LDS = 2 * kKeyTile * ROW * (int)sizeof(T) + 4 * R * 8;
+// ---------------------------------------------------------------------------
+// fp32: 32 query rows to a unit; the four wavefronts take 32 keys each of a
+// tile of 128 in LDS, and join their sums at the end.
+// ---------------------------------------------------------------------------
+template <int D>
+struct F32 {
+  static constexpr int R = 32, KT = 128;
+  static constexpr int ROW = D + 4;                        // padded LDS row
+  static constexpr int LDS = 2 * KT * ROW * 4 + 4 * R * 8;
 };
 
-template <typename T, int D>
-__global__ __launch_bounds__(256) void attend_simple(AttendArgs a) {
-  using P = Simple<T, D>;
-  using M = Mfma<T>;
-  using frag = typename M::frag;
-  constexpr int R = P::R, ROW = P::ROW, NKS = D / M::KSTEP, NCT = D / 32;
+template <int D>
+__global__ __launch_bounds__(256) void attend_f32(AttendArgs a) {
+  using P = F32<D>;
+  using M = Mfma<float>;
+  constexpr int R = P::R, KT = P::KT, ROW = P::ROW, NCT = D / 32;
   using B = MemBlock<D>;
   extern __shared__ __align__(16) char lds[];
-  T* kt = reinterpret_cast<T*>(lds);
-  T* vt = kt + kKeyTile * ROW;
-  float2* ml = reinterpret_cast<float2*>(lds + 2 * kKeyTile * ROW * sizeof(T));   // [4][R]
-  const Unit x = unit_of<R>(a, blockIdx.x);
+  float* kt = reinterpret_cast<float*>(lds);
+  float* vt = kt + KT * ROW;
+  float2* ml = reinterpret_cast<float2*>(vt + KT * ROW);   // [4][R]
+  const Unit x = unit_of<R, KT>(a, blockIdx.x);
   const QuerySeq& s = a.seq[x.s];
   const int lane = threadIdx.x & 63, wave = wave_id(), half = lane >> 5, col = lane & 31;
-  const int row = x.rt * R + col;
-  const bool live = row < x.rows;
-  const int i = live ? row / a.group : 0, hh = row - i * a.group;
-  const int h = x.g * a.group + (live ? hh : 0);
-  const int seen = live ? tail_seen(s, a.causal, i) : 0;
-  const T* q = static_cast<const T*>(s.q) + h * s.q_hs + i * s.q_rs;
-  frag qf[NKS];
+  const Row row = row_of(a, s, x, x.rt * R + col);
+  const float* q = static_cast<const float*>(s.q) + row.h * elems(s.q_hs, 4) + row.i * elems(s.q_rs, 4);
+  const int64_t kv_rs = elems(s.kv_rs, 4);
+  float qf[D / 2];
 #pragma unroll
-  for (int ks = 0; ks < NKS; ++ks) qf[ks] = live ? M::gload(q + ks * M::KSTEP + half * M::PER_LANE) : M::zero();
+  for (int ks = 0; ks < D / 2; ++ks) qf[ks] = row.live ? gload<float>(q + ks * 2 + half) : 0.0f;
 
   floatx16 o[NCT];
 #pragma unroll
@@ -93,12 +133,12 @@ __global__ __launch_bounds__(256) void attend_simple(AttendArgs a) {
   for (int kti = x.k0; kti < x.k1; ++kti) {
     __syncthreads();
     const bool in_mem = kti < x.mem_tiles;
-    const int key0 = (in_mem ? kti : kti - x.mem_tiles) * kKeyTile;
-    const int keys = min(kKeyTile, (in_mem ? s.nm : s.nt) - key0);
+    const int key0 = (in_mem ? kti : kti - x.mem_tiles) * KT;
+    const int keys = min(KT, (in_mem ? s.nm : s.nt) - key0);
     if (in_mem) {
-      const char* data = s.mem + x.g * s.mem_hs + (int64_t)(key0 / kMemRows) * B::BYTES;
+      const char* data = s.mem + x.g * ((int64_t)s.mem_hs * 16) + (int64_t)(key0 / kMemRows) * B::BYTES;
       const int blocks = (keys + kMemRows - 1) / kMemRows;
-      for (int e = threadIdx.x; e < kKeyTile * D / 8; e += 256) {
+      for (int e = threadIdx.x; e < KT * D / 8; e += 256) {
         const int t = e / (D / 8), c8 = e % (D / 8), b = t / kMemRows;
         float y[8] = {};
         if (b < blocks) {
@@ -106,9 +146,9 @@ __global__ __launch_bounds__(256) void attend_simple(AttendArgs a) {
           values8(gload<uint32_t>(blk + (t % kMemRows) * (D / 2) + c8 * 4), gload<uint8_t>(blk + B::k_scale(t % kMemRows, c8 >> 2)), y);
         }
 #pragma unroll
-        for (int j = 0; j < 8; ++j) kt[t * ROW + c8 * 8 + j] = as<T>(y[j]);
+        for (int j = 0; j < 8; ++j) kt[t * ROW + c8 * 8 + j] = y[j];
       }
-      for (int e = threadIdx.x; e < kKeyTile * D / 8; e += 256) {
+      for (int e = threadIdx.x; e < KT * D / 8; e += 256) {
         const int c = e % D, t8 = e / D, b = t8 / 4;
         float y[8] = {};
         if (b < blocks) {
@@ -116,32 +156,27 @@ __global__ __launch_bounds__(256) void attend_simple(AttendArgs a) {
           values8(gload<uint32_t>(blk + B::V + c * 16 + (t8 & 3) * 4), gload<uint8_t>(blk + B::v_scale(c)), y);
         }
 #pragma unroll
-        for (int j = 0; j < 8; ++j) vt[(t8 * 8 + j) * ROW + c] = as<T>(y[j]);
+        for (int j = 0; j < 8; ++j) vt[(t8 * 8 + j) * ROW + c] = y[j];
       }
     } else {
-      constexpr int E = 16 / (int)sizeof(T);
-      const T* k = static_cast<const T*>(s.k) + x.g * s.kv_hs + key0 * s.kv_rs;
-      const T* v = static_cast<const T*>(s.v) + x.g * s.kv_hs + key0 * s.kv_rs;
-      for (int e = threadIdx.x; e < kKeyTile * D / E; e += 256) {
-        const int t = e / (D / E), c = e % (D / E) * E;
+      const float* k = static_cast<const float*>(s.k) + x.g * elems(s.kv_hs, 4) + key0 * kv_rs;
+      const float* v = static_cast<const float*>(s.v) + x.g * elems(s.kv_hs, 4) + key0 * kv_rs;
+      for (int e = threadIdx.x; e < KT * D / 4; e += 256) {
+        const int t = e / (D / 4), c = e % (D / 4) * 4;
         const uint4 z = make_uint4(0, 0, 0, 0);
-        *reinterpret_cast<uint4*>(kt + t * ROW + c) = t < keys ? gload16(k + t * s.kv_rs + c) : z;
-        *reinterpret_cast<uint4*>(vt + t * ROW + c) = t < keys ? gload16(v + t * s.kv_rs + c) : z;
+        *reinterpret_cast<uint4*>(kt + t * ROW + c) = t < keys ? gload16(k + t * kv_rs + c) : z;
+        *reinterpret_cast<uint4*>(vt + t * ROW + c) = t < keys ? gload16(v + t * kv_rs + c) : z;
       }
     }
     __syncthreads();
     floatx16 sc = floatx16{};
 #pragma unroll
-    for (int ks = 0; ks < NKS; ++ks) {
-      const T* kp = kt + (wave * 32 + col) * ROW + ks * M::KSTEP + half * M::PER_LANE;
-      sc = M::mma(M::load(kp), qf[ks], sc);
-    }
-    const int limit = in_mem ? (live ? keys : 0) : seen - key0;
+    for (int ks = 0; ks < D / 2; ++ks) sc = M::mma(kt[(wave * 32 + col) * ROW + ks * 2 + half], qf[ks], sc);
+    const int limit = in_mem ? (row.live ? keys : 0) : row.seen - key0;
     float top = -INFINITY;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      const int key = wave * 32 + acc_row(r, lane);
-      sc[r] = key < limit ? sc[r] * s.scale_log2 : -INFINITY;
+      sc[r] = wave * 32 + acc_row(r, lane) < limit ? sc[r] * s.scale_log2 : -INFINITY;
       top = fmaxf(top, sc[r]);
     }
     top = fmaxf(top, __shfl_xor(top, 32));
@@ -156,28 +191,12 @@ __global__ __launch_bounds__(256) void attend_simple(AttendArgs a) {
     }
     l = l * alpha + sum;
 #pragma unroll
-    for (int c = 0; c < NCT; ++c) o[c] *= alpha;
-    // keys of accumulator registers r .. of this half: (r >> 2) * 8 + half * 4 + (r & 3)
-#pragma unroll
     for (int c = 0; c < NCT; ++c) {
-      const T* vp = vt + (wave * 32 + half * 4) * ROW + c * 32 + col;
-      if constexpr (sizeof(T) == 2) {
+      o[c] *= alpha;
+      // (the keys of accumulator register r of this half)
+      const float* vp = vt + (wave * 32 + half * 4) * ROW + c * 32 + col;
 #pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
-          uint32_t va[4], pa[4];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int t = kk * 16 + (j >> 1) * 8 + (j & 1) * 2;
-            va[j] = (uint32_t)vp[t * ROW] | ((uint32_t)vp[(t + 1) * ROW] << 16);
-            pa[j] = round2(sc[kk * 8 + 2 * j], sc[kk * 8 + 2 * j + 1]);
-          }
-          o[c] = M::mma(__builtin_bit_cast(frag, make_uint4(va[0], va[1], va[2], va[3])),
-                        __builtin_bit_cast(frag, make_uint4(pa[0], pa[1], pa[2], pa[3])), o[c]);
-        }
-      } else {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) o[c] = M::mma(vp[((r >> 2) * 8 + (r & 3)) * ROW], sc[r], o[c]);
-      }
+      for (int r = 0; r < 16; ++r) o[c] = M::mma(vp[((r >> 2) * 8 + (r & 3)) * ROW], sc[r], o[c]);
     }
   }
   l += __shfl_xor(l, 32);
@@ -193,8 +212,7 @@ __global__ __launch_bounds__(256) void attend_simple(AttendArgs a) {
   float total = 0.0f;
 #pragma unroll
   for (int w = 0; w < 4; ++w) total += ml[w * R + col].y * exp2_(ml[w * R + col].x - ref);
-  float* ob = reinterpret_cast<float*>(lds);       // [R][D + 4], the tiles are done with
-  constexpr int OROW = D + 4;
+  float* ob = kt;                                  // [R][ROW], the tiles are done with
   for (int w = 0; w < 4; ++w) {
     __syncthreads();
     if (wave == w) {
@@ -202,74 +220,609 @@ __global__ __launch_bounds__(256) void attend_simple(AttendArgs a) {
       for (int c = 0; c < NCT; ++c)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          float* p = ob + col * OROW + c * 32 + acc_row(r, lane);
+          float* p = ob + col * ROW + c * 32 + acc_row(r, lane);
           const float y = o[c][r] * mine;
           *p = w == 0 ? y : *p + y;
         }
     }
   }
   __syncthreads();
-  if (x.slot >= 0) {
-    float* po = a.part_o + (int64_t)x.slot * R * D;
-    for (int e = threadIdx.x; e < R * D; e += 256) po[e] = ob[e / D * OROW + e % D];
-    if (threadIdx.x < R) a.part_ml[(int64_t)x.slot * R + threadIdx.x] = make_float2(top, total);
-  } else {
-    float* inv = reinterpret_cast<float*>(ml);
-    __syncthreads();
-    if (threadIdx.x < R) {
-      inv[threadIdx.x] = total == 0.0f ? 0.0f : 1.0f / total;
-      if (live && s.lse) s.lse[h * s.lse_hs + i] = total == 0.0f ? -INFINITY : (top + log2f(total)) * kLn2;
+  if (wave == 0 && half == 0) {
+    if (x.slot >= 0) {
+      a.part_ml[(int64_t)x.slot * R + col] = make_float2(top, total);
+    } else {
+      ml[col].x = total == 0.0f ? 0.0f : 1.0f / total;
+      if (row.live && s.lse) s.lse[row.h * (int64_t)s.lse_hs + row.i] = log_of(top, total);
     }
-    __syncthreads();
-    for (int e = threadIdx.x; e < R * D; e += 256) {
-      const int r = e / D, c = e % D, gr = x.rt * R + r;
-      if (gr >= x.rows) break;
-      const int qi = gr / a.group, qh = x.g * a.group + gr % a.group;
-      put(static_cast<T*>(s.out) + qh * s.out_hs + qi * s.out_rs + c, ob[r * OROW + c] * inv[r]);
+  }
+  __syncthreads();
+  for (int e = threadIdx.x; e < R * D / 4; e += 256) {
+    const int r = e / (D / 4), c = e % (D / 4) * 4;
+    const floatx4 y = *reinterpret_cast<const floatx4*>(ob + r * ROW + c);
+    if (x.slot >= 0) {
+      put4(a.part_o + ((int64_t)x.slot * R + r) * D + c, y);
+    } else {
+      const Row w = row_of(a, s, x, x.rt * R + r);
+      if (w.live) put4(static_cast<float*>(s.out) + w.h * elems(s.out_hs, 4) + w.i * elems(s.out_rs, 4) + c, y * ml[r].x);
     }
   }
 }
 
+// ---------------------------------------------------------------------------
+// bf16, few rows (single tokens, short questions): 16 NR query rows to a unit.
+// Its key tiles of 128 rows go round the four wavefronts, each with sums of
+// its own.  A memory tile goes from HBM to registers and from there to the
+// MFMAs: lane (i, g) = (lane % 16, lane / 16) reads a quarter of K row i of
+// eight 16-row sets, and channel i's 32 rows of V block g, 16 bytes each; the
+// sets are chosen (rows 4 T .. 4 T + 3 of each of the four blocks) so that
+// set T's scores in lane (query, g) are those of V's rows 4 T .. of block g.
+// ---------------------------------------------------------------------------
+template <int D, int NR>
+struct Few {
+  static constexpr int R = 16 * NR, KT = 128;
+  static constexpr int OROW = D + 4;
+  static constexpr int VBUF = 32 * D * 2;                  // bytes of a wavefront's tail V rows in LDS
+  static constexpr int JOIN = R * OROW * 4;
+  static constexpr int LDS = (4 * VBUF > JOIN ? 4 * VBUF : JOIN) + 4 * R * 8;
+};
+// 16-byte chunk of row r that holds its chunk c: the 8 rows that 32 lanes read
+// 32 bytes each of lie in different banks.
+template <int D>
+__device__ inline int few_chunk(int r, int c) { return D == 128 ? c ^ ((r & 7) << 1) : c ^ (((r >> 1) & 3) << 1); }
+
+template <int NR>
+struct Stats {
+  float m[NR], l[NR];
+};
+// Scores (log2 units) to weights against the running maximum; the factor that
+// what was summed before has to be taken by.
+template <int NR, int N>
+__device__ inline void weigh(floatx4 (&sc)[NR][N], Stats<NR>& st, float (&alpha)[NR]) {
+#pragma unroll
+  for (int n = 0; n < NR; ++n) {
+    float top = -INFINITY;
+#pragma unroll
+    for (int t = 0; t < N; ++t) top = fmaxf(fmaxf(fmaxf(top, sc[n][t][0]), fmaxf(sc[n][t][1], sc[n][t][2])), sc[n][t][3]);
+    top = fmaxf(top, __shfl_xor(top, 16));
+    top = fmaxf(top, __shfl_xor(top, 32));
+    const float m2 = fmaxf(st.m[n], top), ref = m2 == -INFINITY ? 0.0f : m2;
+    alpha[n] = exp2_(st.m[n] - ref);
+    st.m[n] = m2;
+    float sum = 0.0f;
+#pragma unroll
+    for (int t = 0; t < N; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        sc[n][t][r] = exp2_(sc[n][t][r] - ref);
+        sum += sc[n][t][r];
+      }
+    st.l[n] = st.l[n] * alpha[n] + sum;
+  }
+}
+__device__ inline frag pack_weights(floatx4 x, floatx4 y) {
+  return __builtin_bit_cast(frag, make_uint4(round2(x[0], x[1]), round2(x[2], x[3]), round2(y[0], y[1]), round2(y[2], y[3])));
+}
+__device__ inline uint32_t word(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
+__device__ inline float byte_scale(const uint2& v, int i) { return scale_of(((i < 4 ? v.x : v.y) >> (8 * (i & 3))) & 255u); }
+template <int BYTES>
+__device__ inline uint4 load_part(const char* p) {   // 16 or 8 bytes
+  if constexpr (BYTES == 16) return gload16(p);
+  const uint2 x = gload8(p);
+  return make_uint4(x.x, x.y, 0, 0);
+}
+
+template <int D, int NR>
+__global__ __launch_bounds__(256, NR == 1 ? 2 : 1) void attend_few(AttendArgs a) {
+  using P = Few<D, NR>;
+  using B = MemBlock<D>;
+  constexpr int R = P::R, KT = P::KT, NS = D / 32, NC = D / 16;
+  extern __shared__ __align__(16) char lds[];
+  const Unit x = unit_of<R, KT>(a, blockIdx.x);
+  const QuerySeq& s = a.seq[x.s];
+  const int lane = threadIdx.x & 63, wave = wave_id(), g = lane >> 4, i16 = lane & 15;
+  Row row[NR];
+  const uint16_t* q[NR];
+  frag qf[NR][NS];
+  floatx4 o[NR][NC];
+  Stats<NR> st;
+#pragma unroll
+  for (int n = 0; n < NR; ++n) {
+    row[n] = row_of(a, s, x, x.rt * R + n * 16 + i16);
+    q[n] = static_cast<const uint16_t*>(s.q) + row[n].h * elems(s.q_hs, 2) + row[n].i * elems(s.q_rs, 2);
+    st.m[n] = -INFINITY;
+    st.l[n] = 0.0f;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) o[n][c] = floatx4{};
+  }
+  const float scale = s.scale_log2;
+  int kti = x.k0 + wave;
+
+  if (kti < min(x.k1, x.mem_tiles)) {
+    // channels g D/4 .. of the queries, as the lanes hold K's
+#pragma unroll
+    for (int n = 0; n < NR; ++n)
+#pragma unroll
+      for (int j = 0; j < NS; ++j)
+        qf[n][j] = row[n].live ? gload<frag>(q[n] + g * (D / 4) + j * 8) : frag{};
+    const char* data = s.mem + x.g * ((int64_t)s.mem_hs * 16);
+    const int last_block = tiles_of<kMemRows>(s.nm) - 1;
+    uint4 kc[8], vc[NC];
+    uint2 ks, vs;
+    const auto load_k = [&](int t) {
+      const char* blk = data + (int64_t)min(t * 4 + (i16 >> 2), last_block) * B::BYTES;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) kc[j] = load_part<D / 8>(blk + (j * 4 + (i16 & 3)) * (D / 2) + g * (D / 8));
+      ks = gload8(blk + B::k_scale(i16 & 3, g * (D / 4) / 32));
+    };
+    const auto load_v = [&](int t) {
+      const char* blk = data + (int64_t)min(t * 4 + g, last_block) * B::BYTES;
+#pragma unroll
+      for (int c = 0; c < NC; ++c) vc[c] = gload16(blk + B::V + (c * 16 + i16) * 16);
+      if constexpr (NC == 8) vs = gload8(blk + B::v_scale(i16));
+      else vs = make_uint2(gload<uint32_t>(blk + B::v_scale(i16)), 0);
+    };
+    const int end = min(x.k1, x.mem_tiles);
+    load_k(kti);
+    load_v(kti);
+    for (; kti < end; kti += 4) {
+      floatx4 sc[NR][8];
+#pragma unroll
+      for (int t = 0; t < 8; ++t) {
+#pragma unroll
+        for (int n = 0; n < NR; ++n) sc[n][t] = floatx4{};
+        const float ksc = byte_scale(ks, t);
+#pragma unroll
+        for (int j = 0; j < NS; ++j) {
+          const frag kf = __builtin_bit_cast(frag, values8_bf16(word(kc[t], j), ksc));
+#pragma unroll
+          for (int n = 0; n < NR; ++n) sc[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[n][j], sc[n][t], 0, 0, 0);
+        }
+      }
+      if (kti + 4 < end) load_k(kti + 4);
+      const int keys = s.nm - kti * KT;
+#pragma unroll
+      for (int n = 0; n < NR; ++n)
+#pragma unroll
+        for (int t = 0; t < 8; ++t) sc[n][t] *= scale;
+      if (keys < KT) {
+#pragma unroll
+        for (int n = 0; n < NR; ++n)
+#pragma unroll
+          for (int t = 0; t < 8; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              if (g * 32 + t * 4 + r >= keys) sc[n][t][r] = -INFINITY;
+      }
+      float alpha[NR];
+      weigh<NR, 8>(sc, st, alpha);
+      frag pf[NR][4];
+#pragma unroll
+      for (int n = 0; n < NR; ++n)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) pf[n][j] = pack_weights(sc[n][2 * j], sc[n][2 * j + 1]);
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        const float vsc = byte_scale(vs, c);
+#pragma unroll
+        for (int n = 0; n < NR; ++n) o[n][c] *= alpha[n];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const frag vf = __builtin_bit_cast(frag, values8_bf16(word(vc[c], j), vsc));
+#pragma unroll
+          for (int n = 0; n < NR; ++n) o[n][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[n][j], o[n][c], 0, 0, 0);
+        }
+      }
+      if (kti + 4 < end) load_v(kti + 4);
+    }
+  }
+
+  if (kti < x.k1) {
+    // Tail rows, 32 at a time: K from HBM to registers, V through LDS, which
+    // transposes 16-bit elements as they are read.
+#pragma unroll
+    for (int n = 0; n < NR; ++n)
+#pragma unroll
+      for (int j = 0; j < NS; ++j) qf[n][j] = row[n].live ? gload<frag>(q[n] + j * 32 + g * 8) : frag{};
+    const int64_t rs = elems(s.kv_rs, 2);
+    const uint16_t* kp = static_cast<const uint16_t*>(s.k) + x.g * elems(s.kv_hs, 2);
+    const uint16_t* vp = static_cast<const uint16_t*>(s.v) + x.g * elems(s.kv_hs, 2);
+    uint16_t* vb = reinterpret_cast<uint16_t*>(lds + wave * P::VBUF);
+    frag kc[2][NS];
+    uint4 vc[NC];
+    const auto load = [&](int key) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int j = 0; j < NS; ++j)
+          kc[t][j] = gload<frag>(kp + min(key + t * 16 + i16, s.nt - 1) * rs + j * 32 + g * 8);
+#pragma unroll
+      for (int j = 0; j < NC; ++j) {
+        const int slot = j * 64 + lane, t = slot / (D / 8);
+        vc[j] = key + t < s.nt ? gload16(vp + (key + t) * rs + slot % (D / 8) * 8) : make_uint4(0, 0, 0, 0);
+      }
+    };
+    // (each wavefront's 32-row steps: four to a key tile)
+    const auto next = [&](int key) { return (key & 96) != 96 ? key + 32 : key + 32 + 3 * KT; };
+    const int end = min((x.k1 - x.mem_tiles) * KT, s.nt);
+    int key = (kti - x.mem_tiles) * KT;
+    if (key < end) load(key);
+    while (key < end) {
+#pragma unroll
+      for (int j = 0; j < NC; ++j) {
+        const int slot = j * 64 + lane, t = slot / (D / 8);
+        *reinterpret_cast<uint4*>(vb + t * D + few_chunk<D>(t, slot % (D / 8)) * 8) = vc[j];
+      }
+      floatx4 sc[NR][2];
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int n = 0; n < NR; ++n) {
+          sc[n][t] = floatx4{};
+#pragma unroll
+          for (int j = 0; j < NS; ++j) sc[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kc[t][j], qf[n][j], sc[n][t], 0, 0, 0);
+        }
+      const int here = key;
+      key = next(key);
+      if (key < end) load(key);
+#pragma unroll
+      for (int n = 0; n < NR; ++n)
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            sc[n][t][r] = here + t * 16 + g * 4 + r < row[n].seen ? sc[n][t][r] * scale : -INFINITY;
+      float alpha[NR];
+      weigh<NR, 2>(sc, st, alpha);
+      frag pf[NR];
+#pragma unroll
+      for (int n = 0; n < NR; ++n) pf[n] = pack_weights(sc[n][0], sc[n][1]);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        s16x4 lo, hi;
+        const int t = g * 4 + (i16 >> 2), ch = c * 16 + (i16 & 3) * 4;
+        lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (__attribute__((address_space(3))) s16x4*)(vb + t * D + few_chunk<D>(t, ch >> 3) * 8 + (ch & 7)));
+        hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (__attribute__((address_space(3))) s16x4*)(vb + (t + 16) * D + few_chunk<D>(t + 16, ch >> 3) * 8 + (ch & 7)));
+        const uint2 x0 = __builtin_bit_cast(uint2, lo), x1 = __builtin_bit_cast(uint2, hi);
+        const frag vf = __builtin_bit_cast(frag, make_uint4(x0.x, x0.y, x1.x, x1.y));
+#pragma unroll
+        for (int n = 0; n < NR; ++n) {
+          o[n][c] *= alpha[n];
+          o[n][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[n], o[n][c], 0, 0, 0);
+        }
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+    }
+  }
+
+  // join the four wavefronts
+  float2* ml = reinterpret_cast<float2*>(lds + P::LDS - 4 * R * 8);   // [4][R]
+  float* ob = reinterpret_cast<float*>(lds);                          // [R][OROW]
+#pragma unroll
+  for (int n = 0; n < NR; ++n) {
+    st.l[n] += __shfl_xor(st.l[n], 16);
+    st.l[n] += __shfl_xor(st.l[n], 32);
+    if (g == 0) ml[wave * R + n * 16 + i16] = make_float2(st.m[n], st.l[n]);
+  }
+  __syncthreads();
+  float top[NR], total[NR], mine[NR];
+#pragma unroll
+  for (int n = 0; n < NR; ++n) {
+    top[n] = -INFINITY;
+    total[n] = 0.0f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) top[n] = fmaxf(top[n], ml[w * R + n * 16 + i16].x);
+    const float ref = top[n] == -INFINITY ? 0.0f : top[n];
+    mine[n] = exp2_(st.m[n] - ref);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) total[n] += ml[w * R + n * 16 + i16].y * exp2_(ml[w * R + n * 16 + i16].x - ref);
+  }
+  for (int w = 0; w < 4; ++w) {
+    __syncthreads();
+    if (wave == w) {
+#pragma unroll
+      for (int n = 0; n < NR; ++n)
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+          floatx4* p = reinterpret_cast<floatx4*>(ob + (n * 16 + i16) * P::OROW + c * 16 + g * 4);
+          const floatx4 y = o[n][c] * mine[n];
+          *p = w == 0 ? y : *p + y;
+        }
+    }
+  }
+  __syncthreads();
+  if (wave == 0 && g == 0) {
+#pragma unroll
+    for (int n = 0; n < NR; ++n) {
+      if (x.slot >= 0) {
+        a.part_ml[(int64_t)x.slot * R + n * 16 + i16] = make_float2(top[n], total[n]);
+      } else {
+        ml[n * 16 + i16].x = total[n] == 0.0f ? 0.0f : 1.0f / total[n];
+        if (row[n].live && s.lse) s.lse[row[n].h * (int64_t)s.lse_hs + row[n].i] = log_of(top[n], total[n]);
+      }
+    }
+  }
+  __syncthreads();
+  for (int e = threadIdx.x; e < R * D / 4; e += 256) {
+    const int r = e / (D / 4), c = e % (D / 4) * 4;
+    const Row w = row_of(a, s, x, x.rt * R + r);
+    if (!w.live) break;
+    const floatx4 y = *reinterpret_cast<const floatx4*>(ob + r * P::OROW + c);
+    if (x.slot >= 0) put4(a.part_o + ((int64_t)x.slot * R + r) * D + c, y);
+    else put4(static_cast<uint16_t*>(s.out) + w.h * elems(s.out_hs, 2) + w.i * elems(s.out_rs, 2) + c, y * ml[r].x);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// bf16, many rows (chunks): 256 query rows to a unit, 32 to each of eight
+// wavefronts, against key tiles of 64 rows that they share in LDS (two
+// stages: the next tile is on its way while one is multiplied).  Tail rows
+// are copied as they are, and V is transposed as it is read; a memory's codes
+// go through registers, K as rows and V, whose codes lie by channel, as
+// channels with their rows in the order that the weights have.
+// ---------------------------------------------------------------------------
+template <int D>
+struct Many {
+  static constexpr int R = 256, KT = 64, THREADS = 512;
+  static constexpr int TILE = KT * D;                      // elements of a K or V stage
+  static constexpr int LDS = 4 * TILE * 2;
+  static constexpr int CPR = D / 8;                        // 16-byte chunks per row
+  __device__ static inline int k_chunk(int r, int c) { return c ^ (r & (CPR - 1)); }
+  __device__ static inline int v_chunk(int r, int c) { return D == 128 ? c ^ ((r & 3) << 2) : c ^ (((r >> 1) & 1) << 2); }
+};
+
+template <int D>
+__global__ __launch_bounds__(512, 2) void attend_many(AttendArgs a) {
+  using P = Many<D>;
+  using B = MemBlock<D>;
+  constexpr int R = P::R, KT = P::KT, TILE = P::TILE, CPR = P::CPR, NKS = D / 16, NCT = D / 32;
+  constexpr int W = D / 64;                                // code words per thread and operand of a memory tile
+  extern __shared__ __align__(16) char lds[];
+  uint16_t* kbuf = reinterpret_cast<uint16_t*>(lds);       // [2][TILE]
+  uint16_t* vbuf = kbuf + 2 * TILE;
+  // round by round of the chip's 256 compute units, neighbouring units on one XCD
+  int u = blockIdx.x;
+  if ((u | 255) < a.units) u = (u & ~255) + (u & 7) * 32 + ((u & 255) >> 3);
+  const Unit x = unit_of<R, KT>(a, u);
+  const QuerySeq& s = a.seq[x.s];
+  const int tid = threadIdx.x, lane = tid & 63, wave = wave_id(), half = lane >> 5, col = lane & 31;
+  const Row row = row_of(a, s, x, x.rt * R + wave * 32 + col);
+  frag qf[NKS];
+  const float scale = fabsf(s.scale_log2);
+  {
+    const uint16_t* q = static_cast<const uint16_t*>(s.q) + row.h * elems(s.q_hs, 2) + row.i * elems(s.q_rs, 2);
+    const uint32_t flip = s.scale_log2 < 0.0f ? 0x80008000u : 0u;   // (a negative scale goes into the queries' signs)
+#pragma unroll
+    for (int j = 0; j < NKS; ++j) {
+      uint4 w = row.live ? gload16(q + j * 16 + half * 8) : make_uint4(0, 0, 0, 0);
+      w.x ^= flip; w.y ^= flip; w.z ^= flip; w.w ^= flip;
+      qf[j] = __builtin_bit_cast(frag, w);
+    }
+  }
+  floatx16 o[NCT];
+#pragma unroll
+  for (int c = 0; c < NCT; ++c) o[c] = floatx16{};
+  float m = -INFINITY, l = 0.0f;                           // m: log2 units, the reference of the sums
+
+  const int64_t rs = elems(s.kv_rs, 2);
+  const uint16_t* kp = static_cast<const uint16_t*>(s.k) + x.g * elems(s.kv_hs, 2);
+  const uint16_t* vp = static_cast<const uint16_t*>(s.v) + x.g * elems(s.kv_hs, 2);
+  const char* data = s.mem + x.g * ((int64_t)s.mem_hs * 16);
+  const int last_block = tiles_of<kMemRows>(s.nm) - 1;
+
+  uint32_t kw[W], vw[W], kb = 0, vb = 0;                   // a memory tile on its way
+  const int krow = tid / 8;                                // K: 8 threads to a row; V: 8 / W to a channel
+  const int vch = tid * W / 8, vt8 = tid * W % 8;          // (and the first of its words, of 8 rows each)
+  const auto fetch = [&](int t, int st) {
+    if (t < x.mem_tiles) {
+      const char* blk = data + (int64_t)min(t * 2 + krow / 32, last_block) * B::BYTES;
+      const int r = krow & 31, p = tid & 7;
+      const char* vk = data + (int64_t)min(t * 2 + vt8 / 4, last_block) * B::BYTES;
+      if constexpr (W == 2) {
+        const uint2 k2 = gload8(blk + r * (D / 2) + p * 8), v2 = gload8(vk + B::V + vch * 16 + vt8 % 4 * 4);
+        kw[0] = k2.x; kw[1] = k2.y; vw[0] = v2.x; vw[1] = v2.y;
+      } else {
+        kw[0] = gload<uint32_t>(blk + r * (D / 2) + p * 4);
+        vw[0] = gload<uint32_t>(vk + B::V + vch * 16 + vt8 % 4 * 4);
+      }
+      kb = gload<uint8_t>(blk + B::k_scale(r, p * (D / 8) / 32));
+      vb = gload<uint8_t>(vk + B::v_scale(vch));
+    } else {
+      const int key0 = (t - x.mem_tiles) * KT;
+#pragma unroll
+      for (int j = 0; j < CPR / 8; ++j) {
+        const int J = wave * (CPR / 8) + j, slot = J * 64 + lane, r = slot / CPR, c = slot % CPR;
+        const int64_t at = min(key0 + r, s.nt - 1) * rs;
+        dma16_opaque(kp + at + P::k_chunk(r, c) * 8, kbuf + st * TILE + J * 512);
+        dma16_opaque(vp + at + P::v_chunk(r, c) * 8, vbuf + st * TILE + J * 512);
+      }
+    }
+  };
+  const auto store = [&](int t, int st) {
+    if (t >= x.mem_tiles) return;
+    uint16_t* kd = kbuf + st * TILE;
+    uint16_t* vd = vbuf + st * TILE;
+#pragma unroll
+    for (int j = 0; j < W; ++j) {
+      *reinterpret_cast<uint4*>(kd + krow * D + P::k_chunk(krow, (tid & 7) * W + j) * 8) = values8_bf16(kw[j], scale_of(kb));
+      const uint4 y = values8_bf16(vw[j], scale_of(vb));
+      const int t8 = vt8 + j;                    // rows 8 t8 .. of the tile: 16-row step t8 / 2
+      uint16_t* p = vd + vch * KT + (t8 & 1) * 4;
+      *reinterpret_cast<uint2*>(p + (((t8 >> 1) * 2) ^ (vch & 7)) * 8) = make_uint2(y.x, y.y);
+      *reinterpret_cast<uint2*>(p + (((t8 >> 1) * 2 + 1) ^ (vch & 7)) * 8) = make_uint2(y.z, y.w);
+    }
+  };
+
+  if (x.k0 < x.k1) {
+    fetch(x.k0, 0);
+    store(x.k0, 0);
+  }
+  dma_wait();
+  __syncthreads();
+  for (int t = x.k0; t < x.k1; ++t) {
+    const int st = (t - x.k0) & 1;
+    const bool in_mem = t < x.mem_tiles;
+    if (t + 1 < x.k1) fetch(t + 1, st ^ 1);
+    const uint16_t* kd = kbuf + st * TILE;
+    const uint16_t* vd = vbuf + st * TILE;
+    floatx16 sc[2];
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      sc[b] = floatx16{};
+#pragma unroll
+      for (int j = 0; j < NKS; ++j) {
+        const int r = b * 32 + col;
+        const frag kf = *reinterpret_cast<const frag*>(kd + r * D + P::k_chunk(r, 2 * j + half) * 8);
+        sc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[j], sc[b], 0, 0, 0);
+      }
+    }
+    const int key0 = (in_mem ? t : t - x.mem_tiles) * KT;
+    const int limit = (in_mem ? (row.live ? s.nm : 0) : row.seen) - key0;
+    if (__any(limit < KT)) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (b * 32 + acc_row(r, lane) >= limit) sc[b][r] = -INFINITY;
+    }
+    float top = -INFINITY;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) top = fmaxf(fmaxf(top, sc[0][r]), sc[1][r]);
+    top = fmaxf(top, __shfl_xor(top, 32)) * scale;
+    // The sums keep their reference until a score passes it by 8: weights stay below 2^8, and few tiles scale O.
+    if (__any(top > m + 8.0f)) {
+      const float m2 = fmaxf(m, top);
+      const float alpha = m2 == -INFINITY ? 1.0f : exp2_(m - m2);
+      m = m2;
+      l *= alpha;
+#pragma unroll
+      for (int c = 0; c < NCT; ++c) o[c] *= alpha;
+    }
+    const float ref = m == -INFINITY ? 0.0f : m;
+    frag pf[4];
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        sc[b][r] = exp2_(__builtin_fmaf(sc[b][r], scale, -ref));
+        l += sc[b][r];
+      }
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        uint32_t w[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = round2(sc[b][j * 8 + 2 * e], sc[b][j * 8 + 2 * e + 1]);
+        pf[b * 2 + j] = __builtin_bit_cast(frag, make_uint4(w[0], w[1], w[2], w[3]));
+      }
+    }
+    if (in_mem) {
+#pragma unroll
+      for (int c = 0; c < NCT; ++c)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int ch = c * 32 + col;
+          const frag vf = *reinterpret_cast<const frag*>(vd + ch * KT + ((2 * j + half) ^ (ch & 7)) * 8);
+          o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[j], o[c], 0, 0, 0);
+        }
+    } else {
+#pragma unroll
+      for (int c = 0; c < NCT; ++c)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int r = j * 16 + half * 4 + ((lane & 15) >> 2), ch = c * 32 + (lane & 16) + (lane & 3) * 4;
+          const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+              (__attribute__((address_space(3))) s16x4*)(vd + r * D + P::v_chunk(r, ch >> 3) * 8 + (ch & 7)));
+          const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+              (__attribute__((address_space(3))) s16x4*)(vd + (r + 8) * D + P::v_chunk(r + 8, ch >> 3) * 8 + (ch & 7)));
+          const uint2 x0 = __builtin_bit_cast(uint2, lo), x1 = __builtin_bit_cast(uint2, hi);
+          o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(frag, make_uint4(x0.x, x0.y, x1.x, x1.y)), pf[j], o[c], 0, 0, 0);
+        }
+    }
+    if (t + 1 < x.k1) store(t + 1, st ^ 1);
+    dma_wait();
+    __syncthreads();
+  }
+  l += __shfl_xor(l, 32);
+  if (x.slot >= 0) {
+    const int64_t r = (int64_t)x.slot * R + wave * 32 + col;
+    if (half == 0) a.part_ml[r] = make_float2(m, l);
+#pragma unroll
+    for (int c = 0; c < NCT; ++c)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        put4(a.part_o + r * D + c * 32 + e * 8 + half * 4, floatx4{o[c][4 * e], o[c][4 * e + 1], o[c][4 * e + 2], o[c][4 * e + 3]});
+  } else if (row.live) {
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    uint16_t* out = static_cast<uint16_t*>(s.out) + row.h * elems(s.out_hs, 2) + row.i * elems(s.out_rs, 2);
+    if (half == 0 && s.lse) s.lse[row.h * (int64_t)s.lse_hs + row.i] = log_of(m, l);
+#pragma unroll
+    for (int c = 0; c < NCT; ++c)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        put4(out + c * 32 + e * 8 + half * 4, floatx4{o[c][4 * e], o[c][4 * e + 1], o[c][4 * e + 2], o[c][4 * e + 3]} * inv);
+  }
+}
+
+// ---------------------------------------------------------------------------
 // Puts the partial results of a query row's splits together: a workgroup per
 // row, D/4 threads to a partial.
+// ---------------------------------------------------------------------------
 template <typename T, int D, int R>
 __global__ __launch_bounds__(256) void join_splits(AttendArgs a) {
   constexpr int TPR = D / 4, PAR = 256 / TPR;
   __shared__ floatx4 sums[PAR][TPR];
-  __shared__ float2 stat[4];
-  int u = blockIdx.x, si = 0;
-  for (; si + 1 < a.n_seqs; ++si) {
-    const int n = a.seq[si].splits > 1 ? a.h_kv * a.seq[si].row_tiles : 0;
-    if (u < n) break;
-    u -= n;
+  __shared__ float ls[PAR];
+  __shared__ float tops[4];
+  const int lane = threadIdx.x & 63;
+  int si, tile;
+  int64_t slot;
+  if (a.whole > 0) {
+    tile = a.whole + blockIdx.x;
+    si = seq_of(a.unit0, a.n_seqs, tile);
+    tile -= a.unit0[si];
+    slot = (int64_t)blockIdx.x * a.seq[0].splits;
+  } else {
+    int first = lane < a.n_seqs && a.seq[lane].splits > 1 ? a.h_kv * a.seq[lane].row_tiles : 0;
+    const int count = first;
+    for (int k = 1; k < kQueriesPerLaunch; k *= 2) {
+      const int y = __shfl_up(first, k);
+      if (lane >= k) first += y;
+    }
+    first -= count;                              // split row tiles of the sequences before
+    const uint64_t at = __ballot(count > 0 && first <= (int)blockIdx.x);
+    si = uniform(63 - __clzll((long long)at));
+    tile = blockIdx.x - uniform(__shfl(first, si));
+    slot = a.seq[si].slot0 + (int64_t)tile * a.seq[si].splits;
   }
   const QuerySeq& s = a.seq[si];
-  const int rt = u % s.row_tiles, g = u / s.row_tiles;
+  const int splits = s.splits;
+  const int rt = s.row_tiles - 1 - tile % s.row_tiles, g = tile / s.row_tiles;
   const int row = rt * R + blockIdx.y;
   if (row >= a.group * s.nq) return;
   const int i = row / a.group, h = g * a.group + row % a.group;
-  const int64_t slot = s.slot0 + (int64_t)u * s.splits;
   const float2* ml = a.part_ml + slot * R + blockIdx.y;
   float m = -INFINITY;
-  for (int p = threadIdx.x; p < s.splits; p += 256) m = fmaxf(m, gload<float>(&ml[(int64_t)p * R].x));
+  for (int p = threadIdx.x; p < splits; p += 256) m = fmaxf(m, gload<float>(&ml[(int64_t)p * R].x));
 #pragma unroll
   for (int k = 1; k < 64; k *= 2) m = fmaxf(m, __shfl_xor(m, k));
-  if ((threadIdx.x & 63) == 0) stat[threadIdx.x >> 6].x = m;
+  if (lane == 0) tops[threadIdx.x >> 6] = m;
   __syncthreads();
-  m = fmaxf(fmaxf(stat[0].x, stat[1].x), fmaxf(stat[2].x, stat[3].x));
+  m = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
   const float ref = m == -INFINITY ? 0.0f : m;
   const int c = threadIdx.x % TPR, p0 = threadIdx.x / TPR;
   floatx4 o = floatx4{};
   float l = 0.0f;
-  for (int p = p0; p < s.splits; p += PAR) {
+  for (int p = p0; p < splits; p += PAR) {
     const floatx2 x = gload<floatx2>(&ml[(int64_t)p * R]);
-    if (x[0] == -INFINITY) continue;           // (it may have written no sums)
     const float w = exp2_(x[0] - ref);
     l += w * x[1];
     o += w * gload<floatx4>(a.part_o + ((slot + p) * R + blockIdx.y) * D + c * 4);
   }
   sums[p0][c] = o;
-  __shared__ float ls[PAR];
   if (c == 0) ls[p0] = l;
   __syncthreads();
   if (threadIdx.x >= TPR) return;
@@ -278,63 +831,129 @@ __global__ __launch_bounds__(256) void join_splits(AttendArgs a) {
 #pragma unroll
   for (int p = 0; p < PAR; ++p) { o += sums[p][c]; l += ls[p]; }
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-  T* out = static_cast<T*>(s.out) + h * s.out_hs + i * s.out_rs + c * 4;
-  if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(out) = make_uint2(round2(o[0] * inv, o[1] * inv), round2(o[2] * inv, o[3] * inv));
-  else *reinterpret_cast<floatx4*>(out) = o * inv;
-  if (c == 0 && s.lse) s.lse[h * s.lse_hs + i] = l == 0.0f ? -INFINITY : (m + log2f(l)) * kLn2;
+  constexpr int E = (int)sizeof(T);
+  put4(static_cast<T*>(s.out) + h * elems(s.out_hs, E) + i * elems(s.out_rs, E) + c * 4, o * inv);
+  if (c == 0 && s.lse) s.lse[h * (int64_t)s.lse_hs + i] = log_of(m, l);
 }
 
-// Row tiles of R rows, key tiles in chunks: as few units as fill the chip
-// (`target`), no more partials than the workspace holds.
+// ---------------------------------------------------------------------------
+// Plans and launches.
+// ---------------------------------------------------------------------------
 template <int R, int D>
-int plan(AttendArgs& a, int n, int h_kv, int64_t target) {
-  int64_t most = 1, tiles_all = 0;
-  for (int i = 0; i < n; ++i) {
+constexpr int64_t partials() { return kPartBytes / (R * (D * 4 + 8)); }
+
+template <int R, int KT>
+int64_t count_tiles(AttendArgs& a, int64_t* keys) {
+  int64_t n = 0;
+  *keys = 0;
+  for (int i = 0; i < a.n_seqs; ++i) {
     QuerySeq& s = a.seq[i];
     s.row_tiles = (int)(((int64_t)a.group * s.nq + R - 1) / R);
-    const int64_t t = std::max(tiles_of(s.nm) + tiles_of(s.nt), 1);
-    most = std::max(most, t);
-    tiles_all += (int64_t)h_kv * s.row_tiles * t;
+    n += (int64_t)a.h_kv * s.row_tiles;
+    *keys += (int64_t)a.h_kv * s.row_tiles * (tiles_of<KT>(s.nm) + tiles_of<KT>(s.nt));
   }
-  const int64_t slots = kPartBytes / (R * (D * 4 + 8));
-  int64_t chunk = std::max<int64_t>(1, tiles_all / target);
-  for (;; chunk += 1 + chunk / 16) {
-    int64_t units = 0, parts = 0;
-    for (int i = 0; i < n; ++i) {
+  return n;
+}
+
+// Key tiles in shares of about `share`, or as many more as leave about
+// `target` units, or no more partials than the workspace holds.
+template <int R, int KT>
+int64_t plan_shares(AttendArgs& a, int64_t slots, int64_t share, int64_t target) {
+  int64_t keys;
+  count_tiles<R, KT>(a, &keys);
+  a.whole = 0;
+  for (share = std::max(share, keys / target);; share += 1 + share / 16) {
+    int64_t units = 0, parts = 0, joins = 0;
+    for (int i = 0; i < a.n_seqs; ++i) {
       QuerySeq& s = a.seq[i];
-      const int64_t t = std::max(tiles_of(s.nm) + tiles_of(s.nt), 1);
-      s.splits = (int)((t + chunk - 1) / chunk);
-      s.unit0 = (int)units;
-      s.slot0 = (int)parts;
-      const int64_t u = (int64_t)h_kv * s.row_tiles * s.splits;
-      units += u;
-      if (s.splits > 1) parts += u;
+      const int64_t t = std::max(tiles_of<KT>(s.nm) + tiles_of<KT>(s.nt), 1);
+      s.splits = (int)((t + share - 1) / share);
       if (units > INT32_MAX) return -1;
+      a.unit0[i] = (int)units;
+      s.slot0 = (int)parts;
+      const int64_t u = (int64_t)a.h_kv * s.row_tiles * s.splits;
+      units += u;
+      if (s.splits > 1) {
+        parts += u;
+        joins += (int64_t)a.h_kv * s.row_tiles;
+      }
     }
+    if (units > INT32_MAX) return -1;
     if (parts <= slots) {
-      a.chunk = (int)chunk;
-      return (int)units;
+      a.units = (int)units;
+      return joins;
     }
   }
 }
 
-template <typename T, int D>
-hipError_t attend(AttendArgs& a, int n, int compute_units, void* ws, hipStream_t st) {
-  using P = Simple<T, D>;
-  constexpr int R = P::R;
-  const int units = plan<R, D>(a, n, a.h_kv, 4 * compute_units);
+// As many whole row tiles as fill the chip a number of times, and the rest in
+// so many shares that they fill it once more.
+template <int R, int KT>
+int64_t plan_rounds(AttendArgs& a, int64_t slots, int width) {
+  int64_t keys;
+  const int64_t n = count_tiles<R, KT>(a, &keys);
+  if (n > INT32_MAX / 16) return -1;
+  const int64_t whole = n / width * width, rest = n - whole;
+  int splits = 1;
+  if (rest > 0) {
+    const int64_t most = std::max<int64_t>(1, std::min(slots / rest, keys / n / 4));   // (a share is some tiles at least)
+    double best = 1e30;
+    for (int c = 1; c <= std::min<int64_t>(most, 64); ++c) {
+      const double cost = (double)((rest * c + width - 1) / width) / c + 0.01 * c;
+      if (cost < best) { best = cost; splits = c; }
+    }
+  }
+  a.whole = (int)(splits == 1 ? n : whole);
+  int64_t units = 0, parts = 0;
+  for (int i = 0; i < a.n_seqs; ++i) {
+    QuerySeq& s = a.seq[i];
+    s.splits = splits;
+    a.unit0[i] = (int)units;
+    s.slot0 = (int)parts;
+    const int64_t u = (int64_t)a.h_kv * s.row_tiles * (a.whole > 0 ? 1 : splits);
+    units += u;
+    parts += u;
+  }
+  a.units = (int)(splits == 1 ? n : whole + rest * splits);
+  return splits == 1 ? 0 : rest;
+}
+
+template <int R, int D, typename Kernel>
+hipError_t launch(AttendArgs& a, void* ws, int64_t joins, Kernel kernel, int threads, int lds, bool bf16, hipStream_t st) {
+  if (joins < 0) return hipErrorInvalidConfiguration;
   a.part_o = static_cast<float*>(ws);
-  a.part_ml = reinterpret_cast<float2*>(a.part_o + (int64_t)(kPartBytes / (R * (D * 4 + 8))) * R * D);
-  if (units < 0) return hipErrorInvalidConfiguration;
-  hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(attend_simple<T, D>), hipFuncAttributeMaxDynamicSharedMemorySize, P::LDS);
+  a.part_ml = reinterpret_cast<float2*>(a.part_o + partials<R, D>() * R * D);
+  hipError_t e = hipSuccess;
+  if (lds > 65536) e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
   if (e != hipSuccess) return e;
-  attend_simple<T, D><<<units, 256, P::LDS, st>>>(a);
-  if ((e = hipGetLastError()) != hipSuccess) return e;
-  int joins = 0;
-  for (int i = 0; i < n; ++i)
-    if (a.seq[i].splits > 1) joins += a.h_kv * a.seq[i].row_tiles;
-  if (joins) join_splits<T, D, R><<<dim3(joins, R), 256, 0, st>>>(a);
+  kernel<<<a.units, threads, lds, st>>>(a);
+  if ((e = hipGetLastError()) != hipSuccess || joins == 0) return e;
+  if (bf16) join_splits<uint16_t, D, R><<<dim3((unsigned)joins, R), 256, 0, st>>>(a);
+  else join_splits<float, D, R><<<dim3((unsigned)joins, R), 256, 0, st>>>(a);
   return hipGetLastError();
+}
+
+template <int D, int NR>
+hipError_t attend_few_rows(AttendArgs& a, int cus, void* ws, hipStream_t st) {
+  using P = Few<D, NR>;
+  const int64_t joins = plan_shares<P::R, P::KT>(a, partials<P::R, D>(), 4, 2 * cus);
+  return launch<P::R, D>(a, ws, joins, attend_few<D, NR>, 256, P::LDS, true, st);
+}
+
+template <int D>
+hipError_t attend(const AttnDims& dm, AttendArgs& a, int cus, void* ws, hipStream_t st) {
+  if (dm.dtype == OMNIMEM_F32) {
+    using P = F32<D>;
+    const int64_t joins = plan_shares<P::R, P::KT>(a, partials<P::R, D>(), 1, 4 * cus);
+    return launch<P::R, D>(a, ws, joins, attend_f32<D>, 256, P::LDS, false, st);
+  }
+  int64_t rows = 0;
+  for (int i = 0; i < a.n_seqs; ++i) rows = std::max(rows, (int64_t)a.group * a.seq[i].nq);
+  if (rows <= 16) return attend_few_rows<D, 1>(a, cus, ws, st);
+  if (rows <= 64) return attend_few_rows<D, 2>(a, cus, ws, st);
+  using P = Many<D>;
+  const int64_t joins = plan_rounds<P::R, P::KT>(a, partials<P::R, D>(), cus);
+  return launch<P::R, D>(a, ws, joins, attend_many<D>, P::THREADS, P::LDS, true, st);
 }
 
 }  // namespace
@@ -343,9 +962,7 @@ hipError_t launch_attend(const AttnDims& dm, AttendArgs& a, int n, int compute_u
   a.n_seqs = n;
   a.h_kv = dm.h_kv;
   a.group = dm.group;
-  if (dm.dtype == OMNIMEM_BF16)
-    return dm.d == 128 ? attend<uint16_t, 128>(a, n, compute_units, ws, st) : attend<uint16_t, 64>(a, n, compute_units, ws, st);
-  return dm.d == 128 ? attend<float, 128>(a, n, compute_units, ws, st) : attend<float, 64>(a, n, compute_units, ws, st);
+  return dm.d == 128 ? attend<128>(dm, a, compute_units, ws, st) : attend<64>(dm, a, compute_units, ws, st);
 }
 
 }  // namespace omnimem

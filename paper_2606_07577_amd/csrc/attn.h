@@ -10,7 +10,7 @@ namespace omnimem {
 // Sequences described by one launch: their descriptors are kernel arguments
 // (of which a kernel may have 4 KiB), so a call needs no table on the device,
 // no copy before it, and can be captured as it is.
-constexpr int kSeqsPerLaunch = 16;
+constexpr int kSeqsPerLaunch = 16, kQueriesPerLaunch = 32;
 
 // ---------------------------------------------------------------------------
 // 4-bit memories: blocks of 32 rows and 34 d bytes.
@@ -28,27 +28,28 @@ constexpr uint32_t kScaleNan = 255;    // the scale byte of a group with an infi
 constexpr uint32_t kScaleMin = 7;      // 2^-120
 __device__ inline float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
 
-// The eight values (fp32) of a word of codes; NaN where the scale is kScaleNan.
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+__device__ inline uint2 gload8(const void* p) {
+  const u32x2 v = gload<u32x2>(p);
+  return make_uint2(v[0], v[1]);
+}
+
+// The eight values (fp32) of a word of codes (the conversions give NaN where
+// the scale is kScaleNan).
 __device__ inline void values8(uint32_t w, uint32_t byte, float (&x)[8]) {
   const float s = scale_of(byte);
   const floatx2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 1);
   const floatx2 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 3);
   x[0] = a[0]; x[1] = a[1]; x[2] = b[0]; x[3] = b[1]; x[4] = c[0]; x[5] = c[1]; x[6] = d[0]; x[7] = d[1];
-  if (byte == kScaleNan) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(0x7FC00000u);
-  }
 }
 // The same as eight bf16 values (each is exact: three significant bits and an
 // exponent of at least -121).
-__device__ inline uint4 values8_bf16(uint32_t w, uint32_t byte) {
-  const float s = scale_of(byte);
+__device__ inline uint4 values8_bf16(uint32_t w, float scale) {
   uint4 r;
-  r.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 0));
-  r.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 1));
-  r.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 2));
-  r.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 3));
-  if (byte == kScaleNan) r.x = r.y = r.z = r.w = 0x7FC07FC0u;
+  r.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0));
+  r.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1));
+  r.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2));
+  r.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3));
   return r;
 }
 
@@ -85,26 +86,28 @@ struct HeldArgs {
 struct QuerySeq {
   const void* q; const char* mem; const void* k; const void* v;
   void* out; float* lse;
-  int64_t q_hs, q_rs, mem_hs, kv_hs, kv_rs, out_hs, out_rs, lse_hs;
+  uint32_t q_hs, q_rs, mem_hs, kv_hs, kv_rs, out_hs, out_rs;   // units of 16 bytes
+  uint32_t lse_hs;             // elements
   float scale_log2;            // softmax scale times log2(e)
   int32_t nq, nm, nt;          // queries, memory rows, tail rows
-  int32_t row_tiles, splits;   // of its work (see AttendPlan)
-  int32_t unit0;               // its first unit of the launch
-  int32_t slot0;               // its first partial
+  int32_t row_tiles, splits;   // of its work, see below
+  int32_t slot0;               // its first partial (whole = 0)
 };
 // A call's work.  A KV head's query rows are numbered query-major (row
 // i * G + h is query i of the head's h-th query head: neighbouring rows see
-// the same keys, and share them), in tiles of R rows.  A row tile's keys
-// come in tiles of kKeyTile rows, the memory's and then the tail's; a unit
-// (one workgroup) is a row tile and `chunk` consecutive key tiles.  With more
-// than one unit to a row tile each writes a partial result (sums against its
-// own maximum) and the join puts them together, in the order of the keys.
-constexpr int kKeyTile = 128;
+// the same keys, and share them), in tiles of R rows; row tiles are numbered
+// over sequences, KV heads and rows.  A row tile's keys come in key tiles,
+// the memory's and then the tail's.  A unit (one workgroup) takes a row tile
+// and all its keys, or one of `splits` equal shares of them; then each writes
+// a partial result (sums against its own maximum) and the join puts them
+// together, in the order of the keys.  The first `whole` row tiles are not
+// split (with whole > 0 all others are by the same number).
 struct AttendArgs {
-  QuerySeq seq[kSeqsPerLaunch];
-  int n_seqs, h_kv, group, causal, chunk;
-  float* part_o;               // [slots][R][d] unnormalised sums
-  float2* part_ml;             // [slots][R] (maximum in log2 units, sum of weights)
+  QuerySeq seq[kQueriesPerLaunch];
+  int32_t unit0[kQueriesPerLaunch];   // a sequence's first unit after the whole row tiles (whole = 0), or row tile
+  int n_seqs, h_kv, group, causal, whole, units;
+  float* part_o;               // [partials][R][d] unnormalised sums
+  float2* part_ml;             // [partials][R] (maximum in log2 units, sum of weights)
 };
 static_assert(sizeof(RotateArgs) <= 3968 && sizeof(HeldArgs) <= 3968 && sizeof(AttendArgs) <= 3968,
               "a kernel's arguments, with what the runtime adds, stay below 4 KiB");
@@ -114,7 +117,7 @@ struct AttnDims {
 };
 hipError_t launch_rotate(const AttnDims& dm, const RotateArgs& a, int n, hipStream_t st);
 hipError_t launch_hold(const AttnDims& dm, const HeldArgs& a, int n, bool pack, hipStream_t st);
-constexpr int64_t kPartBytes = (int64_t)32 << 20;   // workspace of a handle
+constexpr int64_t kPartBytes = (int64_t)128 << 20;   // workspace of a handle
 // Fills the plan fields of `a` for n sequences and launches their attention.
 hipError_t launch_attend(const AttnDims& dm, AttendArgs& a, int n, int compute_units, void* workspace, hipStream_t st);
 

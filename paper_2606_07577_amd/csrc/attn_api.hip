@@ -81,11 +81,11 @@ bool overlap(const Span& a, const Span& b) {
   return true;
 }
 bool same(const Span& a, const Span& b) { return a.base == b.base && (a.hs == b.hs || a.heads == 1) && (a.rs == b.rs || a.rows == 1); }
-// Rows that are read: 16-byte units, rows of at least d.
+// Rows that are read: strides of 16-byte units below 64 GiB, rows of at least d.
 bool readable(const omnimem_attn* a, const void* p, int64_t hs, int64_t rs) {
   const int64_t e = (int64_t)elt(a);
   return p && aligned(p, 16) && hs >= 0 && rs >= a->cfg.head_dim && hs % (16 / e) == 0 && rs % (16 / e) == 0 &&
-         hs < ((int64_t)1 << 40) && rs < ((int64_t)1 << 31);
+         hs / (16 / e) <= UINT32_MAX && rs / (16 / e) <= UINT32_MAX;
 }
 // Rows that are written: each row of each head has its own place.
 bool writable(const omnimem_attn* a, const void* p, int64_t heads, int64_t rows, int64_t hs, int64_t rs) {
@@ -295,12 +295,13 @@ omnimem_status omnimem_attend(omnimem_attn* attn, const omnimem_query* seqs, int
       return fail(attn, OMNIMEM_ERR_INVALID_ARG, "sequence %d: k and v %s", i, kStride);
     const int64_t bytes = omnimem_memory_bytes(c.head_dim, s.memory_rows);
     if (s.memory_rows > 0 && (!s.memory || !aligned(s.memory, 16) || s.memory_head_stride % 16 || s.memory_head_stride < 0 ||
+                              s.memory_head_stride / 16 > UINT32_MAX ||
                               (H > 1 && s.memory_head_stride < bytes)))
       return bad(attn, i, "memory must be given, 16-byte aligned, its head stride a multiple of 16 and at least a head's bytes");
     if (!writable(attn, s.out, Hq, s.n_queries, s.out_head_stride, s.out_row_stride))
       return fail(attn, OMNIMEM_ERR_INVALID_ARG, "sequence %d: out %s, no two rows on one place", i, kStride);
-    if (s.lse && (!aligned(s.lse, 4) || (Hq > 1 && s.lse_head_stride < s.n_queries)))
-      return bad(attn, i, "lse must be 4-byte aligned, its head stride at least n_queries");
+    if (s.lse && (!aligned(s.lse, 4) || s.lse_head_stride < (Hq > 1 ? s.n_queries : 0) || s.lse_head_stride > UINT32_MAX))
+      return bad(attn, i, "lse must be 4-byte aligned, its head stride at least n_queries and below 2^32");
     const Span q = span(attn, s.q, Hq, s.n_queries, s.q_head_stride, s.q_row_stride);
     const Span o = span(attn, s.out, Hq, s.n_queries, s.out_head_stride, s.out_row_stride);
     bool clash = overlap(o, q);
@@ -313,19 +314,22 @@ omnimem_status omnimem_attend(omnimem_attn* attn, const omnimem_query* seqs, int
   }
   OnDevice dev(attn->device);
   hipError_t e = dev.err;
+  const int64_t per = 16 / (int64_t)elt(attn);
+  const auto units = [per](int64_t stride) { return (uint32_t)(stride / per); };
   for (int i0 = 0; i0 < n && e == hipSuccess;) {
     AttendArgs a;
     std::memset(&a, 0, sizeof a);
     a.causal = causal ? 1 : 0;
     int m = 0;
-    for (; i0 < n && m < kSeqsPerLaunch; ++i0) {
+    for (; i0 < n && m < kQueriesPerLaunch; ++i0) {
       const omnimem_query& s = seqs[i0];
       if (s.n_queries == 0) continue;
       QuerySeq& x = a.seq[m++];
       x.q = s.q; x.mem = static_cast<const char*>(s.memory); x.k = s.k; x.v = s.v; x.out = s.out; x.lse = s.lse;
-      x.q_hs = s.q_head_stride; x.q_rs = s.q_row_stride; x.mem_hs = s.memory_head_stride;
-      x.kv_hs = s.kv_head_stride; x.kv_rs = s.kv_row_stride;
-      x.out_hs = s.out_head_stride; x.out_rs = s.out_row_stride; x.lse_hs = s.lse_head_stride;
+      x.q_hs = units(s.q_head_stride); x.q_rs = units(s.q_row_stride);
+      x.kv_hs = units(s.kv_head_stride); x.kv_rs = units(s.kv_row_stride);
+      x.out_hs = units(s.out_head_stride); x.out_rs = units(s.out_row_stride);
+      x.mem_hs = (uint32_t)(s.memory_head_stride / 16); x.lse_hs = (uint32_t)s.lse_head_stride;
       const double scale = s.sm_scale != 0.0f ? (double)s.sm_scale : 1.0 / std::sqrt((double)c.head_dim);
       x.scale_log2 = (float)(scale * 1.4426950408889634);
       x.nq = (int32_t)s.n_queries; x.nm = (int32_t)s.memory_rows; x.nt = (int32_t)s.n_tail;

@@ -126,7 +126,7 @@ __device__ inline void store_channels(float* p, const float (&x)[CPL]) {
   for (int i = 0; i < CPL; ++i) p[i] = x[i];
 }
 __device__ inline void store_values(uint16_t* p, uint32_t w, uint32_t byte) {
-  *reinterpret_cast<uint4*>(p) = values8_bf16(w, byte);
+  *reinterpret_cast<uint4*>(p) = values8_bf16(w, scale_of(byte));
 }
 __device__ inline void store_values(float* p, uint32_t w, uint32_t byte) {
   float x[8];
