@@ -507,7 +507,7 @@ typedef struct {
   int64_t memory_rows;      /* 0 without a memory                              */
   const void* k;            /* [H_kv][n_tail][d], or NULL without tail rows    */
   const void* v;
-  int64_t kv_head_stride, kv_row_stride;   /* elements, shared by k and v      */
+  int64_t kv_head_stride, kv_row_stride;   /* elements, shared by k and v; rows less than 16 MiB apart */
   int64_t n_tail;
   float sm_scale;           /* 0 -> 1/sqrt(d)                                   */
   void* out;                /* [H_q][n_queries][d]                             */

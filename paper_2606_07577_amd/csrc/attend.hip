@@ -6,6 +6,8 @@
 // as they enter the second product, O^T = V^T P^T: an MFMA's sum runs over its
 // keys in any order, so K and V are read in the order that the accumulator
 // registers have.
+#include <type_traits>
+
 #include "../../include/omnimem.h"
 #include "attn.h"
 
@@ -36,13 +38,15 @@ struct Unit {
   int slot;                  // partial, or -1: the result is final
 };
 // The last sequence whose entry of `first` is at most u (lane-parallel).
-__device__ inline int seq_of(const int32_t* first, int n, int u) {
+template <int N>
+__device__ inline int seq_of(const int32_t (&first)[N], int n, int u) {
+  if constexpr (N == 1) return 0;
   const int lane = threadIdx.x & 63;
   const int v = lane < n ? first[lane] : INT32_MAX;
   return uniform(__popcll(__ballot(v <= u)) - 1);
 }
-template <int R, int KT>
-__device__ inline Unit unit_of(const AttendArgs& a, int u) {
+template <int R, int KT, int N>
+__device__ inline Unit unit_of(const AttendArgs<N>& a, int u) {
   Unit x;
   int split = 0, splits = 1, tile;
   x.slot = -1;
@@ -81,7 +85,8 @@ struct Row {
   bool live;
   int i, h, seen;
 };
-__device__ inline Row row_of(const AttendArgs& a, const QuerySeq& s, const Unit& x, int row) {
+template <int N>
+__device__ inline Row row_of(const AttendArgs<N>& a, const QuerySeq& s, const Unit& x, int row) {
   Row r;
   r.live = row < x.rows;
   r.i = r.live ? row / a.group : 0;
@@ -105,8 +110,8 @@ struct F32 {
   static constexpr int LDS = 2 * KT * ROW * 4 + 4 * R * 8;
 };
 
-template <int D>
-__global__ __launch_bounds__(256) void attend_f32(AttendArgs a) {
+template <int D, int N>
+__global__ __launch_bounds__(256) void attend_f32(AttendArgs<N> a) {
   using P = F32<D>;
   using M = Mfma<float>;
   constexpr int R = P::R, KT = P::KT, ROW = P::ROW, NCT = D / 32;
@@ -311,8 +316,8 @@ __device__ inline uint4 load_part(const char* p) {   // 16 or 8 bytes
   return make_uint4(x.x, x.y, 0, 0);
 }
 
-template <int D, int NR>
-__global__ __launch_bounds__(256, NR == 1 ? 2 : 1) void attend_few(AttendArgs a) {
+template <int D, int NR, int N>
+__global__ __launch_bounds__(256, D * NR == 256 ? 1 : 2) void attend_few(AttendArgs<N> a) {
   using P = Few<D, NR>;
   using B = MemBlock<D>;
   constexpr int R = P::R, KT = P::KT, NS = D / 32, NC = D / 16;
@@ -559,27 +564,127 @@ __global__ __launch_bounds__(256, NR == 1 ? 2 : 1) void attend_few(AttendArgs a)
 
 // ---------------------------------------------------------------------------
 // bf16, many rows (chunks): 256 query rows to a unit, 32 to each of eight
-// wavefronts, against key tiles of 64 rows that they share in LDS (two
-// stages: the next tile is on its way while one is multiplied).  Tail rows
-// are copied as they are, and V is transposed as it is read; a memory's codes
-// go through registers, K as rows and V, whose codes lie by channel, as
-// channels with their rows in the order that the weights have.
+// wavefronts, against key tiles of 64 rows that they share in LDS.  A step
+// multiplies K of the next tile while it turns this tile's scores to weights,
+// and then V of this tile: its MFMAs do not wait for its vector instructions.
+// Tail rows are copied to LDS as they are, and V is transposed as it is read;
+// a memory's codes go through registers, K as rows and V, whose codes lie by
+// channel, as channels with their rows in the order that the weights have.
 // ---------------------------------------------------------------------------
 template <int D>
 struct Many {
-  static constexpr int R = 256, KT = 64, THREADS = 512;
+  static constexpr int R = 256, KT = 64, WAVES = 8;
   static constexpr int TILE = KT * D;                      // elements of a K or V stage
   static constexpr int LDS = 4 * TILE * 2;
   static constexpr int CPR = D / 8;                        // 16-byte chunks per row
+  static constexpr int COPIES = CPR / WAVES;               // 1 KiB copies of a tile per wavefront
+  static constexpr int NKS = D / 16, NCT = D / 32;
   __device__ static inline int k_chunk(int r, int c) { return c ^ (r & (CPR - 1)); }
   __device__ static inline int v_chunk(int r, int c) { return D == 128 ? c ^ ((r & 3) << 2) : c ^ (((r >> 1) & 1) << 2); }
 };
 
 template <int D>
-__global__ __launch_bounds__(512, 2) void attend_many(AttendArgs a) {
+__device__ inline frag k_frag(const uint16_t* kd, int lane, int i) {   // i-th: keys i / NKS * 32 .., channels i % NKS * 16 ..
+  using P = Many<D>;
+  const int r = i / P::NKS * 32 + (lane & 31), c = 2 * (i % P::NKS) + (lane >> 5);
+  return *reinterpret_cast<const frag*>(kd + r * D + P::k_chunk(r, c) * 8);
+}
+template <int D, bool MEM>
+__device__ inline frag v_frag(const uint16_t* vd, int lane, int i) {   // i-th: keys i / NCT * 16 .., channels i % NCT * 32 ..
+  using P = Many<D>;
+  const int j = i / P::NCT, c = i % P::NCT, half = lane >> 5;
+  if constexpr (MEM) {
+    const int ch = c * 32 + (lane & 31);
+    return *reinterpret_cast<const frag*>(vd + ch * P::KT + ((2 * j + half) ^ (ch & 7)) * 8);
+  } else {
+    typedef __attribute__((address_space(3))) s16x4 lds4;
+    const int r = j * 16 + half * 4 + ((lane & 15) >> 2), ch = c * 32 + (lane & 16) + (lane & 3) * 4;
+    const uint16_t* p = vd + r * D + P::v_chunk(r, ch >> 3) * 8 + (ch & 7);   // (row r + 8 has the same chunks)
+    const uint2 x = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)p));
+    const uint2 y = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(p + 8 * D)));
+    return __builtin_bit_cast(frag, make_uint4(x.x, x.y, y.x, y.y));
+  }
+}
+
+// Weights of the 16-key steps of a tile from their scores, one value at a time
+// (value e of 32 is of step e / 8).
+struct Weights {
+  uint32_t w[4][4];
+  float even;
+  __device__ __forceinline__ void value(int e, const floatx16 (&s)[2], float scale, float ref, float& l) {
+    const float y = exp2_(__builtin_fmaf(s[e >> 4][e & 15], scale, -ref));
+    l += y;
+    pin(l);
+    if (e & 1) {
+      w[e >> 3][(e & 7) >> 1] = round2(even, y);
+      pin(w[e >> 3][(e & 7) >> 1]);
+    } else {
+      even = y;
+    }
+  }
+  __device__ inline frag step(int j) const { return __builtin_bit_cast(frag, make_uint4(w[j][0], w[j][1], w[j][2], w[j][3])); }
+};
+
+// One step: scores of the tile in kd into `next`, weights of the scores s and
+// their products with the tile in vd (MEM: by channel) into o, and the largest
+// next score (raw) of the lane.  The order of MFMAs, LDS reads (kAhead
+// fragments before their use) and vector instructions is that of the source.
+constexpr int kAhead = 4;
+template <int D, bool MEM>
+__device__ __forceinline__ float many_step(const uint16_t* kd, const uint16_t* vd, int lane, const frag (&q)[D / 16], floatx16 (&s)[2],
+                                  floatx16 (&next)[2], floatx16 (&o)[D / 32], float& l, float m, float scale, int limit, bool masked) {
+  using P = Many<D>;
+  constexpr int NK = 2 * P::NKS, NV = 4 * P::NCT;
+  const float ref = m == -INFINITY ? 0.0f : m;
+  Weights wt;
+  frag f[kAhead + 1];
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i) f[i] = k_frag<D>(kd, lane, i);
+#pragma unroll
+  for (int i = 0; i < NK; ++i) {
+    if (i + kAhead < NK) f[(i + kAhead) % (kAhead + 1)] = k_frag<D>(kd, lane, i + kAhead);
+    floatx16& x = next[i / P::NKS];
+    x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[i % (kAhead + 1)], q[i % P::NKS], i % P::NKS ? x : floatx16{}, 0, 0, 0);
+    pin(x);
+#pragma unroll
+    for (int e = 24 * i / NK; e < 24 * (i + 1) / NK; ++e) wt.value(e, s, scale, ref, l);
+  }
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i) f[i] = v_frag<D, MEM>(vd, lane, i);
+  if (masked) {
+    const int mine = limit - (lane >> 5) * 4;
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if (b * 32 + (r >> 2) * 8 + (r & 3) >= mine) next[b][r] = -INFINITY;
+  }
+  float top = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    if (i + kAhead < NV) f[(i + kAhead) % (kAhead + 1)] = v_frag<D, MEM>(vd, lane, i + kAhead);
+    floatx16& x = o[i % P::NCT];
+    x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[i % (kAhead + 1)], wt.step(i / P::NCT), x, 0, 0, 0);
+    pin(x);
+    if (i < NV / 2) {
+#pragma unroll
+      for (int e = 24 + 16 * i / NV; e < 24 + 16 * (i + 1) / NV; ++e) wt.value(e, s, scale, ref, l);
+    } else {
+#pragma unroll
+      for (int e = 32 * i / NV - 16; e < 32 * (i + 1) / NV - 16; ++e) {   // pairs of next scores
+        top = fmaxf(fmaxf(top, next[0][e]), next[1][e]);
+        pin(top);
+      }
+    }
+  }
+  return top;
+}
+
+template <int D, int N>
+__global__ __launch_bounds__(512, 2) void attend_many(AttendArgs<N> a) {
   using P = Many<D>;
   using B = MemBlock<D>;
-  constexpr int R = P::R, KT = P::KT, TILE = P::TILE, CPR = P::CPR, NKS = D / 16, NCT = D / 32;
+  constexpr int R = P::R, KT = P::KT, TILE = P::TILE, CPR = P::CPR, NKS = P::NKS, NCT = P::NCT;
   constexpr int W = D / 64;                                // code words per thread and operand of a memory tile
   extern __shared__ __align__(16) char lds[];
   uint16_t* kbuf = reinterpret_cast<uint16_t*>(lds);       // [2][TILE]
@@ -590,108 +695,88 @@ __global__ __launch_bounds__(512, 2) void attend_many(AttendArgs a) {
   const Unit x = unit_of<R, KT>(a, u);
   const QuerySeq& s = a.seq[x.s];
   const int tid = threadIdx.x, lane = tid & 63, wave = wave_id(), half = lane >> 5, col = lane & 31;
-  const Row row = row_of(a, s, x, x.rt * R + wave * 32 + col);
-  frag qf[NKS];
   const float scale = fabsf(s.scale_log2);
+  const Row row = row_of(a, s, x, x.rt * R + wave * 32 + col);
+  frag q[NKS];
   {
-    const uint16_t* q = static_cast<const uint16_t*>(s.q) + row.h * elems(s.q_hs, 2) + row.i * elems(s.q_rs, 2);
+    const uint16_t* p = static_cast<const uint16_t*>(s.q) + row.h * elems(s.q_hs, 2) + row.i * elems(s.q_rs, 2);
     const uint32_t flip = s.scale_log2 < 0.0f ? 0x80008000u : 0u;   // (a negative scale goes into the queries' signs)
 #pragma unroll
     for (int j = 0; j < NKS; ++j) {
-      uint4 w = row.live ? gload16(q + j * 16 + half * 8) : make_uint4(0, 0, 0, 0);
+      uint4 w = row.live ? gload16(p + j * 16 + half * 8) : make_uint4(0, 0, 0, 0);
       w.x ^= flip; w.y ^= flip; w.z ^= flip; w.w ^= flip;
-      qf[j] = __builtin_bit_cast(frag, w);
+      q[j] = __builtin_bit_cast(frag, w);
     }
   }
   floatx16 o[NCT];
 #pragma unroll
   for (int c = 0; c < NCT; ++c) o[c] = floatx16{};
-  float m = -INFINITY, l = 0.0f;                           // m: log2 units, the reference of the sums
+  float m = -INFINITY, l = 0.0f;                           // reference of the sums (log2 units), sum of weights
 
-  const int64_t rs = elems(s.kv_rs, 2);
-  const uint16_t* kp = static_cast<const uint16_t*>(s.k) + x.g * elems(s.kv_hs, 2);
-  const uint16_t* vp = static_cast<const uint16_t*>(s.v) + x.g * elems(s.kv_hs, 2);
+  const uint32_t rsb = s.kv_rs * 16u;                      // row stride in bytes, below 2^24
+  const char* kp = static_cast<const char*>(s.k) + x.g * ((int64_t)s.kv_hs * 16);
+  const char* vp = static_cast<const char*>(s.v) + x.g * ((int64_t)s.kv_hs * 16);
   const char* data = s.mem + x.g * ((int64_t)s.mem_hs * 16);
-  const int last_block = tiles_of<kMemRows>(s.nm) - 1;
-
-  uint32_t kw[W], vw[W], kb = 0, vb = 0;                   // a memory tile on its way
-  const int krow = tid / 8;                                // K: 8 threads to a row; V: 8 / W to a channel
-  const int vch = tid * W / 8, vt8 = tid * W % 8;          // (and the first of its words, of 8 rows each)
-  const auto fetch = [&](int t, int st) {
-    if (t < x.mem_tiles) {
-      const char* blk = data + (int64_t)min(t * 2 + krow / 32, last_block) * B::BYTES;
-      const int r = krow & 31, p = tid & 7;
-      const char* vk = data + (int64_t)min(t * 2 + vt8 / 4, last_block) * B::BYTES;
-      if constexpr (W == 2) {
-        const uint2 k2 = gload8(blk + r * (D / 2) + p * 8), v2 = gload8(vk + B::V + vch * 16 + vt8 % 4 * 4);
-        kw[0] = k2.x; kw[1] = k2.y; vw[0] = v2.x; vw[1] = v2.y;
-      } else {
-        kw[0] = gload<uint32_t>(blk + r * (D / 2) + p * 4);
-        vw[0] = gload<uint32_t>(vk + B::V + vch * 16 + vt8 % 4 * 4);
-      }
-      kb = gload<uint8_t>(blk + B::k_scale(r, p * (D / 8) / 32));
-      vb = gload<uint8_t>(vk + B::v_scale(vch));
-    } else {
-      const int key0 = (t - x.mem_tiles) * KT;
+  const int mem_tiles = x.mem_tiles, nt = s.nt, nm = s.nm;
+  const int last_block = tiles_of<kMemRows>(nm) - 1;
+  // tail copies: lane / CPR is the row of a copy's 64 / CPR rows, lane % CPR its chunk
+  const uint32_t lane_row = lane / CPR, lane_off = lane_row * rsb;
+  const auto copy = [&](const char* base, uint16_t* to, int t, bool is_k) __attribute__((always_inline)) {
+    const int key0 = (t - mem_tiles) * KT, keys = nt - key0;
+    const char* tile = base + (int64_t)key0 * rsb;
 #pragma unroll
-      for (int j = 0; j < CPR / 8; ++j) {
-        const int J = wave * (CPR / 8) + j, slot = J * 64 + lane, r = slot / CPR, c = slot % CPR;
-        const int64_t at = min(key0 + r, s.nt - 1) * rs;
-        dma16_opaque(kp + at + P::k_chunk(r, c) * 8, kbuf + st * TILE + J * 512);
-        dma16_opaque(vp + at + P::v_chunk(r, c) * 8, vbuf + st * TILE + J * 512);
-      }
+    for (int j = 0; j < P::COPIES; ++j) {
+      const int J = wave * P::COPIES + j, r0 = J * (64 / CPR), r = r0 + lane_row, c = lane % CPR;
+      const uint32_t chunk = (is_k ? P::k_chunk(r, c) : P::v_chunk(r, c)) * 16;
+      if (keys >= KT) dma16_opaque_s(tile + (int64_t)r0 * rsb, lane_off + chunk, to + J * 512);
+      else dma16_opaque_s(tile, (uint32_t)min(r, keys - 1) * rsb + chunk, to + J * 512);
     }
   };
-  const auto store = [&](int t, int st) {
-    if (t >= x.mem_tiles) return;
-    uint16_t* kd = kbuf + st * TILE;
-    uint16_t* vd = vbuf + st * TILE;
+  // a memory tile on its way: K by rows, 8 threads to one; V by channels, 8 / W threads to one
+  uint32_t kw[W], vw[W], kb = 0, vb = 0;
+  const int krow = tid / 8, vch = tid * W / 8, vt8 = tid * W % 8;
+  const auto words = [&](const char* p, uint32_t (&w)[W]) __attribute__((always_inline)) {
+    if constexpr (W == 2) {
+      const uint2 y = gload8(p);
+      w[0] = y.x; w[1] = y.y;
+    } else {
+      w[0] = gload<uint32_t>(p);
+    }
+  };
+  const auto fetch_k = [&](int t, int st) __attribute__((always_inline)) {
+    if (t >= mem_tiles) { copy(kp, kbuf + st * TILE, t, true); return; }
+    const char* p = data + (int64_t)min(t * 2 + krow / 32, last_block) * B::BYTES;
+    words(p + (krow & 31) * (D / 2) + (tid & 7) * (D / 16), kw);
+    kb = gload<uint8_t>(p + B::k_scale(krow & 31, (tid & 7) * (D / 8) / 32));
+  };
+  const auto fetch_v = [&](int t, int st) __attribute__((always_inline)) {
+    if (t >= mem_tiles) { copy(vp, vbuf + st * TILE, t, false); return; }
+    const char* p = data + (int64_t)min(t * 2 + vt8 / 4, last_block) * B::BYTES;
+    words(p + B::V + vch * 16 + vt8 % 4 * 4, vw);
+    vb = gload<uint8_t>(p + B::v_scale(vch));
+  };
+  const auto store_k = [&](int t, int st) __attribute__((always_inline)) {
+    if (t >= mem_tiles) return;
+    uint16_t* p = kbuf + st * TILE + krow * D;
+#pragma unroll
+    for (int j = 0; j < W; ++j)
+      *reinterpret_cast<uint4*>(p + P::k_chunk(krow, (tid & 7) * W + j) * 8) = values8_bf16(kw[j], scale_of(kb));
+  };
+  const auto store_v = [&](int t, int st) __attribute__((always_inline)) {
+    if (t >= mem_tiles) return;
 #pragma unroll
     for (int j = 0; j < W; ++j) {
-      *reinterpret_cast<uint4*>(kd + krow * D + P::k_chunk(krow, (tid & 7) * W + j) * 8) = values8_bf16(kw[j], scale_of(kb));
       const uint4 y = values8_bf16(vw[j], scale_of(vb));
-      const int t8 = vt8 + j;                    // rows 8 t8 .. of the tile: 16-row step t8 / 2
-      uint16_t* p = vd + vch * KT + (t8 & 1) * 4;
-      *reinterpret_cast<uint2*>(p + (((t8 >> 1) * 2) ^ (vch & 7)) * 8) = make_uint2(y.x, y.y);
-      *reinterpret_cast<uint2*>(p + (((t8 >> 1) * 2 + 1) ^ (vch & 7)) * 8) = make_uint2(y.z, y.w);
+      const int t8 = vt8 + j, c = t8 >> 1 << 1;            // rows 8 t8 .. of the tile, in the 16-row step t8 / 2
+      uint16_t* p = vbuf + st * TILE + vch * KT + (t8 & 1) * 4;
+      *reinterpret_cast<uint2*>(p + (c ^ (vch & 7)) * 8) = make_uint2(y.x, y.y);
+      *reinterpret_cast<uint2*>(p + ((c + 1) ^ (vch & 7)) * 8) = make_uint2(y.z, y.w);
     }
   };
-
-  if (x.k0 < x.k1) {
-    fetch(x.k0, 0);
-    store(x.k0, 0);
-  }
-  dma_wait();
-  __syncthreads();
-  for (int t = x.k0; t < x.k1; ++t) {
-    const int st = (t - x.k0) & 1;
-    const bool in_mem = t < x.mem_tiles;
-    if (t + 1 < x.k1) fetch(t + 1, st ^ 1);
-    const uint16_t* kd = kbuf + st * TILE;
-    const uint16_t* vd = vbuf + st * TILE;
-    floatx16 sc[2];
-#pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      sc[b] = floatx16{};
-#pragma unroll
-      for (int j = 0; j < NKS; ++j) {
-        const int r = b * 32 + col;
-        const frag kf = *reinterpret_cast<const frag*>(kd + r * D + P::k_chunk(r, 2 * j + half) * 8);
-        sc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[j], sc[b], 0, 0, 0);
-      }
-    }
-    const int key0 = (in_mem ? t : t - x.mem_tiles) * KT;
-    const int limit = (in_mem ? (row.live ? s.nm : 0) : row.seen) - key0;
-    if (__any(limit < KT)) {
-#pragma unroll
-      for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (b * 32 + acc_row(r, lane) >= limit) sc[b][r] = -INFINITY;
-    }
-    float top = -INFINITY;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) top = fmaxf(fmaxf(top, sc[0][r]), sc[1][r]);
+  const auto limit_of = [&](int t) __attribute__((always_inline)) {                       // keys of tile t that the lane's query sees
+    return t < mem_tiles ? nm - t * KT : row.seen - (t - mem_tiles) * KT;
+  };
+  const auto raise = [&](float top) __attribute__((always_inline)) {                      // largest raw score of the tile to come
     top = fmaxf(top, __shfl_xor(top, 32)) * scale;
     // The sums keep their reference until a score passes it by 8: weights stay below 2^8, and few tiles scale O.
     if (__any(top > m + 8.0f)) {
@@ -702,49 +787,65 @@ __global__ __launch_bounds__(512, 2) void attend_many(AttendArgs a) {
 #pragma unroll
       for (int c = 0; c < NCT; ++c) o[c] *= alpha;
     }
-    const float ref = m == -INFINITY ? 0.0f : m;
-    frag pf[4];
-#pragma unroll
-    for (int b = 0; b < 2; ++b) {
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        sc[b][r] = exp2_(__builtin_fmaf(sc[b][r], scale, -ref));
-        l += sc[b][r];
-      }
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        uint32_t w[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) w[e] = round2(sc[b][j * 8 + 2 * e], sc[b][j * 8 + 2 * e + 1]);
-        pf[b * 2 + j] = __builtin_bit_cast(frag, make_uint4(w[0], w[1], w[2], w[3]));
-      }
+  };
+
+  if (x.k0 < x.k1) {
+    const int k0 = x.k0, k1 = x.k1;
+    fetch_k(k0, 0);
+    fetch_v(k0, 0);
+    store_k(k0, 0);
+    store_v(k0, 0);
+    if (k0 + 1 < k1) {
+      fetch_k(k0 + 1, 1);
+      store_k(k0 + 1, 1);
     }
-    if (in_mem) {
-#pragma unroll
-      for (int c = 0; c < NCT; ++c)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int ch = c * 32 + col;
-          const frag vf = *reinterpret_cast<const frag*>(vd + ch * KT + ((2 * j + half) ^ (ch & 7)) * 8);
-          o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[j], o[c], 0, 0, 0);
-        }
-    } else {
-#pragma unroll
-      for (int c = 0; c < NCT; ++c)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int r = j * 16 + half * 4 + ((lane & 15) >> 2), ch = c * 32 + (lane & 16) + (lane & 3) * 4;
-          const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-              (__attribute__((address_space(3))) s16x4*)(vd + r * D + P::v_chunk(r, ch >> 3) * 8 + (ch & 7)));
-          const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-              (__attribute__((address_space(3))) s16x4*)(vd + (r + 8) * D + P::v_chunk(r + 8, ch >> 3) * 8 + (ch & 7)));
-          const uint2 x0 = __builtin_bit_cast(uint2, lo), x1 = __builtin_bit_cast(uint2, hi);
-          o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(frag, make_uint4(x0.x, x0.y, x1.x, x1.y)), pf[j], o[c], 0, 0, 0);
-        }
-    }
-    if (t + 1 < x.k1) store(t + 1, st ^ 1);
     dma_wait();
     __syncthreads();
+    floatx16 s0[2], s1[2];
+    {  // scores of the first tile
+      s0[0] = s0[1] = floatx16{};
+#pragma unroll
+      for (int i = 0; i < 2 * NKS; ++i)
+        s0[i / NKS] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_frag<D>(kbuf, lane, i), q[i % NKS], s0[i / NKS], 0, 0, 0);
+      const int mine = limit_of(k0) - half * 4;
+      float top = -INFINITY;
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          if (b * 32 + (r >> 2) * 8 + (r & 3) >= mine) s0[b][r] = -INFINITY;
+          top = fmaxf(top, s0[b][r]);
+        }
+      raise(top);
+      __syncthreads();
+    }
+    const auto step = [&](auto mem, int t, floatx16 (&sc)[2], floatx16 (&next)[2]) __attribute__((always_inline)) {
+      const int st = (t - k0) & 1;                         // (every wavefront is done with K of tile t and V of tile t - 1)
+      if (t + 2 < k1) fetch_k(t + 2, st);
+      if (t + 1 < k1) fetch_v(t + 1, st ^ 1);
+      const int limit = limit_of(t + 1);
+      const float top = many_step<D, decltype(mem)::value>(kbuf + (st ^ 1) * TILE, vbuf + st * TILE, lane, q, sc, next, o, l, m, scale,
+                                                           limit, __any(limit < KT));
+      if (t + 1 < k1) raise(top);
+      if (t + 2 < k1) store_k(t + 2, st);
+      if (t + 1 < k1) store_v(t + 1, st ^ 1);
+      dma_wait();
+      __syncthreads();
+    };
+    const auto steps = [&](auto mem, int t, int end) __attribute__((always_inline)) {     // (two at a time: scores stay where they are)
+      for (; t + 1 < end; t += 2) {
+        step(mem, t, s0, s1);
+        step(mem, t + 1, s1, s0);
+      }
+      if (t < end) {
+        step(mem, t, s0, s1);
+        s0[0] = s1[0];
+        s0[1] = s1[1];
+      }
+    };
+    const int mid = min(max(mem_tiles, k0), k1);
+    steps(std::true_type{}, k0, mid);
+    steps(std::false_type{}, mid, k1);
   }
   l += __shfl_xor(l, 32);
   if (x.slot >= 0) {
@@ -768,82 +869,108 @@ __global__ __launch_bounds__(512, 2) void attend_many(AttendArgs a) {
 }
 
 // ---------------------------------------------------------------------------
-// Puts the partial results of a query row's splits together: a workgroup per
-// row, D/4 threads to a partial.
+// Puts the partial results of query rows' splits together.  SHARES threads to a
+// row and 4 channels: one for few splits (it has all its loads on their way at
+// once), 4 or a whole workgroup of 1024 threads that share out more.
 // ---------------------------------------------------------------------------
-template <typename T, int D, int R>
-__global__ __launch_bounds__(256) void join_splits(AttendArgs a) {
-  constexpr int TPR = D / 4, PAR = 256 / TPR;
-  __shared__ floatx4 sums[PAR][TPR];
-  __shared__ float ls[PAR];
-  __shared__ float tops[4];
-  const int lane = threadIdx.x & 63;
-  int si, tile;
+struct JoinTile {
+  int s, g, rt, splits;
   int64_t slot;
+};
+template <int N>
+__device__ inline JoinTile split_tile(const AttendArgs<N>& a, int j) {   // the j-th row tile with splits
+  const int lane = threadIdx.x & 63;
+  JoinTile x;
+  int tile;
   if (a.whole > 0) {
-    tile = a.whole + blockIdx.x;
-    si = seq_of(a.unit0, a.n_seqs, tile);
-    tile -= a.unit0[si];
-    slot = (int64_t)blockIdx.x * a.seq[0].splits;
+    tile = a.whole + j;
+    x.s = seq_of(a.unit0, a.n_seqs, tile);
+    tile -= a.unit0[x.s];
+    x.slot = (int64_t)j * a.seq[0].splits;
   } else {
-    int first = lane < a.n_seqs && a.seq[lane].splits > 1 ? a.h_kv * a.seq[lane].row_tiles : 0;
+    int first = lane < N && lane < a.n_seqs && a.seq[lane].splits > 1 ? a.h_kv * a.seq[lane].row_tiles : 0;
     const int count = first;
-    for (int k = 1; k < kQueriesPerLaunch; k *= 2) {
+    for (int k = 1; k < N; k *= 2) {
       const int y = __shfl_up(first, k);
       if (lane >= k) first += y;
     }
     first -= count;                              // split row tiles of the sequences before
-    const uint64_t at = __ballot(count > 0 && first <= (int)blockIdx.x);
-    si = uniform(63 - __clzll((long long)at));
-    tile = blockIdx.x - uniform(__shfl(first, si));
-    slot = a.seq[si].slot0 + (int64_t)tile * a.seq[si].splits;
+    const uint64_t at = __ballot(count > 0 && first <= j);
+    x.s = uniform(63 - __clzll((long long)at));
+    tile = j - uniform(__shfl(first, x.s));
+    x.slot = a.seq[x.s].slot0 + (int64_t)tile * a.seq[x.s].splits;
   }
-  const QuerySeq& s = a.seq[si];
-  const int splits = s.splits;
-  const int rt = s.row_tiles - 1 - tile % s.row_tiles, g = tile / s.row_tiles;
-  const int row = rt * R + blockIdx.y;
-  if (row >= a.group * s.nq) return;
-  const int i = row / a.group, h = g * a.group + row % a.group;
-  const float2* ml = a.part_ml + slot * R + blockIdx.y;
-  float m = -INFINITY;
-  for (int p = threadIdx.x; p < splits; p += 256) m = fmaxf(m, gload<float>(&ml[(int64_t)p * R].x));
-#pragma unroll
-  for (int k = 1; k < 64; k *= 2) m = fmaxf(m, __shfl_xor(m, k));
-  if (lane == 0) tops[threadIdx.x >> 6] = m;
-  __syncthreads();
-  m = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
-  const float ref = m == -INFINITY ? 0.0f : m;
-  const int c = threadIdx.x % TPR, p0 = threadIdx.x / TPR;
-  floatx4 o = floatx4{};
-  float l = 0.0f;
-  for (int p = p0; p < splits; p += PAR) {
-    const floatx2 x = gload<floatx2>(&ml[(int64_t)p * R]);
-    const float w = exp2_(x[0] - ref);
-    l += w * x[1];
-    o += w * gload<floatx4>(a.part_o + ((slot + p) * R + blockIdx.y) * D + c * 4);
-  }
-  sums[p0][c] = o;
-  if (c == 0) ls[p0] = l;
-  __syncthreads();
-  if (threadIdx.x >= TPR) return;
-  l = 0.0f;
-  o = floatx4{};
-#pragma unroll
-  for (int p = 0; p < PAR; ++p) { o += sums[p][c]; l += ls[p]; }
-  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+  const QuerySeq& s = a.seq[x.s];
+  x.splits = s.splits;
+  x.rt = s.row_tiles - 1 - tile % s.row_tiles;
+  x.g = tile / s.row_tiles;
+  return x;
+}
+
+template <typename T, int D, int R, int SHARES, int THREADS, int N>
+__global__ __launch_bounds__(THREADS) void join_splits(AttendArgs<N> a) {
+  constexpr int TPR = D / 4, ROWS = THREADS / TPR / SHARES; // rows per workgroup
   constexpr int E = (int)sizeof(T);
-  put4(static_cast<T*>(s.out) + h * elems(s.out_hs, E) + i * elems(s.out_rs, E) + c * 4, o * inv);
+  const JoinTile x = split_tile(a, blockIdx.x);
+  const QuerySeq& s = a.seq[x.s];
+  const int c = threadIdx.x % TPR * 4, share = threadIdx.x / TPR % SHARES, r = blockIdx.y * ROWS + threadIdx.x / TPR / SHARES;
+  const int row = x.rt * R + r;
+  const bool live = row < a.group * s.nq;
+  if (__syncthreads_or(live) == 0) return;
+  const float2* ml = a.part_ml + x.slot * R + r;
+  const float* po = a.part_o + (x.slot * R + r) * D + c;
+  float m = -INFINITY, l = 0.0f;
+  floatx4 o = floatx4{};
+  if (live) {
+#pragma unroll 4
+    for (int p = share; p < x.splits; p += SHARES) {
+      const floatx2 y = gload<floatx2>(ml + (int64_t)p * R);
+      const floatx4 z = gload<floatx4>(po + (int64_t)p * R * D);
+      const float m2 = fmaxf(m, y[0]), ref = m2 == -INFINITY ? 0.0f : m2;
+      const float was = exp2_(m - ref), is = exp2_(y[0] - ref);
+      l = l * was + y[1] * is;
+      o = o * was + z * is;
+      m = m2;
+    }
+  }
+  if constexpr (SHARES > 1) {
+    __shared__ floatx4 os[THREADS];
+    __shared__ float2 mls[THREADS];
+    os[threadIdx.x] = o;
+    mls[threadIdx.x] = make_float2(m, l);
+    __syncthreads();
+    if (share != 0) return;
+    float top = -INFINITY;
+#pragma unroll
+    for (int p = 0; p < SHARES; ++p) top = fmaxf(top, mls[threadIdx.x + p * TPR].x);
+    const float ref = top == -INFINITY ? 0.0f : top;
+    o = floatx4{};
+    l = 0.0f;
+#pragma unroll
+    for (int p = 0; p < SHARES; ++p) {
+      const float w = exp2_(mls[threadIdx.x + p * TPR].x - ref);
+      l += mls[threadIdx.x + p * TPR].y * w;
+      o += os[threadIdx.x + p * TPR] * w;
+    }
+    m = top;
+  }
+  if (!live) return;
+  const int i = row / a.group, h = x.g * a.group + row % a.group;
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+  put4(static_cast<T*>(s.out) + h * elems(s.out_hs, E) + i * elems(s.out_rs, E) + c, o * inv);
   if (c == 0 && s.lse) s.lse[h * (int64_t)s.lse_hs + i] = log_of(m, l);
 }
 
 // ---------------------------------------------------------------------------
 // Plans and launches.
 // ---------------------------------------------------------------------------
+using Args = AttendArgs<kQueriesPerLaunch>;
+
 template <int R, int D>
 constexpr int64_t partials() { return kPartBytes / (R * (D * 4 + 8)); }
 
 template <int R, int KT>
-int64_t count_tiles(AttendArgs& a, int64_t* keys) {
+int64_t count_tiles(Args& a, int64_t* keys) {
   int64_t n = 0;
   *keys = 0;
   for (int i = 0; i < a.n_seqs; ++i) {
@@ -858,7 +985,7 @@ int64_t count_tiles(AttendArgs& a, int64_t* keys) {
 // Key tiles in shares of about `share`, or as many more as leave about
 // `target` units, or no more partials than the workspace holds.
 template <int R, int KT>
-int64_t plan_shares(AttendArgs& a, int64_t slots, int64_t share, int64_t target) {
+int64_t plan_shares(Args& a, int64_t slots, int64_t share, int64_t target) {
   int64_t keys;
   count_tiles<R, KT>(a, &keys);
   a.whole = 0;
@@ -887,19 +1014,22 @@ int64_t plan_shares(AttendArgs& a, int64_t slots, int64_t share, int64_t target)
 }
 
 // As many whole row tiles as fill the chip a number of times, and the rest in
-// so many shares that they fill it once more.
+// so many shares that it takes least: rounds of a share's key tiles, with
+// about 3 more to begin and end it, and the join, which moves a partial in
+// about 0.03 of a key tile's time and costs 3 to launch.
 template <int R, int KT>
-int64_t plan_rounds(AttendArgs& a, int64_t slots, int width) {
+int64_t plan_rounds(Args& a, int64_t slots, int width) {
   int64_t keys;
   const int64_t n = count_tiles<R, KT>(a, &keys);
-  if (n > INT32_MAX / 16) return -1;
+  if (n > INT32_MAX / 64) return -1;
   const int64_t whole = n / width * width, rest = n - whole;
   int splits = 1;
   if (rest > 0) {
-    const int64_t most = std::max<int64_t>(1, std::min(slots / rest, keys / n / 4));   // (a share is some tiles at least)
+    const double tiles = (double)keys / n;
+    const int64_t most = std::max<int64_t>(1, std::min<int64_t>(slots / rest, 512));
     double best = 1e30;
-    for (int c = 1; c <= std::min<int64_t>(most, 64); ++c) {
-      const double cost = (double)((rest * c + width - 1) / width) / c + 0.01 * c;
+    for (int c = 1; c <= most && c <= tiles; ++c) {
+      const double cost = (double)((rest * c + width - 1) / width) * (tiles / c + 3) + (c > 1 ? 3 + 0.03 * rest * c : 0);
       if (cost < best) { best = cost; splits = c; }
     }
   }
@@ -918,47 +1048,71 @@ int64_t plan_rounds(AttendArgs& a, int64_t slots, int width) {
   return splits == 1 ? 0 : rest;
 }
 
-template <int R, int D, typename Kernel>
-hipError_t launch(AttendArgs& a, void* ws, int64_t joins, Kernel kernel, int threads, int lds, bool bf16, hipStream_t st) {
-  if (joins < 0) return hipErrorInvalidConfiguration;
-  a.part_o = static_cast<float*>(ws);
-  a.part_ml = reinterpret_cast<float2*>(a.part_o + partials<R, D>() * R * D);
+template <typename T, int D, int R, int SHARES, int THREADS, int N>
+void join(const AttendArgs<N>& a, int64_t joins, hipStream_t st) {
+  constexpr int ROWS = THREADS / (D / 4) / SHARES;
+  join_splits<T, D, R, SHARES, THREADS, N><<<dim3((unsigned)joins, R / ROWS), THREADS, 0, st>>>(a);
+}
+
+template <typename T, int D, int R, int N, typename Kernel>
+hipError_t launch(const AttendArgs<N>& a, int64_t joins, Kernel kernel, int threads, int lds, hipStream_t st) {
   hipError_t e = hipSuccess;
   if (lds > 65536) e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
   if (e != hipSuccess) return e;
   kernel<<<a.units, threads, lds, st>>>(a);
   if ((e = hipGetLastError()) != hipSuccess || joins == 0) return e;
-  if (bf16) join_splits<uint16_t, D, R><<<dim3((unsigned)joins, R), 256, 0, st>>>(a);
-  else join_splits<float, D, R><<<dim3((unsigned)joins, R), 256, 0, st>>>(a);
+  int splits = 0;
+  for (int i = 0; i < a.n_seqs; ++i) splits = std::max(splits, a.seq[i].splits);
+  if (splits <= 8) join<T, D, R, 1, 256, N>(a, joins, st);
+  else if (splits <= 32 || R == 256) join<T, D, R, 4, 256, N>(a, joins, st);
+  else join<T, D, R, 1024 / (D / 4), 1024, N>(a, joins, st);
   return hipGetLastError();
 }
 
+// The kernel with room for one sequence, or for all that a launch describes.
+template <typename T, int D, int R, typename One, typename All>
+hipError_t launch(Args& a, void* ws, int64_t joins, One one, All all, int threads, int lds, hipStream_t st) {
+  if (joins < 0) return hipErrorInvalidConfiguration;
+  a.part_o = static_cast<float*>(ws);
+  a.part_ml = reinterpret_cast<float2*>(a.part_o + partials<R, D>() * R * D);
+  if (a.n_seqs > 1) return launch<T, D, R, kQueriesPerLaunch>(a, joins, all, threads, lds, st);
+  AttendArgs<1> x;
+  x.seq[0] = a.seq[0];
+  x.unit0[0] = a.unit0[0];
+  x.n_seqs = 1; x.h_kv = a.h_kv; x.group = a.group; x.causal = a.causal; x.whole = a.whole; x.units = a.units;
+  x.part_o = a.part_o; x.part_ml = a.part_ml;
+  return launch<T, D, R, 1>(x, joins, one, threads, lds, st);
+}
+
 template <int D, int NR>
-hipError_t attend_few_rows(AttendArgs& a, int cus, void* ws, hipStream_t st) {
+hipError_t attend_few_rows(Args& a, int cus, void* ws, hipStream_t st) {
   using P = Few<D, NR>;
-  const int64_t joins = plan_shares<P::R, P::KT>(a, partials<P::R, D>(), 4, 2 * cus);
-  return launch<P::R, D>(a, ws, joins, attend_few<D, NR>, 256, P::LDS, true, st);
+  const int64_t joins = plan_shares<P::R, P::KT>(a, partials<P::R, D>(), 4, 3 * cus);
+  return launch<uint16_t, D, P::R>(a, ws, joins, attend_few<D, NR, 1>, attend_few<D, NR, kQueriesPerLaunch>, 256, P::LDS, st);
 }
 
 template <int D>
-hipError_t attend(const AttnDims& dm, AttendArgs& a, int cus, void* ws, hipStream_t st) {
+hipError_t attend(const AttnDims& dm, Args& a, int cus, void* ws, hipStream_t st) {
   if (dm.dtype == OMNIMEM_F32) {
     using P = F32<D>;
     const int64_t joins = plan_shares<P::R, P::KT>(a, partials<P::R, D>(), 1, 4 * cus);
-    return launch<P::R, D>(a, ws, joins, attend_f32<D>, 256, P::LDS, false, st);
+    return launch<float, D, P::R>(a, ws, joins, attend_f32<D, 1>, attend_f32<D, kQueriesPerLaunch>, 256, P::LDS, st);
   }
-  int64_t rows = 0;
+  int64_t rows = 0, keys = 0;
   for (int i = 0; i < a.n_seqs; ++i) rows = std::max(rows, (int64_t)a.group * a.seq[i].nq);
   if (rows <= 16) return attend_few_rows<D, 1>(a, cus, ws, st);
-  if (rows <= 64) return attend_few_rows<D, 2>(a, cus, ws, st);
+  // Up to 8192 / d rows of every head, and further where that leaves a wavefront at most 896 / d tiles of 32 rows
+  // and 128 keys for each compute unit, the few-row kernel.
+  count_tiles<32, 128>(a, &keys);
+  if (rows <= 8192 / D || keys <= 896 / D * cus) return attend_few_rows<D, 2>(a, cus, ws, st);
   using P = Many<D>;
   const int64_t joins = plan_rounds<P::R, P::KT>(a, partials<P::R, D>(), cus);
-  return launch<P::R, D>(a, ws, joins, attend_many<D>, P::THREADS, P::LDS, true, st);
+  return launch<uint16_t, D, P::R>(a, ws, joins, attend_many<D, 1>, attend_many<D, kQueriesPerLaunch>, 512, P::LDS, st);
 }
 
 }  // namespace
 
-hipError_t launch_attend(const AttnDims& dm, AttendArgs& a, int n, int compute_units, void* ws, hipStream_t st) {
+hipError_t launch_attend(const AttnDims& dm, AttendArgs<kQueriesPerLaunch>& a, int n, int compute_units, void* ws, hipStream_t st) {
   a.n_seqs = n;
   a.h_kv = dm.h_kv;
   a.group = dm.group;

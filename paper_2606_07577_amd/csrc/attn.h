@@ -9,8 +9,10 @@ namespace omnimem {
 
 // Sequences described by one launch: their descriptors are kernel arguments
 // (of which a kernel may have 4 KiB), so a call needs no table on the device,
-// no copy before it, and can be captured as it is.
-constexpr int kSeqsPerLaunch = 16, kQueriesPerLaunch = 32;
+// no copy before it, and can be captured as it is.  The host writes arguments
+// to device memory; a call for one sequence has a kernel with room for one
+// (rotation of a token, 3 KB and 0.9 KB of arguments: RTIME).
+constexpr int kRotatesPerLaunch = 16, kHeldPerLaunch = 64, kQueriesPerLaunch = 32;
 
 // ---------------------------------------------------------------------------
 // 4-bit memories: blocks of 32 rows and 34 d bytes.
@@ -65,8 +67,9 @@ struct RotateSeq {
   int64_t q_hs, q_rs, kv_hs, kv_rs, pos_s, qo_hs, qo_rs, o_hs, o_rs;
   int64_t n;
 };
+template <int N>
 struct RotateArgs {
-  RotateSeq seq[kSeqsPerLaunch];
+  RotateSeq seq[N];
   double turns[64];            // inv_freq / 2 pi
   uint8_t axis[64];
   const void* q_w; const void* k_w;
@@ -80,7 +83,7 @@ struct HeldSeq {
   int64_t n;
 };
 struct HeldArgs {
-  HeldSeq seq[kSeqsPerLaunch];
+  HeldSeq seq[kHeldPerLaunch];
 };
 
 struct QuerySeq {
@@ -102,23 +105,25 @@ struct QuerySeq {
 // a partial result (sums against its own maximum) and the join puts them
 // together, in the order of the keys.  The first `whole` row tiles are not
 // split (with whole > 0 all others are by the same number).
+template <int N>
 struct AttendArgs {
-  QuerySeq seq[kQueriesPerLaunch];
-  int32_t unit0[kQueriesPerLaunch];   // a sequence's first unit after the whole row tiles (whole = 0), or row tile
+  QuerySeq seq[N];
+  int32_t unit0[N];            // a sequence's first unit after the whole row tiles (whole = 0), or row tile
   int n_seqs, h_kv, group, causal, whole, units;
   float* part_o;               // [partials][R][d] unnormalised sums
   float2* part_ml;             // [partials][R] (maximum in log2 units, sum of weights)
 };
-static_assert(sizeof(RotateArgs) <= 3968 && sizeof(HeldArgs) <= 3968 && sizeof(AttendArgs) <= 3968,
+static_assert(sizeof(RotateArgs<kRotatesPerLaunch>) <= 3968 && sizeof(HeldArgs) <= 3968 && sizeof(AttendArgs<kQueriesPerLaunch>) <= 3968,
               "a kernel's arguments, with what the runtime adds, stay below 4 KiB");
 
 struct AttnDims {
   int h_q, h_kv, group, d, dtype;
 };
-hipError_t launch_rotate(const AttnDims& dm, const RotateArgs& a, int n, hipStream_t st);
+// (a: room for the most; the launch takes what n sequences need)
+hipError_t launch_rotate(const AttnDims& dm, const RotateArgs<kRotatesPerLaunch>& a, int n, hipStream_t st);
 hipError_t launch_hold(const AttnDims& dm, const HeldArgs& a, int n, bool pack, hipStream_t st);
 constexpr int64_t kPartBytes = (int64_t)128 << 20;   // workspace of a handle
 // Fills the plan fields of `a` for n sequences and launches their attention.
-hipError_t launch_attend(const AttnDims& dm, AttendArgs& a, int n, int compute_units, void* workspace, hipStream_t st);
+hipError_t launch_attend(const AttnDims& dm, AttendArgs<kQueriesPerLaunch>& a, int n, int compute_units, void* workspace, hipStream_t st);
 
 }  // namespace omnimem

@@ -134,9 +134,9 @@ omnimem_status hold(omnimem_attn* attn, const omnimem_held* seqs, int32_t n, hip
     if ((st = check_held(attn, seqs[i], i, pack)) != OMNIMEM_OK) return st;
   OnDevice dev(attn->device);
   hipError_t e = dev.err;
-  for (int i0 = 0; i0 < n && e == hipSuccess; i0 += kSeqsPerLaunch) {
+  for (int i0 = 0; i0 < n && e == hipSuccess; i0 += kHeldPerLaunch) {
     HeldArgs a;
-    const int m = std::min(kSeqsPerLaunch, n - i0);
+    const int m = std::min(kHeldPerLaunch, n - i0);
     for (int i = 0; i < m; ++i) {
       const omnimem_held& s = seqs[i0 + i];
       a.seq[i] = {static_cast<char*>(s.k), static_cast<char*>(s.v), static_cast<char*>(s.data),
@@ -211,8 +211,7 @@ omnimem_status omnimem_rotate(omnimem_attn* attn, const omnimem_rope* rope, cons
   if (!std::isfinite(r.eps) || r.eps < 0.0f) return fail(attn, OMNIMEM_ERR_INVALID_ARG, "rope: eps must be finite and >= 0");
   if (!aligned(r.q_weight, 16) || !aligned(r.k_weight, 16))
     return fail(attn, OMNIMEM_ERR_INVALID_ARG, "rope: weights must be 16-byte aligned");
-  RotateArgs a;
-  std::memset(&a, 0, sizeof a);
+  RotateArgs<kRotatesPerLaunch> a;
   for (int j = 0; j < r.rotary_dim / 2; ++j) {
     const double f = r.inv_freq[j];
     if (!std::isfinite(f) || (r.axis && r.axis[j] >= r.n_axes))
@@ -255,8 +254,8 @@ omnimem_status omnimem_rotate(omnimem_attn* attn, const omnimem_rope* rope, cons
   }
   OnDevice dev(attn->device);
   hipError_t e = dev.err;
-  for (int i0 = 0; i0 < n && e == hipSuccess; i0 += kSeqsPerLaunch) {
-    const int m = std::min(kSeqsPerLaunch, n - i0);
+  for (int i0 = 0; i0 < n && e == hipSuccess; i0 += kRotatesPerLaunch) {
+    const int m = std::min(kRotatesPerLaunch, n - i0);
     for (int i = 0; i < m; ++i) {
       const omnimem_projection& s = seqs[i0 + i];
       a.seq[i] = {s.q, s.k, s.v, s.pos, s.modality, s.q_out, s.k_out, s.v_out, s.modality_out,
@@ -293,6 +292,8 @@ omnimem_status omnimem_attend(omnimem_attn* attn, const omnimem_query* seqs, int
     if (s.n_tail > 0 && (!readable(attn, s.k, s.kv_head_stride, s.kv_row_stride) ||
                          !readable(attn, s.v, s.kv_head_stride, s.kv_row_stride)))
       return fail(attn, OMNIMEM_ERR_INVALID_ARG, "sequence %d: k and v %s", i, kStride);
+    if (s.n_tail > 0 && s.kv_row_stride * (int64_t)elt(attn) >= (int64_t)1 << 24)
+      return bad(attn, i, "k and v need a row stride below 16 MiB");
     const int64_t bytes = omnimem_memory_bytes(c.head_dim, s.memory_rows);
     if (s.memory_rows > 0 && (!s.memory || !aligned(s.memory, 16) || s.memory_head_stride % 16 || s.memory_head_stride < 0 ||
                               s.memory_head_stride / 16 > UINT32_MAX ||
@@ -317,8 +318,7 @@ omnimem_status omnimem_attend(omnimem_attn* attn, const omnimem_query* seqs, int
   const int64_t per = 16 / (int64_t)elt(attn);
   const auto units = [per](int64_t stride) { return (uint32_t)(stride / per); };
   for (int i0 = 0; i0 < n && e == hipSuccess;) {
-    AttendArgs a;
-    std::memset(&a, 0, sizeof a);
+    AttendArgs<kQueriesPerLaunch> a;
     a.causal = causal ? 1 : 0;
     int m = 0;
     for (; i0 < n && m < kQueriesPerLaunch; ++i0) {

@@ -1,5 +1,8 @@
 // A chunk's projected rows to their places behind the cache: per-head norm
 // and rotation of queries and keys, values copied, in one pass.
+#include <cstddef>
+#include <cstring>
+
 #include "../../include/omnimem.h"
 #include "attn.h"
 
@@ -33,8 +36,8 @@ __device__ inline void store8(float* p, const float (&x)[8]) {
 // 8, D/16 lanes to a head.  The lanes of a wavefront form each of a token's
 // cosines and sines once (there are at most 64 frequencies) and take their 8
 // from one another; they serve all its heads.
-template <typename T, int D, int WPT>
-__global__ __launch_bounds__(256) void rotate_rows(RotateArgs a) {
+template <typename T, int D, int WPT, int N>
+__global__ __launch_bounds__(256) void rotate_rows(RotateArgs<N> a) {
   constexpr int U = D / 16, HEADS = 64 / U;
   const RotateSeq& s = a.seq[blockIdx.y];
   const int lane = threadIdx.x & 63, wave = wave_id();
@@ -108,13 +111,20 @@ __global__ __launch_bounds__(256) void rotate_rows(RotateArgs a) {
 }
 
 template <typename T, int D>
-void launch(const RotateArgs& a, int n, int64_t rows, hipStream_t st) {
-  rotate_rows<T, D, 4><<<dim3((unsigned)rows, n), 256, 0, st>>>(a);
+void launch(const RotateArgs<kRotatesPerLaunch>& a, int n, int64_t rows, hipStream_t st) {
+  if (n == 1) {
+    RotateArgs<1> one;
+    one.seq[0] = a.seq[0];
+    std::memcpy(one.turns, a.turns, sizeof a - offsetof(RotateArgs<kRotatesPerLaunch>, turns));
+    rotate_rows<T, D, 4, 1><<<dim3((unsigned)rows, n), 256, 0, st>>>(one);
+  } else {
+    rotate_rows<T, D, 4, kRotatesPerLaunch><<<dim3((unsigned)rows, n), 256, 0, st>>>(a);
+  }
 }
 
 }  // namespace
 
-hipError_t launch_rotate(const AttnDims& dm, const RotateArgs& a, int n, hipStream_t st) {
+hipError_t launch_rotate(const AttnDims& dm, const RotateArgs<kRotatesPerLaunch>& a, int n, hipStream_t st) {
   int64_t rows = 0;
   for (int i = 0; i < n; ++i) rows = std::max(rows, a.seq[i].n);
   if (rows == 0) return hipSuccess;

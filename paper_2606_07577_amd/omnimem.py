@@ -527,10 +527,10 @@ class Attention:
     def _call(self, function, descriptors, kind, *more, stream=None):
         if len(descriptors) and not (isinstance(descriptors, ctypes.Array) and descriptors._type_ is kind):
             descriptors = (kind * len(descriptors))(*descriptors)
-        s = stream if stream is not None else torch.cuda.current_stream(self.device)
+        # (the raw handle costs a tenth of a microsecond, a Stream object a whole one: a fifth of a small call)
+        s = stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(self.device)
         before, after = (more[:1], more[1:]) if kind is Projection else ((), more)
-        st = function(self.handle, *before, descriptors if len(descriptors) else None, len(descriptors), *after,
-                      ctypes.c_void_p(s.cuda_stream))
+        st = function(self.handle, *before, descriptors if len(descriptors) else None, len(descriptors), *after, s)
         if st != OK:
             raise OmnimemError(st, self._lib.omnimem_attn_last_error(self.handle).decode())
 
