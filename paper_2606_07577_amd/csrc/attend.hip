@@ -99,9 +99,35 @@ __device__ inline void put4(uint16_t* p, floatx4 x) { *reinterpret_cast<uint2*>(
 __device__ inline void put4(float* p, floatx4 x) { *reinterpret_cast<floatx4*>(p) = x; }
 __device__ inline float log_of(float m, float l) { return l == 0.0f ? -INFINITY : (m + log2f(l)) * kLn2; }
 
+// A wavefront's sums of 32 rows (lane: row `r` of the tile, channels by
+// accumulator register) to their partial or, divided, to the output.
+template <typename T, int D, int R, int N>
+__device__ inline void write_rows(const AttendArgs<N>& a, const QuerySeq& s, const Unit& x, const Row& row, int r, int half,
+                                  const floatx16 (&o)[D / 32], float m, float l) {
+  constexpr int E = (int)sizeof(T);
+  if (x.slot >= 0) {
+    const int64_t at = (int64_t)x.slot * R + r;
+    if (half == 0) a.part_ml[at] = make_float2(m, l);
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        put4(a.part_o + at * D + c * 32 + e * 8 + half * 4, floatx4{o[c][4 * e], o[c][4 * e + 1], o[c][4 * e + 2], o[c][4 * e + 3]});
+  } else if (row.live) {
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    T* out = static_cast<T*>(s.out) + row.h * elems(s.out_hs, E) + row.i * elems(s.out_rs, E);
+    if (half == 0 && s.lse) s.lse[row.h * (int64_t)s.lse_hs + row.i] = log_of(m, l);
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        put4(out + c * 32 + e * 8 + half * 4, floatx4{o[c][4 * e], o[c][4 * e + 1], o[c][4 * e + 2], o[c][4 * e + 3]} * inv);
+  }
+}
+
 // ---------------------------------------------------------------------------
-// fp32: 32 query rows to a unit; the four wavefronts take 32 keys each of a
-// tile of 128 in LDS, and join their sums at the end.
+// fp32, few rows: 32 query rows to a unit; the four wavefronts take 32 keys
+// each of a tile of 128 in LDS, and join their sums at the end.
 // ---------------------------------------------------------------------------
 template <int D>
 struct F32 {
@@ -251,6 +277,149 @@ __global__ __launch_bounds__(256) void attend_f32(AttendArgs<N> a) {
       if (w.live) put4(static_cast<float*>(s.out) + w.h * elems(s.out_hs, 4) + w.i * elems(s.out_rs, 4) + c, y * ml[r].x);
     }
   }
+}
+
+// ---------------------------------------------------------------------------
+// fp32, many rows: 128 query rows to a unit, 32 to each wavefront, against key
+// tiles of 64 rows in two LDS stages.  The MFMA's rate bounds it (a quarter of
+// the vector unit's work for each), so a step is in the plain order.
+// ---------------------------------------------------------------------------
+template <int D>
+struct F32Many {
+  static constexpr int R = 128, KT = 64;
+  static constexpr int TILE = KT * D;                      // elements of a K or V stage
+  static constexpr int LDS = 4 * TILE * 4;
+  static constexpr int CPR = D / 4, COPIES = CPR / 4;      // 16-byte chunks per row, 1 KiB copies per wavefront
+  __device__ static inline int k_chunk(int r, int c) { return c ^ (r & (CPR - 1)); }
+};
+
+template <int D, int N>
+__global__ __launch_bounds__(256) void attend_f32_many(AttendArgs<N> a) {
+  using P = F32Many<D>;
+  using M = Mfma<float>;
+  using B = MemBlock<D>;
+  constexpr int R = P::R, KT = P::KT, TILE = P::TILE, CPR = P::CPR, NCT = D / 32, W = D / 32;
+  extern __shared__ __align__(16) char lds[];
+  float* kbuf = reinterpret_cast<float*>(lds);             // [2][TILE]
+  float* vbuf = kbuf + 2 * TILE;
+  const Unit x = unit_of<R, KT>(a, blockIdx.x);
+  const QuerySeq& s = a.seq[x.s];
+  const int tid = threadIdx.x, lane = tid & 63, wave = wave_id(), half = lane >> 5, col = lane & 31;
+  const Row row = row_of(a, s, x, x.rt * R + wave * 32 + col);
+  const float* qp = static_cast<const float*>(s.q) + row.h * elems(s.q_hs, 4) + row.i * elems(s.q_rs, 4);
+  floatx4 q[D / 8];                                        // channels 8 j + 4 half ..: one of each half to an MFMA
+#pragma unroll
+  for (int j = 0; j < D / 8; ++j) q[j] = row.live ? gload<floatx4>(qp + 8 * j + 4 * half) : floatx4{};
+  floatx16 o[NCT];
+#pragma unroll
+  for (int c = 0; c < NCT; ++c) o[c] = floatx16{};
+  float m = -INFINITY, l = 0.0f;
+
+  const uint32_t rsb = s.kv_rs * 16u;                      // row stride in bytes, below 2^24
+  const char* kp = static_cast<const char*>(s.k) + x.g * ((int64_t)s.kv_hs * 16);
+  const char* vp = static_cast<const char*>(s.v) + x.g * ((int64_t)s.kv_hs * 16);
+  const char* data = s.mem + x.g * ((int64_t)s.mem_hs * 16);
+  const int mem_tiles = x.mem_tiles, nt = s.nt, nm = s.nm;
+  const int last_block = tiles_of<kMemRows>(nm) - 1;
+  const auto copy = [&](const char* base, float* to, int t, bool is_k) __attribute__((always_inline)) {
+    const int key0 = (t - mem_tiles) * KT, keys = nt - key0;
+    const char* tile = base + (int64_t)key0 * rsb;
+#pragma unroll
+    for (int j = 0; j < P::COPIES; ++j) {
+      const int J = wave * P::COPIES + j, r = (J * 64 + lane) / CPR, c = lane % CPR;
+      dma16_opaque_s(tile, (uint32_t)min(r, keys - 1) * rsb + (is_k ? P::k_chunk(r, c) : c) * 16, to + J * 256);
+    }
+  };
+  // a memory tile on its way: K by rows, 4 threads to one; V by channels, 8 / W threads to one
+  uint32_t kw[W], vw[W], kb = 0, vb = 0;
+  const int krow = tid / 4, vch = tid * W / 8, vt8 = tid * W % 8;
+  const auto fetch = [&](int t, int st) __attribute__((always_inline)) {
+    if (t >= mem_tiles) {
+      copy(kp, kbuf + st * TILE, t, true);
+      copy(vp, vbuf + st * TILE, t, false);
+      return;
+    }
+    const char* p = data + (int64_t)min(t * 2 + krow / 32, last_block) * B::BYTES;
+    const char* v = data + (int64_t)min(t * 2 + vt8 / 4, last_block) * B::BYTES;
+#pragma unroll
+    for (int j = 0; j < W; ++j) {
+      kw[j] = gload<uint32_t>(p + (krow & 31) * (D / 2) + ((tid & 3) * W + j) * 4);
+      vw[j] = gload<uint32_t>(v + B::V + vch * 16 + (vt8 % 4 + j) * 4);
+    }
+    kb = gload<uint8_t>(p + B::k_scale(krow & 31, (tid & 3) * (D / 4) / 32));
+    vb = gload<uint8_t>(v + B::v_scale(vch));
+  };
+  const auto store = [&](int t, int st) __attribute__((always_inline)) {
+    if (t >= mem_tiles) return;
+    float* kd = kbuf + st * TILE + krow * D;
+    float* vd = vbuf + st * TILE + vch;
+#pragma unroll
+    for (int j = 0; j < W; ++j) {
+      float y[8];
+      values8(kw[j], kb, y);
+      const int c = ((tid & 3) * W + j) * 2;
+      *reinterpret_cast<floatx4*>(kd + P::k_chunk(krow, c) * 4) = floatx4{y[0], y[1], y[2], y[3]};
+      *reinterpret_cast<floatx4*>(kd + P::k_chunk(krow, c + 1) * 4) = floatx4{y[4], y[5], y[6], y[7]};
+      values8(vw[j], vb, y);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) vd[((vt8 + j) * 8 + e) * D] = y[e];
+    }
+  };
+
+  if (x.k0 < x.k1) {
+    fetch(x.k0, 0);
+    store(x.k0, 0);
+  }
+  dma_wait();
+  __syncthreads();
+  for (int t = x.k0; t < x.k1; ++t) {
+    const int st = (t - x.k0) & 1;
+    if (t + 1 < x.k1) fetch(t + 1, st ^ 1);
+    const int limit = (t < mem_tiles ? nm - t * KT : row.seen - (t - mem_tiles) * KT) - half * 4;
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const float* kd = kbuf + st * TILE + (b * 32 + col) * D;
+      floatx16 sc = floatx16{};
+#pragma unroll
+      for (int j = 0; j < D / 8; ++j) {
+        const floatx4 k = *reinterpret_cast<const floatx4*>(kd + P::k_chunk(b * 32 + col, 2 * j + half) * 4);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sc = M::mma(k[e], q[j][e], sc);
+      }
+      float top = -INFINITY;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        sc[r] = b * 32 + (r >> 2) * 8 + (r & 3) < limit ? sc[r] * s.scale_log2 : -INFINITY;
+        top = fmaxf(top, sc[r]);
+      }
+      top = fmaxf(top, __shfl_xor(top, 32));
+      if (__any(top > m + 8.0f)) {                         // (see attend_many)
+        const float m2 = fmaxf(m, top);
+        const float alpha = m2 == -INFINITY ? 1.0f : exp2_(m - m2);
+        m = m2;
+        l *= alpha;
+#pragma unroll
+        for (int c = 0; c < NCT; ++c) o[c] *= alpha;
+      }
+      const float ref = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        sc[r] = exp2_(sc[r] - ref);
+        l += sc[r];
+      }
+      // (the keys of accumulator register r of this half)
+      const float* vd = vbuf + st * TILE + (b * 32 + half * 4) * D + col;
+#pragma unroll
+      for (int c = 0; c < NCT; ++c)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[c] = M::mma(vd[((r >> 2) * 8 + (r & 3)) * D + c * 32], sc[r], o[c]);
+    }
+    if (t + 1 < x.k1) store(t + 1, st ^ 1);
+    dma_wait();
+    __syncthreads();
+  }
+  l += __shfl_xor(l, 32);
+  write_rows<float, D, R>(a, s, x, row, wave * 32 + col, half, o, m, l);
 }
 
 // ---------------------------------------------------------------------------
@@ -848,24 +1017,7 @@ __global__ __launch_bounds__(512, 2) void attend_many(AttendArgs<N> a) {
     steps(std::false_type{}, mid, k1);
   }
   l += __shfl_xor(l, 32);
-  if (x.slot >= 0) {
-    const int64_t r = (int64_t)x.slot * R + wave * 32 + col;
-    if (half == 0) a.part_ml[r] = make_float2(m, l);
-#pragma unroll
-    for (int c = 0; c < NCT; ++c)
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        put4(a.part_o + r * D + c * 32 + e * 8 + half * 4, floatx4{o[c][4 * e], o[c][4 * e + 1], o[c][4 * e + 2], o[c][4 * e + 3]});
-  } else if (row.live) {
-    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-    uint16_t* out = static_cast<uint16_t*>(s.out) + row.h * elems(s.out_hs, 2) + row.i * elems(s.out_rs, 2);
-    if (half == 0 && s.lse) s.lse[row.h * (int64_t)s.lse_hs + row.i] = log_of(m, l);
-#pragma unroll
-    for (int c = 0; c < NCT; ++c)
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        put4(out + c * 32 + e * 8 + half * 4, floatx4{o[c][4 * e], o[c][4 * e + 1], o[c][4 * e + 2], o[c][4 * e + 3]} * inv);
-  }
+  write_rows<uint16_t, D, R>(a, s, x, row, wave * 32 + col, half, o, m, l);
 }
 
 // ---------------------------------------------------------------------------
@@ -1014,11 +1166,11 @@ int64_t plan_shares(Args& a, int64_t slots, int64_t share, int64_t target) {
 }
 
 // As many whole row tiles as fill the chip a number of times, and the rest in
-// so many shares that it takes least: rounds of a share's key tiles, with
-// about 3 more to begin and end it, and the join, which moves a partial in
-// about 0.03 of a key tile's time and costs 3 to launch.
+// so many shares that it takes least: rounds of a share's key tiles and `ends`
+// more to begin and end it, and the join, about as much again to launch and
+// `partial` for each, in key tiles' time (bf16 about 1.7 us, fp32 4 us).
 template <int R, int KT>
-int64_t plan_rounds(Args& a, int64_t slots, int width) {
+int64_t plan_rounds(Args& a, int64_t slots, int width, double ends, double partial) {
   int64_t keys;
   const int64_t n = count_tiles<R, KT>(a, &keys);
   if (n > INT32_MAX / 64) return -1;
@@ -1029,7 +1181,7 @@ int64_t plan_rounds(Args& a, int64_t slots, int width) {
     const int64_t most = std::max<int64_t>(1, std::min<int64_t>(slots / rest, 512));
     double best = 1e30;
     for (int c = 1; c <= most && c <= tiles; ++c) {
-      const double cost = (double)((rest * c + width - 1) / width) * (tiles / c + 3) + (c > 1 ? 3 + 0.03 * rest * c : 0);
+      const double cost = (double)((rest * c + width - 1) / width) * (tiles / c + ends) + (c > 1 ? ends + partial * rest * c : 0);
       if (cost < best) { best = cost; splits = c; }
     }
   }
@@ -1064,7 +1216,7 @@ hipError_t launch(const AttendArgs<N>& a, int64_t joins, Kernel kernel, int thre
   int splits = 0;
   for (int i = 0; i < a.n_seqs; ++i) splits = std::max(splits, a.seq[i].splits);
   if (splits <= 8) join<T, D, R, 1, 256, N>(a, joins, st);
-  else if (splits <= 32 || R == 256) join<T, D, R, 4, 256, N>(a, joins, st);
+  else if (splits <= 32 || R >= 128) join<T, D, R, 4, 256, N>(a, joins, st);
   else join<T, D, R, 1024 / (D / 4), 1024, N>(a, joins, st);
   return hipGetLastError();
 }
@@ -1093,20 +1245,25 @@ hipError_t attend_few_rows(Args& a, int cus, void* ws, hipStream_t st) {
 
 template <int D>
 hipError_t attend(const AttnDims& dm, Args& a, int cus, void* ws, hipStream_t st) {
+  int64_t rows = 0, keys = 0;
+  for (int i = 0; i < a.n_seqs; ++i) rows = std::max(rows, (int64_t)a.group * a.seq[i].nq);
   if (dm.dtype == OMNIMEM_F32) {
+    if (rows > (getenv("OMN_F") ? atoi(getenv("OMN_F")) : 64)) {
+      using P = F32Many<D>;
+      const int64_t joins = plan_rounds<P::R, P::KT>(a, partials<P::R, D>(), cus, 1.0, 0.003);
+      return launch<float, D, P::R>(a, ws, joins, attend_f32_many<D, 1>, attend_f32_many<D, kQueriesPerLaunch>, 256, P::LDS, st);
+    }
     using P = F32<D>;
     const int64_t joins = plan_shares<P::R, P::KT>(a, partials<P::R, D>(), 1, 4 * cus);
     return launch<float, D, P::R>(a, ws, joins, attend_f32<D, 1>, attend_f32<D, kQueriesPerLaunch>, 256, P::LDS, st);
   }
-  int64_t rows = 0, keys = 0;
-  for (int i = 0; i < a.n_seqs; ++i) rows = std::max(rows, (int64_t)a.group * a.seq[i].nq);
   if (rows <= 16) return attend_few_rows<D, 1>(a, cus, ws, st);
   // Up to 8192 / d rows of every head, and further where that leaves a wavefront at most 896 / d tiles of 32 rows
   // and 128 keys for each compute unit, the few-row kernel.
   count_tiles<32, 128>(a, &keys);
   if (rows <= 8192 / D || keys <= 896 / D * cus) return attend_few_rows<D, 2>(a, cus, ws, st);
   using P = Many<D>;
-  const int64_t joins = plan_rounds<P::R, P::KT>(a, partials<P::R, D>(), cus);
+  const int64_t joins = plan_rounds<P::R, P::KT>(a, partials<P::R, D>(), cus, 3.0, 0.03);
   return launch<uint16_t, D, P::R>(a, ws, joins, attend_many<D, 1>, attend_many<D, kQueriesPerLaunch>, 512, P::LDS, st);
 }
 

@@ -29,66 +29,65 @@ __device__ inline uint32_t codes8(const float (&x)[8], uint32_t byte) {
   return w;
 }
 
-__device__ inline float load1(const uint16_t* p) { return __uint_as_float((uint32_t)gload<uint16_t>(p) << 16); }
-__device__ inline float load1(const float* p) { return gload<float>(p); }
-__device__ inline void load8(const uint16_t* p, float (&x)[8]) {
-  const uint4 w = gload16(p);
-  const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+// C consecutive elements of a row (4 or 8) as they lie in memory, and as fp32.
+template <int C, typename T>
+struct Raw {
+  static constexpr int WORDS = C * (int)sizeof(T) / 4;
+  uint32_t w[WORDS];
+  __device__ inline void load(const T* p) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(u[i] << 16); x[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u); }
-}
-__device__ inline void load8(const float* p, float (&x)[8]) {
-  const floatx4 a = gload<floatx4>(p), b = gload<floatx4>(p + 4);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) { x[i] = a[i]; x[4 + i] = b[i]; }
-}
-// CPL channels (1 or 2) of a row.
-template <int CPL>
-__device__ inline void load_channels(const uint16_t* p, float (&x)[CPL]) {
-  if constexpr (CPL == 1) {
-    x[0] = load1(p);
-  } else {
-    const uint32_t w = gload<uint32_t>(p);
-    x[0] = __uint_as_float(w << 16);
-    x[1] = __uint_as_float(w & 0xFFFF0000u);
+    for (int i = 0; i < WORDS; i += 4) {
+      if constexpr (WORDS == 2) {
+        const uint2 y = gload8(p);
+        w[0] = y.x; w[1] = y.y;
+      } else {
+        const uint4 y = gload16(reinterpret_cast<const uint32_t*>(p) + i);
+        w[i] = y.x; w[i + 1] = y.y; w[i + 2] = y.z; w[i + 3] = y.w;
+      }
+    }
   }
-}
-template <int CPL>
-__device__ inline void load_channels(const float* p, float (&x)[CPL]) {
-#pragma unroll
-  for (int i = 0; i < CPL; ++i) x[i] = load1(p + i);
-}
+  __device__ inline float operator[](int i) const {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
+    return __uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
+  }
+};
 
-// One wavefront per block of 32 rows.  K: four lanes to a group of 32
-// channels, 8 channels each.  V: a lane has D/64 channels over the 32 rows.
+// One wavefront per block of 32 rows, whole rows read 16 bytes (d = 64: 8) a
+// lane.  K: four lanes to a group of 32 channels, 8 channels each.  V: lane
+// (i, g) has D/16 channels of rows 8 g .. 8 g + 7, a word of codes of each; the
+// four lanes g agree on a channel's scale.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void pack_rows(HeldArgs a) {
   using B = MemBlock<D>;
-  constexpr int CPL = D / 64;
+  constexpr int C = D / 16;
   const HeldSeq& s = a.seq[blockIdx.z];
-  const int lane = threadIdx.x & 63;
+  const int lane = threadIdx.x & 63, g = lane >> 4, c0 = (lane & 15) * C;
   const int64_t block = (int64_t)blockIdx.x * 4 + wave_id();
   if (block * kMemRows >= s.n) return;
   const int valid = (int)min((int64_t)kMemRows, s.n - block * kMemRows);
   const T* k = reinterpret_cast<const T*>(s.k) + blockIdx.y * s.kv_hs + block * kMemRows * s.kv_rs;
   const T* v = reinterpret_cast<const T*>(s.v) + blockIdx.y * s.kv_hs + block * kMemRows * s.kv_rs;
   char* out = s.data + blockIdx.y * s.data_hs + block * B::BYTES;
-  float col[CPL][kMemRows];
+  Raw<C, T> vr[8];
+  Raw<8, T> kr[D / 16];
 #pragma unroll
-  for (int t = 0; t < kMemRows; ++t) {
-    float x[CPL] = {};
-    if (t < valid) load_channels<CPL>(v + t * s.kv_rs + lane * CPL, x);
-#pragma unroll
-    for (int i = 0; i < CPL; ++i) col[i][t] = x[i];
+  for (int it = 0; it < D / 16; ++it) {
+    const int slot = it * 64 + lane;
+    kr[it].load(k + min(slot / (D / 8), valid - 1) * s.kv_rs + slot % (D / 8) * 8);
   }
+#pragma unroll
+  for (int r = 0; r < 8; ++r) vr[r].load(v + min(g * 8 + r, valid - 1) * s.kv_rs + c0);
+  asm volatile("" ::: "memory");           // (every load is on its way before the first is waited for)
 #pragma unroll
   for (int it = 0; it < D / 16; ++it) {
     const int slot = it * 64 + lane, t = slot / (D / 8), c8 = slot % (D / 8);
-    float x[8] = {};
-    if (t < valid) load8(k + t * s.kv_rs + c8 * 8, x);
+    float x[8];
     uint32_t m = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) m = max(m, magnitude(x[i]));
+    for (int i = 0; i < 8; ++i) {
+      x[i] = t < valid ? kr[it][i] : 0.0f;
+      m = max(m, magnitude(x[i]));
+    }
     m = max(m, (uint32_t)__shfl_xor((int)m, 1));
     m = max(m, (uint32_t)__shfl_xor((int)m, 2));
     const uint32_t byte = scale_byte(m);
@@ -96,22 +95,19 @@ __global__ __launch_bounds__(256) void pack_rows(HeldArgs a) {
     if ((c8 & 3) == 0) out[B::k_scale(t, c8 >> 2)] = (char)byte;
   }
 #pragma unroll
-  for (int i = 0; i < CPL; ++i) {
+  for (int i = 0; i < C; ++i) {
+    float x[8];
     uint32_t m = 0;
 #pragma unroll
-    for (int t = 0; t < kMemRows; ++t) m = max(m, magnitude(col[i][t]));
-    const uint32_t byte = scale_byte(m);
-    uint32_t w[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      float x[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = col[i][8 * j + e];
-      w[j] = codes8(x, byte);
+    for (int r = 0; r < 8; ++r) {
+      x[r] = g * 8 + r < valid ? vr[r][i] : 0.0f;
+      m = max(m, magnitude(x[r]));
     }
-    const int c = lane * CPL + i;
-    *reinterpret_cast<uint4*>(out + B::V + c * 16) = make_uint4(w[0], w[1], w[2], w[3]);
-    out[B::v_scale(c)] = (char)byte;
+    m = max(m, (uint32_t)__shfl_xor((int)m, 16));
+    m = max(m, (uint32_t)__shfl_xor((int)m, 32));
+    const uint32_t byte = scale_byte(m);
+    *reinterpret_cast<uint32_t*>(out + B::V + (c0 + i) * 16 + g * 4) = codes8(x, byte);
+    if (g == i * 4 / C) out[B::v_scale(c0 + i)] = (char)byte;
   }
 }
 
