@@ -97,7 +97,123 @@ __device__ inline Row row_of(const AttendArgs<N>& a, const QuerySeq& s, const Un
 
 __device__ inline void put4(uint16_t* p, floatx4 x) { *reinterpret_cast<uint2*>(p) = make_uint2(round2(x[0], x[1]), round2(x[2], x[3])); }
 __device__ inline void put4(float* p, floatx4 x) { *reinterpret_cast<floatx4*>(p) = x; }
+__device__ inline void put1(uint16_t* p, float x) { *p = (uint16_t)round2(x, 0.0f); }
+__device__ inline void put1(float* p, float x) { *p = x; }
 __device__ inline float log_of(float m, float l) { return l == 0.0f ? -INFINITY : (m + log2f(l)) * kLn2; }
+
+// ---------------------------------------------------------------------------
+// Rows that a query does not see have weight 0, but the matrix cores multiply
+// it with what the row holds, and 0 times an infinity or NaN is NaN.  A unit
+// whose sums are not finite forms the rows again that have such a row among
+// its keys, each by one wavefront over the keys that the row sees, and writes
+// them over what it wrote.
+// ---------------------------------------------------------------------------
+template <typename T, int D, int KT>
+__device__ inline bool sees_all(const QuerySeq& s, const Unit& x, const Row& row) {
+  return row.seen >= min((int64_t)s.nt, (int64_t)(x.k1 - x.mem_tiles) * KT);
+}
+template <int D, typename T>
+__device__ inline void channels(const T* p, int lane, float (&y)[D / 64]) {
+#pragma unroll
+  for (int i = 0; i < D / 64; ++i) {
+    if constexpr (sizeof(T) == 2) y[i] = __uint_as_float((uint32_t)gload<uint16_t>(p + lane + i * 64) << 16);
+    else y[i] = gload<float>(p + lane + i * 64);
+  }
+}
+template <typename T, int D, int R, int KT, int N>
+__device__ __forceinline__ void form_again(const AttendArgs<N>& a, const QuerySeq& s, const Unit& x, int r, float m, float l) {
+  using B = MemBlock<D>;
+  constexpr int E = (int)sizeof(T), C = D / 64;
+  const int lane = threadIdx.x & 63;
+  const Row row = row_of(a, s, x, x.rt * R + r);
+  if (!row.live || sees_all<T, D, KT>(s, x, row)) return;
+  const float ref = m == -INFINITY ? 0.0f : m;
+  float q[C], o[C] = {};
+  channels<D>(static_cast<const T*>(s.q) + row.h * elems(s.q_hs, E) + row.i * elems(s.q_rs, E), lane, q);
+  const auto add = [&](const float (&k)[C], const float (&v)[C]) __attribute__((always_inline)) {
+    float dot = 0.0f;
+#pragma unroll
+    for (int i = 0; i < C; ++i) dot += q[i] * k[i];
+#pragma unroll
+    for (int e = 1; e < 64; e *= 2) dot += __shfl_xor(dot, e);
+    const float p = exp2_(dot * s.scale_log2 - ref);
+#pragma unroll
+    for (int i = 0; i < C; ++i) o[i] += p * v[i];
+  };
+  const int64_t mem_end = min((int64_t)s.nm, (int64_t)x.k1 * KT);
+  for (int64_t j = (int64_t)x.k0 * KT; j < mem_end; ++j) {
+    const char* blk = s.mem + x.g * ((int64_t)s.mem_hs * 16) + j / kMemRows * B::BYTES;
+    const int t = (int)(j % kMemRows);
+    float k[C], v[C], y[8];
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+      const int c = lane + i * 64;
+      values8(gload<uint8_t>(blk + t * (D / 2) + c / 2), gload<uint8_t>(blk + B::k_scale(t, c >> 5)), y);
+      k[i] = c & 1 ? y[1] : y[0];
+      values8(gload<uint8_t>(blk + B::V + c * 16 + t / 2), gload<uint8_t>(blk + B::v_scale(c)), y);
+      v[i] = t & 1 ? y[1] : y[0];
+    }
+    add(k, v);
+  }
+  const int64_t rs = elems(s.kv_rs, E), hs = x.g * elems(s.kv_hs, E);
+  const int64_t end = min((int64_t)row.seen, (int64_t)(x.k1 - x.mem_tiles) * KT);
+  for (int64_t j = max(x.k0 - x.mem_tiles, 0) * (int64_t)KT; j < end; ++j) {
+    float k[C], v[C];
+    channels<D>(static_cast<const T*>(s.k) + hs + j * rs, lane, k);
+    channels<D>(static_cast<const T*>(s.v) + hs + j * rs, lane, v);
+    add(k, v);
+  }
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");   // (after what the wavefront wrote there)
+#pragma unroll
+  for (int i = 0; i < C; ++i) {
+    const int c = lane + i * 64;
+    if (x.slot >= 0) a.part_o[((int64_t)x.slot * R + r) * D + c] = o[i];
+    else put1(static_cast<T*>(s.out) + row.h * elems(s.out_hs, E) + row.i * elems(s.out_rs, E) + c, o[i] * inv);
+  }
+}
+// The same for the rows of a workgroup whose flags are set (in LDS, with their
+// statistics), and for a wavefront's own 32 rows (a lane each, twice).
+template <typename T, int D, int R, int KT, int N>
+__device__ __forceinline__ void form_flagged(const AttendArgs<N>& a, const QuerySeq& s, const Unit& x, const int* flag, const float2* ml) {
+  for (int r = wave_id(); r < R; r += (int)blockDim.x / 64)
+    if (uniform(flag[r])) form_again<T, D, R, KT>(a, s, x, r, ml[r].x, ml[r].y);
+}
+template <typename T, int D, int R, int KT, int N>
+__device__ __forceinline__ void form_own(const AttendArgs<N>& a, const QuerySeq& s, const Unit& x, const Row& row, int r0,
+                                const floatx16 (&o)[D / 32], float m, float l) {
+  if (x.k1 <= x.mem_tiles) return;
+  float zero = 0.0f;
+#pragma unroll
+  for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) zero = __builtin_fmaf(o[c][e], 0.0f, zero);
+  uint64_t odd = __ballot(zero != 0.0f && row.live && !sees_all<T, D, KT>(s, x, row));
+  for (odd = (odd | odd >> 32) & 0xFFFFFFFFu; odd; odd &= odd - 1) {
+    const int r = __builtin_ctzll(odd);
+    form_again<T, D, R, KT>(a, s, x, r0 + r, __shfl(m, r), __shfl(l, r));
+  }
+}
+
+// A workgroup's joined sums [R][ROW] in LDS to its partial or, divided, to the
+// output; flags the rows that are not finite.
+template <typename T, int D, int R, int ROW, int N>
+__device__ inline void write_joined(const AttendArgs<N>& a, const QuerySeq& s, const Unit& x, const float* ob, const float2* ml, int* flag) {
+  constexpr int E = (int)sizeof(T);
+  for (int e = threadIdx.x; e < R * D / 4; e += blockDim.x) {
+    const int r = e / (D / 4), c = e % (D / 4) * 4;
+    const Row row = row_of(a, s, x, x.rt * R + r);
+    if (!row.live) break;
+    const floatx4 y = *reinterpret_cast<const floatx4*>(ob + r * ROW + c);
+    if (x.slot >= 0) {
+      put4(a.part_o + ((int64_t)x.slot * R + r) * D + c, y);
+    } else {
+      const float l = ml[r].y;
+      put4(static_cast<T*>(s.out) + row.h * elems(s.out_hs, E) + row.i * elems(s.out_rs, E) + c, y * (l == 0.0f ? 0.0f : 1.0f / l));
+    }
+    if (x.k1 > x.mem_tiles && (y[0] + y[1] + y[2] + y[3]) * 0.0f != 0.0f) flag[r] = 1;
+  }
+}
 
 // A wavefront's sums of 32 rows (lane: row `r` of the tile, channels by
 // accumulator register) to their partial or, divided, to the output.
@@ -133,7 +249,7 @@ template <int D>
 struct F32 {
   static constexpr int R = 32, KT = 128;
   static constexpr int ROW = D + 4;                        // padded LDS row
-  static constexpr int LDS = 2 * KT * ROW * 4 + 4 * R * 8;
+  static constexpr int LDS = 2 * KT * ROW * 4 + 4 * R * 8 + R * 4;
 };
 
 template <int D, int N>
@@ -146,6 +262,7 @@ __global__ __launch_bounds__(256) void attend_f32(AttendArgs<N> a) {
   float* kt = reinterpret_cast<float*>(lds);
   float* vt = kt + KT * ROW;
   float2* ml = reinterpret_cast<float2*>(vt + KT * ROW);   // [4][R]
+  int* flag = reinterpret_cast<int*>(ml + 4 * R);           // [R]
   const Unit x = unit_of<R, KT>(a, blockIdx.x);
   const QuerySeq& s = a.seq[x.s];
   const int lane = threadIdx.x & 63, wave = wave_id(), half = lane >> 5, col = lane & 31;
@@ -259,24 +376,15 @@ __global__ __launch_bounds__(256) void attend_f32(AttendArgs<N> a) {
   }
   __syncthreads();
   if (wave == 0 && half == 0) {
-    if (x.slot >= 0) {
-      a.part_ml[(int64_t)x.slot * R + col] = make_float2(top, total);
-    } else {
-      ml[col].x = total == 0.0f ? 0.0f : 1.0f / total;
-      if (row.live && s.lse) s.lse[row.h * (int64_t)s.lse_hs + row.i] = log_of(top, total);
-    }
+    ml[col] = make_float2(top, total);
+    flag[col] = 0;
+    if (x.slot >= 0) a.part_ml[(int64_t)x.slot * R + col] = make_float2(top, total);
+    else if (row.live && s.lse) s.lse[row.h * (int64_t)s.lse_hs + row.i] = log_of(top, total);
   }
   __syncthreads();
-  for (int e = threadIdx.x; e < R * D / 4; e += 256) {
-    const int r = e / (D / 4), c = e % (D / 4) * 4;
-    const floatx4 y = *reinterpret_cast<const floatx4*>(ob + r * ROW + c);
-    if (x.slot >= 0) {
-      put4(a.part_o + ((int64_t)x.slot * R + r) * D + c, y);
-    } else {
-      const Row w = row_of(a, s, x, x.rt * R + r);
-      if (w.live) put4(static_cast<float*>(s.out) + w.h * elems(s.out_hs, 4) + w.i * elems(s.out_rs, 4) + c, y * ml[r].x);
-    }
-  }
+  write_joined<float, D, R, ROW>(a, s, x, ob, ml, flag);
+  __syncthreads();
+  form_flagged<float, D, R, KT>(a, s, x, flag, ml);
 }
 
 // ---------------------------------------------------------------------------
@@ -420,6 +528,7 @@ __global__ __launch_bounds__(256) void attend_f32_many(AttendArgs<N> a) {
   }
   l += __shfl_xor(l, 32);
   write_rows<float, D, R>(a, s, x, row, wave * 32 + col, half, o, m, l);
+  form_own<float, D, R, KT>(a, s, x, row, wave * 32, o, m, l);
 }
 
 // ---------------------------------------------------------------------------
@@ -437,7 +546,7 @@ struct Few {
   static constexpr int OROW = D + 4;
   static constexpr int VBUF = 32 * D * 2;                  // bytes of a wavefront's tail V rows in LDS
   static constexpr int JOIN = R * OROW * 4;
-  static constexpr int LDS = (4 * VBUF > JOIN ? 4 * VBUF : JOIN) + 4 * R * 8;
+  static constexpr int LDS = (4 * VBUF > JOIN ? 4 * VBUF : JOIN) + 4 * R * 8 + R * 4;
 };
 // 16-byte chunk of row r that holds its chunk c: the 8 rows that 32 lanes read
 // 32 bytes each of lie in different banks.
@@ -674,7 +783,8 @@ __global__ __launch_bounds__(256, D * NR == 256 ? 1 : 2) void attend_few(AttendA
   }
 
   // join the four wavefronts
-  float2* ml = reinterpret_cast<float2*>(lds + P::LDS - 4 * R * 8);   // [4][R]
+  float2* ml = reinterpret_cast<float2*>(lds + P::LDS - 4 * R * 8 - R * 4);   // [4][R]
+  int* flag = reinterpret_cast<int*>(ml + 4 * R);                     // [R]
   float* ob = reinterpret_cast<float*>(lds);                          // [R][OROW]
 #pragma unroll
   for (int n = 0; n < NR; ++n) {
@@ -712,23 +822,16 @@ __global__ __launch_bounds__(256, D * NR == 256 ? 1 : 2) void attend_few(AttendA
   if (wave == 0 && g == 0) {
 #pragma unroll
     for (int n = 0; n < NR; ++n) {
-      if (x.slot >= 0) {
-        a.part_ml[(int64_t)x.slot * R + n * 16 + i16] = make_float2(top[n], total[n]);
-      } else {
-        ml[n * 16 + i16].x = total[n] == 0.0f ? 0.0f : 1.0f / total[n];
-        if (row[n].live && s.lse) s.lse[row[n].h * (int64_t)s.lse_hs + row[n].i] = log_of(top[n], total[n]);
-      }
+      ml[n * 16 + i16] = make_float2(top[n], total[n]);
+      flag[n * 16 + i16] = 0;
+      if (x.slot >= 0) a.part_ml[(int64_t)x.slot * R + n * 16 + i16] = make_float2(top[n], total[n]);
+      else if (row[n].live && s.lse) s.lse[row[n].h * (int64_t)s.lse_hs + row[n].i] = log_of(top[n], total[n]);
     }
   }
   __syncthreads();
-  for (int e = threadIdx.x; e < R * D / 4; e += 256) {
-    const int r = e / (D / 4), c = e % (D / 4) * 4;
-    const Row w = row_of(a, s, x, x.rt * R + r);
-    if (!w.live) break;
-    const floatx4 y = *reinterpret_cast<const floatx4*>(ob + r * P::OROW + c);
-    if (x.slot >= 0) put4(a.part_o + ((int64_t)x.slot * R + r) * D + c, y);
-    else put4(static_cast<uint16_t*>(s.out) + w.h * elems(s.out_hs, 2) + w.i * elems(s.out_rs, 2) + c, y * ml[r].x);
-  }
+  write_joined<uint16_t, D, R, P::OROW>(a, s, x, ob, ml, flag);
+  __syncthreads();
+  form_flagged<uint16_t, D, R, KT>(a, s, x, flag, ml);
 }
 
 // ---------------------------------------------------------------------------
@@ -1018,6 +1121,7 @@ __global__ __launch_bounds__(512, 2) void attend_many(AttendArgs<N> a) {
   }
   l += __shfl_xor(l, 32);
   write_rows<uint16_t, D, R>(a, s, x, row, wave * 32 + col, half, o, m, l);
+  form_own<uint16_t, D, R, KT>(a, s, x, row, wave * 32, o, m, l);
 }
 
 // ---------------------------------------------------------------------------

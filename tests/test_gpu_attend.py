@@ -136,3 +136,48 @@ def test_flat_and_sharp_weights(dtype, scale, nq):
     torch.cuda.synchronize()
     c.check(True)
     attn.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), float("-inf")])
+@pytest.mark.parametrize("nq,nm,nt", [(4, 40, 30), (9, 0, 200), (60, 100, 130), (200, 0, 333), (3, 2100, 2000)])
+def test_rows_that_a_query_does_not_see_have_no_part(dtype, value, nq, nm, nt):
+    """Infinities and NaN in keys and values of the last rows: the queries before them are as without them, those that
+    see them get what the definition gives."""
+    attn = handle(6, 2, 64, dtype)
+    c = Case(attn, torch.Generator(device="cuda").manual_seed(nq), 6, 2, 64, dtype, nq, nm, nt)
+    clean = Case(attn, torch.Generator(device="cuda").manual_seed(nq), 6, 2, 64, dtype, nq, nm, nt)
+    at = nt - nq // 2 - 1                          # the first half of the queries does not see it
+    c.v[0, at, 5:9] = value
+    c.k[1, at, 0] = value
+    attn.omnimem_attend([c.query()])
+    attn.omnimem_attend([clean.query()])
+    torch.cuda.synchronize()
+    before = nq - (nt - at)                        # queries that do not see it
+    assert before >= 1
+    # Rows with such values are summed in another order and with weights that are not rounded: twice the bound above of
+    # the sums, and in bf16 half a step for the weights of the one and for each result.
+    reach = float((clean.q.float().abs().sum(-1).amax() * torch.cat([clean.k[:, :nt].float().flatten(),
+                  torch.tensor(clean.held[0], device="cuda").float().flatten()]).abs().amax()) * c.scale)
+    near = 2 * (2 * (64 + 6) * U * reach + 2 * (nm + nt + 8) * U) + (3 * 2.0 ** -8 if dtype == "bf16" else 0.0)
+    size = torch.cat([clean.v[:, :nt].float().flatten(), torch.tensor(clean.held[1], device="cuda").float().flatten()]).abs().amax()
+    assert ((c.out[:, :before].float() - clean.out[:, :before].float()).abs() <= near * size).all()
+    assert torch.equal(c.lse[:, :before], clean.lse[:, :before])
+    after, plain = c.out[:3, before: nq], clean.out[:3, before: nq]
+    assert (~torch.isfinite(after[..., 5:9])).all()            # (heads 0 .. 2 read KV head 0)
+    assert ((after[..., 9:].float() - plain[..., 9:].float()).abs() <= near * size).all()
+    attn.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("nq", [1, 40, 100])
+def test_products_that_are_all_minus_infinity_count_as_none(dtype, nq):
+    attn = handle(2, 1, 64, dtype)
+    c = Case(attn, torch.Generator(device="cuda").manual_seed(1), 2, 1, 64, dtype, nq, 0, nq)
+    c.q.fill_(1.0)
+    c.k[:, :nq] = 0.0
+    c.k[:, :nq, 0] = float("-inf")
+    attn.omnimem_attend([c.query()])
+    torch.cuda.synchronize()
+    assert (c.out[:, :nq] == 0).all() and torch.isneginf(c.lse[:, :nq]).all()
+    attn.close()
