@@ -10,6 +10,7 @@ from __future__ import annotations
 import ctypes
 import math
 import os
+import typing
 
 import torch
 
@@ -384,9 +385,21 @@ def make_chunk(k, v, modality):
 MEMORY_ROWS = 32   # rows of a memory block
 
 
+class _Layout(typing.NamedTuple):
+    """What a descriptor's tensors say of the handle and the rope that they fit (None: nothing)."""
+    n_q_heads: object = None
+    n_kv_heads: object = None
+    head_dim: object = None
+    dtype: object = None
+    device: object = None
+    axes: object = None
+
+
 def array_of(descriptors):
     """A ctypes array of descriptors of one type: built once, passed to any number of calls."""
-    return (type(descriptors[0]) * len(descriptors))(*descriptors)
+    arr = (type(descriptors[0]) * len(descriptors))(*descriptors)
+    arr._layouts = {d._layout for d in descriptors if hasattr(d, "_layout")}
+    return arr
 
 
 def memory_shape(n_kv_heads, head_dim, rows):
@@ -435,7 +448,7 @@ def make_rope(head_dim, inv_freq, axis=None, n_axes=None, rotary_dim=None, neigh
     r.inv_freq, r.axis = r._freq, r._axis
     r.q_weight, r.k_weight, r.eps = _ptr(q_weight), _ptr(k_weight), float(eps)
     r._weights = weights    # (kept alive with the descriptor)
-    r._dtypes = {w.dtype for w in weights}
+    r._layouts = {_Layout(head_dim=head_dim)} | {_Layout(dtype=w.dtype, device=w.device.index) for w in weights}
     return r
 
 
@@ -462,7 +475,7 @@ def make_projection(q, k, v, pos, q_out, k_out, v_out, modality=None, modality_o
     p.q_out, p.q_out_head_stride, p.q_out_row_stride = _ptr(q_out), q_out.stride(0), q_out.stride(1)
     p.k_out, p.v_out, p.out_head_stride, p.out_row_stride = _ptr(k_out), _ptr(v_out), k_out.stride(0), k_out.stride(1)
     p.modality, p.modality_out = _ptr(modality), _ptr(modality_out)
-    p._axes, p._dtype = pos.shape[0], q.dtype
+    p._layout = _Layout(q.shape[0], k.shape[0], q.shape[2], q.dtype, q.device.index, pos.shape[0])
     return p
 
 
@@ -473,6 +486,7 @@ def make_held(k, v, data):
     h = Held()
     h.k, h.v, h.kv_head_stride, h.kv_row_stride = _ptr(k), _ptr(v), k.stride(0), k.stride(1)
     h.data, h.data_head_stride, h.n_rows = _ptr(data), data.stride(0), k.shape[1]
+    h._layout = _Layout(None, k.shape[0], k.shape[2], k.dtype, k.device.index)
     return h
 
 
@@ -483,28 +497,32 @@ def make_query(q, out, k=None, v=None, memory=None, memory_rows=0, sm_scale=0.0,
     _rows("out", out)
     if out.shape != q.shape or out.dtype != q.dtype:
         raise ValueError("out must have q's shape and type")
-    x = Query()
-    x.q, x.q_head_stride, x.q_row_stride, x.n_queries = _ptr(q), q.stride(0), q.stride(1), q.shape[1]
-    x.out, x.out_head_stride, x.out_row_stride = _ptr(out), out.stride(0), out.stride(1)
-    x.sm_scale = float(sm_scale)
     if (k is None) != (v is None):
         raise ValueError("k and v must both be given")
     if k is not None:
         _rows("k and v", k, v)
         if k.dtype != q.dtype or k.shape[2] != q.shape[2]:
             raise ValueError("k and v must have q's type and width")
-        x.k, x.v, x.kv_head_stride, x.kv_row_stride, x.n_tail = _ptr(k), _ptr(v), k.stride(0), k.stride(1), k.shape[1]
     if memory is not None:
         _memory(memory, int(memory_rows), k)
         if memory.shape[2] != 34 * q.shape[2]:
             raise ValueError("the memory's width differs from the queries'")
-        x.memory, x.memory_head_stride, x.memory_rows = _ptr(memory), memory.stride(0), int(memory_rows)
     elif memory_rows:
         raise ValueError("memory_rows without a memory")
+    if lse is not None and (lse.dtype != torch.float32 or lse.shape != q.shape[:2] or lse.stride(1) != 1):
+        raise ValueError("lse must be fp32 [H_q, n], its queries contiguous")
+    x = Query()
+    x.q, x.q_head_stride, x.q_row_stride, x.n_queries = _ptr(q), q.stride(0), q.stride(1), q.shape[1]
+    x.out, x.out_head_stride, x.out_row_stride = _ptr(out), out.stride(0), out.stride(1)
+    x.sm_scale = float(sm_scale)
+    if k is not None:
+        x.k, x.v, x.kv_head_stride, x.kv_row_stride, x.n_tail = _ptr(k), _ptr(v), k.stride(0), k.stride(1), k.shape[1]
+    if memory is not None:
+        x.memory, x.memory_head_stride, x.memory_rows = _ptr(memory), memory.stride(0), int(memory_rows)
     if lse is not None:
-        if lse.dtype != torch.float32 or lse.shape != q.shape[:2] or lse.stride(1) != 1:
-            raise ValueError("lse must be fp32 [H_q, n], its queries contiguous")
         x.lse, x.lse_head_stride = _ptr(lse), lse.stride(0)
+    kv = k if k is not None else memory
+    x._layout = _Layout(q.shape[0], kv.shape[0] if kv is not None else None, q.shape[2], q.dtype, q.device.index)
     return x
 
 
@@ -523,20 +541,34 @@ class Attention:
             raise OmnimemError(st, lib.omnimem_attn_last_error(None).decode())
         self.handle = handle
         self.device = torch.cuda.current_device()
+        self._layout = _Layout(n_q_heads, n_kv_heads, head_dim, torch.bfloat16 if dtype == BF16 else torch.float32, self.device)
+        self._fits = set()      # layouts that were compared
 
-    def _call(self, function, descriptors, kind, *more, stream=None):
-        if len(descriptors) and not (isinstance(descriptors, ctypes.Array) and descriptors._type_ is kind):
-            descriptors = (kind * len(descriptors))(*descriptors)
+    def _check_layouts(self, layouts):
+        for layout in layouts - self._fits:
+            for name, want, got in zip(_Layout._fields, self._layout, layout):
+                if want is not None and got is not None and want != got:
+                    raise ValueError(f"the handle's {name} is {want}, a descriptor's {got}")
+            self._fits.add(layout)
+
+    def _call(self, function, descriptors, kind, *more, before=(), stream=None):
+        if not (isinstance(descriptors, ctypes.Array) and descriptors._type_ is kind):
+            descriptors = array_of(descriptors) if len(descriptors) else None
+        n = len(descriptors) if descriptors is not None else 0
+        self._check_layouts(getattr(descriptors, "_layouts", frozenset()))
         # (the raw handle costs a tenth of a microsecond, a Stream object a whole one: a fifth of a small call)
         s = stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(self.device)
-        before, after = (more[:1], more[1:]) if kind is Projection else ((), more)
-        st = function(self.handle, *before, descriptors if len(descriptors) else None, len(descriptors), *after, s)
+        st = function(self.handle, *before, descriptors, n, *more, s)
         if st != OK:
             raise OmnimemError(st, self._lib.omnimem_attn_last_error(self.handle).decode())
 
     # Same names as the C ABI.
     def omnimem_rotate(self, rope, projections, stream=None):
-        self._call(self._lib.omnimem_rotate, projections, Projection, ctypes.byref(rope), stream=stream)
+        self._check_layouts(getattr(rope, "_layouts", frozenset()))
+        for layout in getattr(projections, "_layouts", None) or {p._layout for p in projections if hasattr(p, "_layout")}:
+            if layout.axes < rope.n_axes:
+                raise ValueError(f"the rope has {rope.n_axes} axes, a projection positions for {layout.axes}")
+        self._call(self._lib.omnimem_rotate, projections, Projection, before=(ctypes.byref(rope),), stream=stream)
 
     def omnimem_pack(self, held, stream=None):
         self._call(self._lib.omnimem_pack, held, Held, stream=stream)

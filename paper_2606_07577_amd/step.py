@@ -51,6 +51,7 @@ class DeviceStep:
         self.layer_budgets = torch.zeros(self.n_layers, device=dev, dtype=torch.int32)
         self.fixed_budgets = False          # run() splits self.layer_budgets instead of Eq. (14)
         self.lse_in = [None] * self.n_layers
+        self.attn = None                    # made by attend()
         self.descs = self._descs()
 
     def _descs(self):
@@ -78,6 +79,23 @@ class DeviceStep:
     def select_compact(self, stream=None, a=None, s=None, budgets=None):
         self.ctx.omnimem_select_compact(self.descs, self.a if a is None else a, self.s if s is None else s,
                                         self.budgets if budgets is None else budgets, self.idx, stream)
+
+    def attend(self, stream=None):
+        """The chunk's attention over the working sets (Eq. 1), all layers in
+        one call: self.attn_out[l] [H_q, C, d] (query-major in memory, as the
+        output projection takes it), and its log-sum-exp, which the score
+        stage then takes instead of computing it."""
+        if self.attn is None:
+            self.attn = om.Attention(self.h_q, self.h_kv, self.d, om.BF16 if self.dtype_name == "bf16" else om.F32)
+            chunk = [n - c for n, c in zip(self.n, self.n_cache)]
+            self.attn_out = [torch.zeros((c, self.h_q, self.d), device=self.device, dtype=self.tdtype).transpose(0, 1)
+                             for c in chunk]
+            lse = [torch.zeros((self.h_q, c), device=self.device, dtype=torch.float32) for c in chunk]
+            self._queries = om.array_of([om.make_query(self.q[l], self.attn_out[l], self.k[l], self.v[l],
+                                                       sm_scale=self.sm_scale[l], lse=lse[l])
+                                         for l in range(self.n_layers)])
+            self.set_lse_inputs(lse)
+        self.attn.omnimem_attend(self._queries, self.ctx.cfg.causal, stream)
 
     # offline budgets (calibration) ----------------------------------------
     def calibrate(self, stream=None, a=None, s=None):
@@ -119,6 +137,8 @@ class DeviceStep:
         return t[l].cpu().numpy()
 
     def close(self):
+        if self.attn is not None:
+            self.attn.close()
         self.ctx.close()
 
 
@@ -187,6 +207,7 @@ class StreamRunner:
         self.fallbacks = 0         # steps compacted out of place for lack of staging rows
         self.keep_working_set = keep_working_set
         self.working_set = None    # [L] of (k, v, modality) copies of the last step's working set
+        self.attn = None           # made by hold() and restore()
         self._layers = (om.Layer * n_layers)()
         self._chunks = (om.Chunk * n_layers)()
         self._budget_ready = torch.cuda.Event()
@@ -221,6 +242,44 @@ class StreamRunner:
         mb[:m_v] = 0
         mb[m_v:m] = 1
         self.n_cache[l] = m
+
+    # memories ------------------------------------------------------------
+    def hold(self, stream=None):
+        """The kept rows of every layer in 4 bits (a HeldMemory): what answers
+        are read from (see Reader), a quarter of the cache's bytes to keep
+        until the stream goes on (see restore)."""
+        budgets = self.finish()
+        if budgets is None:
+            budgets = self._held_budgets()
+        if self.attn is None:
+            self.attn = om.Attention(self.h_q, self.h_kv, self.d, om.BF16 if self.tdtype == torch.bfloat16 else om.F32)
+        data = [torch.empty(om.memory_shape(self.h_kv, self.d, n), dtype=torch.uint8, device=self.device)
+                for n in self.n_cache]
+        self.attn.omnimem_pack(self._held(data), stream)
+        return HeldMemory(data, list(self.n_cache), [int(b) for b in budgets[:, 0]])
+
+    def restore(self, held, stream=None):
+        """Take a held memory's rows, as they are held, for the retained caches."""
+        self.finish()
+        if len(held.rows) != self.L or max(held.rows) > self.cache_cap:
+            raise ValueError("the memory has another number of layers, or more rows than the caches hold")
+        if self.attn is None:
+            self.attn = om.Attention(self.h_q, self.h_kv, self.d, om.BF16 if self.tdtype == torch.bfloat16 else om.F32)
+        self.n_cache = list(held.rows)
+        self.attn.omnimem_unpack(self._held(held.data), stream)
+        with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream()):
+            for mod, n, visual in zip(self.mbuf[self.cur], held.rows, held.visual):
+                mod[:visual] = 0
+                mod[visual:n] = 1
+
+    def _held(self, data):
+        return [om.make_held(self.kbuf[self.cur][l][:, : self.n_cache[l]], self.vbuf[self.cur][l][:, : self.n_cache[l]], data[l])
+                for l in range(self.L)]
+
+    def _held_budgets(self):
+        """Kept visual and audio rows of the caches as they are."""
+        audio = [int(m[:n].sum()) for m, n in zip(self.mbuf[self.cur], self.n_cache)]
+        return np.array([[n - a, a] for n, a in zip(self.n_cache, audio)], dtype=np.int32)
 
     # one step ----------------------------------------------------------
     def _describe(self, chunk, qs, cur):
@@ -374,4 +433,72 @@ class StreamRunner:
 
     def close(self):
         self.finish()
+        if self.attn is not None:
+            self.attn.close()
         self.ctx.close()
+
+
+class HeldMemory:
+    """A stream's kept rows in 4 bits: data[l] uint8 [H_kv, blocks, 34 d],
+    rows[l] kept rows, visual[l] of them visual (in front)."""
+
+    def __init__(self, data, rows, visual):
+        self.data, self.rows, self.visual = data, rows, visual
+
+
+class Reader:
+    """Answers from the memories of several streams at once: every layer's
+    tokens so far lie in a tail of their own behind each stream's memory.
+
+    A model calls layer() for each of its layers with the projections of the
+    streams' next tokens (a prompt's, or one each), in order, and next() after
+    the last layer.  `capacity`: tail rows of a stream.
+    """
+
+    def __init__(self, memories, h_q, h_kv, d, rope, capacity, dtype="bf16", device="cuda", sm_scale=0.0):
+        self.device = torch.device(device)
+        self.tdtype = torch.bfloat16 if dtype == "bf16" else torch.float32
+        self.h_q, self.h_kv, self.d, self.cap = h_q, h_kv, d, int(capacity)
+        self.memories, self.rope, self.sm_scale = list(memories), rope, float(sm_scale)
+        self.attn = om.Attention(h_q, h_kv, d, om.BF16 if dtype == "bf16" else om.F32)
+        n_layers = len(self.memories[0].data)
+        shape = (n_layers, len(self.memories), h_kv, self.cap, d)
+        self.k, self.v = (torch.zeros(shape, device=self.device, dtype=self.tdtype) for _ in range(2))
+        self.tail = [0] * len(self.memories)     # tail rows of each stream
+        self._new = None                         # and those that the current tokens add
+
+    def layer(self, l, q, k, v, pos, stream=None):
+        """One layer of the streams' next tokens: for each stream b q[b] [H_q,
+        n_b, d], k[b] and v[b] [H_kv, n_b, d] as projected, and their positions
+        pos[b] int32 [axes, n_b].  Keys and queries are normalised and rotated,
+        keys and values go behind the stream's tail, and the queries attend to
+        its memory and tail.  Returns [H_q, n_b, d] for each stream."""
+        new = [x.shape[1] for x in k]
+        if self._new is not None and new != self._new:
+            raise ValueError("every layer takes the same numbers of tokens (next() begins the next ones)")
+        if any(t + n > self.cap for t, n in zip(self.tail, new)):
+            raise ValueError(f"more than {self.cap} tail rows")
+        self._new = new
+        rows, queries, outs, rotated = [], [], [], []   # (rotated: the queries, kept until the calls are queued)
+        with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream()):
+            for b, (t, n) in enumerate(zip(self.tail, new)):
+                q_rot = torch.empty((n, self.h_q, self.d), device=self.device, dtype=self.tdtype).transpose(0, 1)
+                out = torch.empty_like(q_rot)
+                kc, vc, mem = self.k[l, b], self.v[l, b], self.memories[b]
+                rows.append(om.make_projection(q[b], k[b], v[b], pos[b], q_rot, kc[:, t: t + n], vc[:, t: t + n]))
+                queries.append(om.make_query(q_rot, out, kc[:, : t + n], vc[:, : t + n], mem.data[l] if mem.rows[l] else None,
+                                             mem.rows[l], self.sm_scale))
+                outs.append(out)
+                rotated.append(q_rot)
+        self.attn.omnimem_rotate(self.rope, rows, stream)
+        self.attn.omnimem_attend(queries, True, stream)
+        return outs
+
+    def next(self):
+        """The tokens of the last layer() calls are part of the tails."""
+        if self._new is not None:
+            self.tail = [t + n for t, n in zip(self.tail, self._new)]
+        self._new = None
+
+    def close(self):
+        self.attn.close()

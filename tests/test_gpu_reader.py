@@ -1,0 +1,199 @@
+"""The operators around the step as they are used together: a chunk's attention and the scores that take its
+log-sum-exp, a stream's caches held in 4 bits and brought back, answers read from held memories, and a token's calls
+captured into a graph."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import operators_oracle as orc
+from paper_2606_07577_amd import omnimem as om
+from paper_2606_07577_amd import synth
+from paper_2606_07577_amd.step import DeviceStep, HeldMemory, Reader, StreamRunner
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+
+
+def host(t):
+    return t.double().cpu().numpy()
+
+
+def stream_chunk(g, layers, h_q, h_kv, d, n, dtype=torch.bfloat16):
+    rnd = lambda *s: torch.randn(*s, generator=g, device="cuda").to(dtype)
+    mod = (torch.arange(n, device="cuda") % 4 == 3).to(torch.uint8)
+    return [dict(q=rnd(h_q, n, d), k=rnd(h_kv, n, d), v=rnd(h_kv, n, d), modality=mod, sm_scale=d ** -0.5)
+            for _ in range(layers)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_the_chunks_attention_gives_the_scores_their_lse(dtype):
+    """Scores that take attend()'s log-sum-exp are those that compute it.  Both are sums of exp(s - lse) over the chunk's
+    queries: a difference of the two lse is a relative one of their terms.  Each is off by at most (d + 6) u S + (N + 8) u
+    + 2 u |lse| (S: the largest sum of |q||k| scale), below 2^-12 here; the sums themselves add (C + 8) u each."""
+    layer = synth.make_layer([3, 1], h_q=8, h_kv=2, d=128, n_cache_v=301, n_cache_a=77, n_frames=3, frame_v=41, frame_a=13,
+                             dup_frac=0.3, head_scale=(0.5, 2.0), dtype=dtype)
+    plain, step = DeviceStep([layer], 250), DeviceStep([layer], 250)
+    plain.score()
+    step.attend()
+    step.score()
+    torch.cuda.synchronize()
+    n, c = step.n[0], step.n[0] - step.n_cache[0]
+    q, k, v = host(step.q[0]), host(step.k[0]), host(step.v[0])
+    _, lse, _, reach = orc.attend(q, k, v, 0, step.sm_scale[0], True)
+    bound = float(((128 + 6) * U * reach + (n + 8) * U + 2 * U * np.abs(lse)).max())
+    assert bound < 2.0 ** -12
+    a, b = plain.host("a", 0), step.host("a", 0)
+    assert (np.abs(a - b) <= (2 * bound + 2 * (4 * c + 8) * U) * np.abs(a) + 1e-30).all()
+    assert np.array_equal(step.host("lse", 0), step.lse_in[0].cpu().numpy())
+    step.run()                                     # and the whole step goes on from there
+    torch.cuda.synchronize()
+    assert int(step.budgets.sum()) == 250
+    plain.close()
+    step.close()
+
+
+def test_a_streams_caches_held_and_brought_back():
+    layers, h_q, h_kv, d, n = 3, 4, 2, 64, 160
+    g = torch.Generator(device="cuda").manual_seed(6)
+    run = StreamRunner(layers, h_q, h_kv, d, n, 300)
+    for _ in range(3):
+        budgets = run.push(stream_chunk(g, layers, h_q, h_kv, d, n))
+    held = run.hold()
+    again = run.hold()                             # (no step in between: the rows' modality says what is visual)
+    torch.cuda.synchronize()
+    assert held.rows == again.rows == [int(b.sum()) for b in budgets] and held.visual == again.visual == [int(b[0]) for b in budgets]
+    other = StreamRunner(layers, h_q, h_kv, d, n, 300)
+    other.restore(held)
+    torch.cuda.synchronize()
+    for l in range(layers):
+        want = orc.pack(host(run.cache_k(l)), host(run.cache_v(l)))
+        assert np.array_equal(held.data[l].cpu().numpy(), want) and torch.equal(held.data[l], again.data[l])
+        k, v = orc.unpack(want, held.rows[l])
+        assert np.array_equal(host(other.cache_k(l)), k) and np.array_equal(host(other.cache_v(l)), v)
+        assert torch.equal(other.cache_modality(l), run.cache_modality(l))
+    other.push(stream_chunk(g, layers, h_q, h_kv, d, n))   # the stream goes on
+    assert sum(other.n_cache) == 300
+    with pytest.raises(ValueError):
+        StreamRunner(layers, h_q, h_kv, d, n, 30).restore(held)
+    run.close()
+    other.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_answers_from_held_memories(dtype):
+    """Prompts of different lengths over three memories (one empty), then single tokens: each layer's result against the
+    definition on the memories' values and the rotated rows as the library wrote them (their own bounds are tested with
+    the rotation)."""
+    td = torch.bfloat16 if dtype == "bf16" else torch.float32
+    layers, h_q, h_kv, d, cap = 2, 6, 2, 64, 40
+    g = torch.Generator(device="cuda").manual_seed(8)
+    rnd = lambda *s: torch.randn(*s, generator=g, device="cuda").to(td)
+    attn = om.Attention(h_q, h_kv, d, om.BF16 if dtype == "bf16" else om.F32)
+    memories = []
+    for rows in (77, 0, 300):
+        data = [torch.zeros(om.memory_shape(h_kv, d, rows), dtype=torch.uint8, device="cuda") for _ in range(layers)]
+        if rows:
+            attn.omnimem_pack([om.make_held(rnd(h_kv, rows, d), rnd(h_kv, rows, d), x) for x in data])
+        memories.append(HeldMemory(data, [rows] * layers, [rows // 2] * layers))
+    freq = [1000.0 ** (-j / 16) for j in range(16)]
+    axis = [j % 3 for j in range(16)]
+    weight = rnd(2, d)
+    rope = om.make_rope(d, freq, axis, q_weight=weight[0], k_weight=weight[1])
+    reader = Reader(memories, h_q, h_kv, d, rope, cap, dtype=dtype)
+    tails = [[([], []) for _ in memories] for _ in range(layers)]
+    for lengths in ([5, 17, 1], [1, 1, 1], [1, 1, 1]):
+        for l in range(layers):
+            q, k, v = ([rnd(h, n, d) for n in lengths] for h in (h_q, h_kv, h_kv))
+            pos = [torch.randint(0, 5000, (3, n), generator=g, device="cuda").to(torch.int32) for n in lengths]
+            outs = reader.layer(l, q, k, v, pos)
+            torch.cuda.synchronize()
+            for b, n in enumerate(lengths):
+                t = reader.tail[b]
+                p = pos[b].cpu().numpy()
+                kr = orc.rotate(host(k[b]), p, freq, axis, 32, False, host(weight[1]), 1e-6)
+                got = host(reader.k[l, b, :, t: t + n])
+                assert np.abs(got - kr).max() <= torch.finfo(td).eps * np.abs(kr).max() + 64 * U * np.abs(kr).max()
+                assert torch.equal(reader.v[l, b, :, t: t + n], v[b])
+                qr = torch.zeros(h_q, n, d, device="cuda", dtype=td)
+                kv = torch.zeros(2, h_kv, n, d, device="cuda", dtype=td)
+                attn.omnimem_rotate(rope, [om.make_projection(q[b], k[b], v[b], pos[b], qr, kv[0], kv[1])])
+                torch.cuda.synchronize()
+                mk, mv = orc.unpack(memories[b].data[l].cpu().numpy(), memories[b].rows[l])
+                kk = np.concatenate([mk, host(reader.k[l, b, :, : t + n])], 1)
+                vv = np.concatenate([mv, host(reader.v[l, b, :, : t + n])], 1)
+                out, _, size, reach = orc.attend(host(qr), kk, vv, memories[b].rows[l], d ** -0.5, True)
+                half = torch.finfo(td).eps / 2 if dtype == "bf16" else 0.0
+                near = 2 * (d + 6) * U * reach[..., None] + 2 * (kk.shape[1] + 8) * U + half
+                off = np.abs(host(outs[b]) - out) / (size * near + (half or U) * np.abs(out))
+                assert off.max() <= 1, (l, b, lengths, off.max((1, 2)), off.max((0, 2)))
+        reader.next()
+    assert reader.tail == [7, 19, 3]
+    with pytest.raises(ValueError):
+        reader.layer(0, [rnd(h_q, 40, d)] * 3, [rnd(h_kv, 40, d)] * 3, [rnd(h_kv, 40, d)] * 3, [pos[0]] * 3)
+    reader.close()
+    attn.close()
+
+
+def test_a_tokens_calls_captured_and_replayed():
+    """Rotation, packing and attention of a token in one graph: every replay gives what the calls give on the same
+    buffers, with eager work and other graphs' replays between."""
+    h_q, h_kv, d, rows, tail = 7, 1, 128, 1500, 40
+    g = torch.Generator(device="cuda").manual_seed(9)
+    rnd = lambda *s: torch.randn(*s, generator=g, device="cuda").bfloat16()
+    attn, eager = om.Attention(h_q, h_kv, d), om.Attention(h_q, h_kv, d)
+    rope = om.make_rope(d, [0.8 ** j for j in range(64)])
+    k, v, kc, vc = rnd(h_kv, rows, d), rnd(h_kv, rows, d), rnd(h_kv, tail, d), rnd(h_kv, tail, d)
+    q, kn, vn = rnd(h_q, 1, d), rnd(h_kv, 1, d), rnd(h_kv, 1, d)
+    pos = torch.tensor([[12345]], dtype=torch.int32, device="cuda")
+    data = torch.zeros(om.memory_shape(h_kv, d, rows), dtype=torch.uint8, device="cuda")
+    q_rot, out = torch.zeros_like(q), torch.zeros(2, h_q, 1, d, device="cuda", dtype=torch.bfloat16)
+
+    def calls(a, to, stream=None):
+        a.omnimem_pack([om.make_held(k, v, data)], stream)
+        a.omnimem_rotate(rope, [om.make_projection(q, kn, vn, pos, q_rot, kc[:, -1:], vc[:, -1:])], stream)
+        a.omnimem_attend([om.make_query(q_rot, to, kc, vc, data, rows)], True, stream)
+
+    calls(attn, out[0])
+    torch.cuda.synchronize()
+    stream = torch.cuda.Stream()
+    graphs = []
+    for _ in range(2):                             # two graphs of one handle, replayed one after the other
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            calls(attn, out[0], stream)
+        graphs.append(graph)
+    for i in range(6):
+        for t in (k, v, q, kn, vn):
+            t.copy_(rnd(*t.shape))
+        pos.fill_(1000 * i)
+        out.fill_(7.0)
+        torch.cuda.synchronize()
+        graphs[i % 2].replay()
+        torch.cuda.synchronize()
+        got, memory, rotated = out[0].clone(), data.clone(), kc.clone()
+        calls(eager, out[1])
+        torch.cuda.synchronize()
+        assert torch.equal(got, out[1]) and torch.equal(memory, data) and torch.equal(rotated, kc)
+    attn.close()
+    eager.close()
+
+
+def test_handles_on_two_streams_at_once():
+    """Two handles on two streams: results are those of one after the other."""
+    h_q, h_kv, d, rows = 7, 1, 128, 6000
+    g = torch.Generator(device="cuda").manual_seed(10)
+    rnd = lambda *s: torch.randn(*s, generator=g, device="cuda").bfloat16()
+    handles = [om.Attention(h_q, h_kv, d) for _ in range(2)]
+    q, k, v = rnd(2, h_q, 3, d), rnd(2, h_kv, rows, d), rnd(2, h_kv, rows, d)
+    out, ref = torch.zeros_like(q), torch.zeros_like(q)
+    for b in range(2):
+        handles[b].omnimem_attend([om.make_query(q[b], ref[b], k[b], v[b])])
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(20):
+        for b in range(2):
+            handles[b].omnimem_attend([om.make_query(q[b], out[b], k[b], v[b])], stream=streams[b])
+    torch.cuda.synchronize()
+    assert torch.equal(out, ref)
+    for h in handles:
+        h.close()
