@@ -36,6 +36,7 @@ struct Unit {
   int k0, k1;                // key tiles
   int mem_tiles;             // of the sequence
   int slot;                  // partial, or -1: the result is final
+  int split, splits;         // its share of the row tile
 };
 // The last sequence whose entry of `first` is at most u (lane-parallel).
 template <int N>
@@ -48,25 +49,27 @@ __device__ inline int seq_of(const int32_t (&first)[N], int n, int u) {
 template <int R, int KT, int N>
 __device__ inline Unit unit_of(const AttendArgs<N>& a, int u) {
   Unit x;
-  int split = 0, splits = 1, tile;
+  int tile;
+  x.split = 0;
+  x.splits = 1;
   x.slot = -1;
   if (a.whole > 0) {
     tile = u;
     if (u >= a.whole) {
-      splits = a.seq[0].splits;
+      x.splits = a.seq[0].splits;
       x.slot = u - a.whole;
-      tile = a.whole + x.slot / splits;
-      split = x.slot % splits;
+      tile = a.whole + x.slot / x.splits;
+      x.split = x.slot % x.splits;
     }
     x.s = seq_of(a.unit0, a.n_seqs, tile);
     tile -= a.unit0[x.s];
   } else {
     x.s = seq_of(a.unit0, a.n_seqs, u);
     u -= a.unit0[x.s];
-    splits = a.seq[x.s].splits;
-    if (splits > 1) x.slot = a.seq[x.s].slot0 + u;
-    tile = u / splits;
-    split = u % splits;
+    x.splits = a.seq[x.s].splits;
+    if (x.splits > 1) x.slot = a.seq[x.s].slot0 + u;
+    tile = u / x.splits;
+    x.split = u % x.splits;
   }
   const QuerySeq& s = a.seq[x.s];
   x.g = tile / s.row_tiles;
@@ -75,8 +78,8 @@ __device__ inline Unit unit_of(const AttendArgs<N>& a, int u) {
   x.mem_tiles = tiles_of<KT>(s.nm);
   const int last = (min((x.rt + 1) * R, x.rows) - 1) / a.group;
   const int tiles = x.mem_tiles + tiles_of<KT>(tail_seen(s, a.causal, last));
-  x.k0 = (int)((int64_t)tiles * split / splits);
-  x.k1 = (int)((int64_t)tiles * (split + 1) / splits);
+  x.k0 = (int)((int64_t)tiles * x.split / x.splits);
+  x.k1 = (int)((int64_t)tiles * (x.split + 1) / x.splits);
   return x;
 }
 
@@ -99,6 +102,19 @@ __device__ inline void put4(uint16_t* p, floatx4 x) { *reinterpret_cast<uint2*>(
 __device__ inline void put4(float* p, floatx4 x) { *reinterpret_cast<floatx4*>(p) = x; }
 __device__ inline void put1(uint16_t* p, float x) { *p = (uint16_t)round2(x, 0.0f); }
 __device__ inline void put1(float* p, float x) { *p = x; }
+// Partials pass between workgroups of one launch: they are written to and read
+// from the device's coherent memory (8 bytes at a time, past the XCD's L2), and
+// a wait for the writes orders them before the count of the units that wrote
+// theirs.  A release of all that the L2 holds, and an acquire, are not needed:
+// with them at the end of each unit 32 users' tokens took 58 us instead of 50.
+__device__ inline void share8(float* p, float x, float y) {
+  const uint64_t v = (uint64_t)__float_as_uint(y) << 32 | __float_as_uint(x);
+  __hip_atomic_store(reinterpret_cast<uint64_t*>(p), v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ inline floatx2 shared8(const float* p) {
+  const uint64_t v = __hip_atomic_load(reinterpret_cast<const uint64_t*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return floatx2{__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32))};
+}
 __device__ inline float log_of(float m, float l) { return l == 0.0f ? -INFINITY : (m + log2f(l)) * kLn2; }
 
 // ---------------------------------------------------------------------------
@@ -164,21 +180,15 @@ __device__ __forceinline__ void form_again(const AttendArgs<N>& a, const QuerySe
     add(k, v);
   }
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");   // (after what the wavefront wrote there)
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");   // (after what the workgroup wrote there)
 #pragma unroll
   for (int i = 0; i < C; ++i) {
     const int c = lane + i * 64;
-    if (x.slot >= 0) a.part_o[((int64_t)x.slot * R + r) * D + c] = o[i];
+    if (x.slot >= 0) __hip_atomic_store(a.part_o + ((int64_t)x.slot * R + r) * D + c, o[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     else put1(static_cast<T*>(s.out) + row.h * elems(s.out_hs, E) + row.i * elems(s.out_rs, E) + c, o[i] * inv);
   }
 }
-// The same for the rows of a workgroup whose flags are set (in LDS, with their
-// statistics), and for a wavefront's own 32 rows (a lane each, twice).
-template <typename T, int D, int R, int KT, int N>
-__device__ __forceinline__ void form_flagged(const AttendArgs<N>& a, const QuerySeq& s, const Unit& x, const int* flag, const float2* ml) {
-  for (int r = wave_id(); r < R; r += (int)blockDim.x / 64)
-    if (uniform(flag[r])) form_again<T, D, R, KT>(a, s, x, r, ml[r].x, ml[r].y);
-}
+// The same for a wavefront's own 32 rows (a lane each, twice).
 template <typename T, int D, int R, int KT, int N>
 __device__ __forceinline__ void form_own(const AttendArgs<N>& a, const QuerySeq& s, const Unit& x, const Row& row, int r0,
                                 const floatx16 (&o)[D / 32], float m, float l) {
@@ -195,23 +205,122 @@ __device__ __forceinline__ void form_own(const AttendArgs<N>& a, const QuerySeq&
   }
 }
 
-// A workgroup's joined sums [R][ROW] in LDS to its partial or, divided, to the
-// output; flags the rows that are not finite.
-template <typename T, int D, int R, int ROW, int N>
-__device__ inline void write_joined(const AttendArgs<N>& a, const QuerySeq& s, const Unit& x, const float* ob, const float2* ml, int* flag) {
-  constexpr int E = (int)sizeof(T);
-  for (int e = threadIdx.x; e < R * D / 4; e += blockDim.x) {
-    const int r = e / (D / 4), c = e % (D / 4) * 4;
+// The end of a unit whose wavefronts have sums of their own, in LDS [WAVES]
+// [R][ROW], taken by their share of the row's maximum: added up, they go to the
+// output or, with more than one unit to the row tile, to a partial.  The last
+// unit of a row tile to write its partial joins them all (`arrived` counts
+// them, and is 0 again afterwards), in the order of the keys, unless that is
+// more work than a kernel for it (see kJoinBatches).
+struct Joint {
+  float2 ml[64];             // (maximum, sum) of a row
+  int flag[64];              // its sums are not finite
+  int last;
+};
+template <typename T, int D, int R, int KT, int ROW, int WAVES, int N>
+__device__ __forceinline__ void finish(const AttendArgs<N>& a, const QuerySeq& s, const Unit& x, float* ob, Joint* joint) {
+  static_assert(R <= 64, "rows of a Joint");
+  constexpr int E = (int)sizeof(T), THREADS = 64 * WAVES, TPR = D / 4;
+  const int tid = threadIdx.x, live = min(R, x.rows - x.rt * R);
+  const auto put_row = [&](int r, int c, floatx4 y, float l) __attribute__((always_inline)) {
     const Row row = row_of(a, s, x, x.rt * R + r);
-    if (!row.live) break;
-    const floatx4 y = *reinterpret_cast<const floatx4*>(ob + r * ROW + c);
+    put4(static_cast<T*>(s.out) + row.h * elems(s.out_hs, E) + row.i * elems(s.out_rs, E) + c, y * (l == 0.0f ? 0.0f : 1.0f / l));
+  };
+  const auto put_lse = [&](int r, float m, float l) __attribute__((always_inline)) {
+    const Row row = row_of(a, s, x, x.rt * R + r);
+    if (s.lse) s.lse[row.h * (int64_t)s.lse_hs + row.i] = log_of(m, l);
+  };
+  if (tid < R) joint->flag[tid] = 0;
+  __syncthreads();
+  for (int e = tid; e < live * TPR; e += THREADS) {
+    const int r = e / TPR, c = e % TPR * 4;
+    floatx4 y = floatx4{};
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) y += *reinterpret_cast<const floatx4*>(ob + (w * R + r) * ROW + c);
     if (x.slot >= 0) {
-      put4(a.part_o + ((int64_t)x.slot * R + r) * D + c, y);
+      float* p = a.part_o + ((int64_t)x.slot * R + r) * D + c;
+      if (a.joined) {
+        share8(p, y[0], y[1]);
+        share8(p + 2, y[2], y[3]);
+      } else {
+        put4(p, y);
+      }
     } else {
-      const float l = ml[r].y;
-      put4(static_cast<T*>(s.out) + row.h * elems(s.out_hs, E) + row.i * elems(s.out_rs, E) + c, y * (l == 0.0f ? 0.0f : 1.0f / l));
+      put_row(r, c, y, joint->ml[r].y);
     }
-    if (x.k1 > x.mem_tiles && (y[0] + y[1] + y[2] + y[3]) * 0.0f != 0.0f) flag[r] = 1;
+    if (x.k1 > x.mem_tiles && (y[0] + y[1] + y[2] + y[3]) * 0.0f != 0.0f) joint->flag[r] = 1;
+  }
+  if (tid < live) {
+    const float2 ml = joint->ml[tid];
+    if (x.slot >= 0) share8(&a.part_ml[(int64_t)x.slot * R + tid].x, ml.x, ml.y);
+    else put_lse(tid, ml.x, ml.y);
+  }
+  __syncthreads();
+  for (int r = wave_id(); r < live; r += WAVES)
+    if (uniform(joint->flag[r])) form_again<T, D, R, KT>(a, s, x, r, joint->ml[r].x, joint->ml[r].y);
+  if (x.slot < 0 || !a.joined) return;
+
+  const int first = x.slot - x.split;
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");         // (this wavefront's part of the partial is in coherent memory)
+  __syncthreads();
+  if (tid == 0)
+    joint->last = __hip_atomic_fetch_add(a.arrived + first, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == x.splits - 1;
+  __syncthreads();
+  if (!joint->last) return;
+  if (tid == 0) __hip_atomic_store(a.arrived + first, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  // `shares` threads to a row's 4 channels, with 8 partials on their way each
+  const int items = live * TPR;
+  int shares = 1;
+  while (2 * shares * items <= THREADS && shares < x.splits) shares *= 2;
+  floatx4* os = reinterpret_cast<floatx4*>(ob);            // [shares][items], and their statistics
+  float2* mls = reinterpret_cast<float2*>(os + THREADS);
+  for (int e = tid; e < items * shares; e += THREADS) {
+    const int item = e % items, r = item / TPR, c = item % TPR * 4;
+    const float* ml = &a.part_ml[(int64_t)first * R + r].x;
+    const float* po = a.part_o + ((int64_t)first * R + r) * D + c;
+    float m = -INFINITY, l = 0.0f;
+    floatx4 o = floatx4{};
+    for (int p0 = e / items; p0 < x.splits; p0 += 8 * shares) {
+      floatx2 y[8], z[8][2];
+#pragma unroll
+      for (int b = 0; b < 8; ++b) {
+        const int64_t p = min(p0 + b * shares, x.splits - 1);
+        y[b] = shared8(ml + p * R * 2);
+        z[b][0] = shared8(po + p * R * D);
+        z[b][1] = shared8(po + p * R * D + 2);
+      }
+#pragma unroll
+      for (int b = 0; b < 8; ++b) {
+        if (p0 + b * shares >= x.splits) break;
+        const float m2 = fmaxf(m, y[b][0]), ref = m2 == -INFINITY ? 0.0f : m2;
+        const float was = exp2_(m - ref), is = exp2_(y[b][0] - ref);
+        l = l * was + y[b][1] * is;
+        o = o * was + floatx4{z[b][0][0], z[b][0][1], z[b][1][0], z[b][1][1]} * is;
+        m = m2;
+      }
+    }
+    if (shares == 1) {
+      put_row(r, c, o, l);
+      if (c == 0) put_lse(r, m, l);
+    } else {
+      os[e] = o;
+      mls[e] = make_float2(m, l);
+    }
+  }
+  if (shares == 1) return;
+  __syncthreads();
+  for (int e = tid; e < items; e += THREADS) {
+    const int r = e / TPR, c = e % TPR * 4;
+    float m = -INFINITY, l = 0.0f;
+    for (int p = 0; p < shares; ++p) m = fmaxf(m, mls[e + p * items].x);
+    const float ref = m == -INFINITY ? 0.0f : m;
+    floatx4 o = floatx4{};
+    for (int p = 0; p < shares; ++p) {
+      const float w = exp2_(mls[e + p * items].x - ref);
+      l += mls[e + p * items].y * w;
+      o += os[e + p * items] * w;
+    }
+    put_row(r, c, o, l);
+    if (c == 0) put_lse(r, m, l);
   }
 }
 
@@ -247,9 +356,9 @@ __device__ inline void write_rows(const AttendArgs<N>& a, const QuerySeq& s, con
 // ---------------------------------------------------------------------------
 template <int D>
 struct F32 {
-  static constexpr int R = 32, KT = 128;
+  static constexpr int R = 32, KT = 128, WAVES = 4;
   static constexpr int ROW = D + 4;                        // padded LDS row
-  static constexpr int LDS = 2 * KT * ROW * 4 + 4 * R * 8 + R * 4;
+  static constexpr int LDS = 2 * KT * ROW * 4 + 4 * R * 8 + (int)sizeof(Joint);
 };
 
 template <int D, int N>
@@ -262,7 +371,7 @@ __global__ __launch_bounds__(256) void attend_f32(AttendArgs<N> a) {
   float* kt = reinterpret_cast<float*>(lds);
   float* vt = kt + KT * ROW;
   float2* ml = reinterpret_cast<float2*>(vt + KT * ROW);   // [4][R]
-  int* flag = reinterpret_cast<int*>(ml + 4 * R);           // [R]
+  Joint* joint = reinterpret_cast<Joint*>(ml + 4 * R);
   const Unit x = unit_of<R, KT>(a, blockIdx.x);
   const QuerySeq& s = a.seq[x.s];
   const int lane = threadIdx.x & 63, wave = wave_id(), half = lane >> 5, col = lane & 31;
@@ -360,31 +469,15 @@ __global__ __launch_bounds__(256) void attend_f32(AttendArgs<N> a) {
   float total = 0.0f;
 #pragma unroll
   for (int w = 0; w < 4; ++w) total += ml[w * R + col].y * exp2_(ml[w * R + col].x - ref);
-  float* ob = kt;                                  // [R][ROW], the tiles are done with
-  for (int w = 0; w < 4; ++w) {
-    __syncthreads();
-    if (wave == w) {
+  float* ob = kt;                                  // [4][R][ROW], the tiles are done with
 #pragma unroll
-      for (int c = 0; c < NCT; ++c)
+  for (int c = 0; c < NCT; ++c)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          float* p = ob + col * ROW + c * 32 + acc_row(r, lane);
-          const float y = o[c][r] * mine;
-          *p = w == 0 ? y : *p + y;
-        }
-    }
-  }
-  __syncthreads();
-  if (wave == 0 && half == 0) {
-    ml[col] = make_float2(top, total);
-    flag[col] = 0;
-    if (x.slot >= 0) a.part_ml[(int64_t)x.slot * R + col] = make_float2(top, total);
-    else if (row.live && s.lse) s.lse[row.h * (int64_t)s.lse_hs + row.i] = log_of(top, total);
-  }
-  __syncthreads();
-  write_joined<float, D, R, ROW>(a, s, x, ob, ml, flag);
-  __syncthreads();
-  form_flagged<float, D, R, KT>(a, s, x, flag, ml);
+    for (int e = 0; e < 4; ++e)
+      *reinterpret_cast<floatx4*>(ob + (wave * R + col) * ROW + c * 32 + e * 8 + half * 4) =
+          floatx4{o[c][4 * e], o[c][4 * e + 1], o[c][4 * e + 2], o[c][4 * e + 3]} * mine;
+  if (wave == 0 && half == 0) joint->ml[col] = make_float2(top, total);
+  finish<float, D, R, KT, ROW, 4>(a, s, x, ob, joint);
 }
 
 // ---------------------------------------------------------------------------
@@ -394,7 +487,7 @@ __global__ __launch_bounds__(256) void attend_f32(AttendArgs<N> a) {
 // ---------------------------------------------------------------------------
 template <int D>
 struct F32Many {
-  static constexpr int R = 128, KT = 64;
+  static constexpr int R = 128, KT = 64, WAVES = 4;
   static constexpr int TILE = KT * D;                      // elements of a K or V stage
   static constexpr int LDS = 4 * TILE * 4;
   static constexpr int CPR = D / 4, COPIES = CPR / 4;      // 16-byte chunks per row, 1 KiB copies per wavefront
@@ -533,8 +626,7 @@ __global__ __launch_bounds__(256) void attend_f32_many(AttendArgs<N> a) {
 
 // ---------------------------------------------------------------------------
 // bf16, few rows (single tokens, short questions): 16 NR query rows to a unit.
-// Its key tiles of 128 rows go round the four wavefronts, each with sums of
-// its own.  A memory tile goes from HBM to registers and from there to the
+// Its key tiles of 128 rows go round the wavefronts, each with sums of its own.  A memory tile goes from HBM to registers and from there to the
 // MFMAs: lane (i, g) = (lane % 16, lane / 16) reads a quarter of K row i of
 // eight 16-row sets, and channel i's 32 rows of V block g, 16 bytes each; the
 // sets are chosen (rows 4 T .. 4 T + 3 of each of the four blocks) so that
@@ -543,10 +635,12 @@ __global__ __launch_bounds__(256) void attend_f32_many(AttendArgs<N> a) {
 template <int D, int NR>
 struct Few {
   static constexpr int R = 16 * NR, KT = 128;
+  static constexpr int WAVES = 4;
   static constexpr int OROW = D + 4;
   static constexpr int VBUF = 32 * D * 2;                  // bytes of a wavefront's tail V rows in LDS
-  static constexpr int JOIN = R * OROW * 4;
-  static constexpr int LDS = (4 * VBUF > JOIN ? 4 * VBUF : JOIN) + 4 * R * 8 + R * 4;
+  static constexpr int JOIN = WAVES * R * OROW * 4;
+  static constexpr int STAT = WAVES * VBUF > JOIN ? WAVES * VBUF : JOIN;
+  static constexpr int LDS = STAT + WAVES * R * 8 + (int)sizeof(Joint);
 };
 // 16-byte chunk of row r that holds its chunk c: the 8 rows that 32 lanes read
 // 32 bytes each of lie in different banks.
@@ -598,7 +692,7 @@ template <int D, int NR, int N>
 __global__ __launch_bounds__(256, D * NR == 256 ? 1 : 2) void attend_few(AttendArgs<N> a) {
   using P = Few<D, NR>;
   using B = MemBlock<D>;
-  constexpr int R = P::R, KT = P::KT, NS = D / 32, NC = D / 16;
+  constexpr int R = P::R, KT = P::KT, WAVES = P::WAVES, NS = D / 32, NC = D / 16;
   extern __shared__ __align__(16) char lds[];
   const Unit x = unit_of<R, KT>(a, blockIdx.x);
   const QuerySeq& s = a.seq[x.s];
@@ -647,7 +741,7 @@ __global__ __launch_bounds__(256, D * NR == 256 ? 1 : 2) void attend_few(AttendA
     const int end = min(x.k1, x.mem_tiles);
     load_k(kti);
     load_v(kti);
-    for (; kti < end; kti += 4) {
+    for (; kti < end; kti += WAVES) {
       floatx4 sc[NR][8];
 #pragma unroll
       for (int t = 0; t < 8; ++t) {
@@ -661,7 +755,7 @@ __global__ __launch_bounds__(256, D * NR == 256 ? 1 : 2) void attend_few(AttendA
           for (int n = 0; n < NR; ++n) sc[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[n][j], sc[n][t], 0, 0, 0);
         }
       }
-      if (kti + 4 < end) load_k(kti + 4);
+      if (kti + WAVES < end) load_k(kti + WAVES);
       const int keys = s.nm - kti * KT;
 #pragma unroll
       for (int n = 0; n < NR; ++n)
@@ -695,7 +789,7 @@ __global__ __launch_bounds__(256, D * NR == 256 ? 1 : 2) void attend_few(AttendA
           for (int n = 0; n < NR; ++n) o[n][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[n][j], o[n][c], 0, 0, 0);
         }
       }
-      if (kti + 4 < end) load_v(kti + 4);
+      if (kti + WAVES < end) load_v(kti + WAVES);
     }
   }
 
@@ -725,7 +819,7 @@ __global__ __launch_bounds__(256, D * NR == 256 ? 1 : 2) void attend_few(AttendA
       }
     };
     // (each wavefront's 32-row steps: four to a key tile)
-    const auto next = [&](int key) { return (key & 96) != 96 ? key + 32 : key + 32 + 3 * KT; };
+    const auto next = [&](int key) { return (key & 96) != 96 ? key + 32 : key + 32 + (WAVES - 1) * KT; };
     const int end = min((x.k1 - x.mem_tiles) * KT, s.nt);
     int key = (kti - x.mem_tiles) * KT;
     if (key < end) load(key);
@@ -782,10 +876,10 @@ __global__ __launch_bounds__(256, D * NR == 256 ? 1 : 2) void attend_few(AttendA
     }
   }
 
-  // join the four wavefronts
-  float2* ml = reinterpret_cast<float2*>(lds + P::LDS - 4 * R * 8 - R * 4);   // [4][R]
-  int* flag = reinterpret_cast<int*>(ml + 4 * R);                     // [R]
-  float* ob = reinterpret_cast<float*>(lds);                          // [R][OROW]
+  // join the wavefronts
+  float2* ml = reinterpret_cast<float2*>(lds + P::STAT);              // [WAVES][R]
+  Joint* joint = reinterpret_cast<Joint*>(ml + WAVES * R);
+  float* ob = reinterpret_cast<float*>(lds);                          // [WAVES][R][OROW]
 #pragma unroll
   for (int n = 0; n < NR; ++n) {
     st.l[n] += __shfl_xor(st.l[n], 16);
@@ -793,45 +887,20 @@ __global__ __launch_bounds__(256, D * NR == 256 ? 1 : 2) void attend_few(AttendA
     if (g == 0) ml[wave * R + n * 16 + i16] = make_float2(st.m[n], st.l[n]);
   }
   __syncthreads();
-  float top[NR], total[NR], mine[NR];
 #pragma unroll
   for (int n = 0; n < NR; ++n) {
-    top[n] = -INFINITY;
-    total[n] = 0.0f;
+    float top = -INFINITY, total = 0.0f;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) top[n] = fmaxf(top[n], ml[w * R + n * 16 + i16].x);
-    const float ref = top[n] == -INFINITY ? 0.0f : top[n];
-    mine[n] = exp2_(st.m[n] - ref);
+    for (int w = 0; w < WAVES; ++w) top = fmaxf(top, ml[w * R + n * 16 + i16].x);
+    const float ref = top == -INFINITY ? 0.0f : top, mine = exp2_(st.m[n] - ref);
 #pragma unroll
-    for (int w = 0; w < 4; ++w) total[n] += ml[w * R + n * 16 + i16].y * exp2_(ml[w * R + n * 16 + i16].x - ref);
+    for (int w = 0; w < WAVES; ++w) total += ml[w * R + n * 16 + i16].y * exp2_(ml[w * R + n * 16 + i16].x - ref);
+    if (wave == 0 && g == 0) joint->ml[n * 16 + i16] = make_float2(top, total);
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+      *reinterpret_cast<floatx4*>(ob + (wave * R + n * 16 + i16) * P::OROW + c * 16 + g * 4) = o[n][c] * mine;
   }
-  for (int w = 0; w < 4; ++w) {
-    __syncthreads();
-    if (wave == w) {
-#pragma unroll
-      for (int n = 0; n < NR; ++n)
-#pragma unroll
-        for (int c = 0; c < NC; ++c) {
-          floatx4* p = reinterpret_cast<floatx4*>(ob + (n * 16 + i16) * P::OROW + c * 16 + g * 4);
-          const floatx4 y = o[n][c] * mine[n];
-          *p = w == 0 ? y : *p + y;
-        }
-    }
-  }
-  __syncthreads();
-  if (wave == 0 && g == 0) {
-#pragma unroll
-    for (int n = 0; n < NR; ++n) {
-      ml[n * 16 + i16] = make_float2(top[n], total[n]);
-      flag[n * 16 + i16] = 0;
-      if (x.slot >= 0) a.part_ml[(int64_t)x.slot * R + n * 16 + i16] = make_float2(top[n], total[n]);
-      else if (row[n].live && s.lse) s.lse[row[n].h * (int64_t)s.lse_hs + row[n].i] = log_of(top[n], total[n]);
-    }
-  }
-  __syncthreads();
-  write_joined<uint16_t, D, R, P::OROW>(a, s, x, ob, ml, flag);
-  __syncthreads();
-  form_flagged<uint16_t, D, R, KT>(a, s, x, flag, ml);
+  finish<uint16_t, D, R, KT, P::OROW, WAVES>(a, s, x, ob, joint);
 }
 
 // ---------------------------------------------------------------------------
@@ -1126,8 +1195,8 @@ __global__ __launch_bounds__(512, 2) void attend_many(AttendArgs<N> a) {
 
 // ---------------------------------------------------------------------------
 // Puts the partial results of query rows' splits together.  SHARES threads to a
-// row and 4 channels: one for few splits (it has all its loads on their way at
-// once), 4 or a whole workgroup of 1024 threads that share out more.
+// row and 4 channels: one for up to 8 splits (it has all its loads on their way
+// at once), 4 for more, a workgroup of 1024 threads for many splits of few rows.
 // ---------------------------------------------------------------------------
 struct JoinTile {
   int s, g, rt, splits;
@@ -1241,30 +1310,27 @@ int64_t count_tiles(Args& a, int64_t* keys) {
 // Key tiles in shares of about `share`, or as many more as leave about
 // `target` units, or no more partials than the workspace holds.
 template <int R, int KT>
-int64_t plan_shares(Args& a, int64_t slots, int64_t share, int64_t target) {
+bool plan_shares(Args& a, int64_t slots, int64_t share, int64_t target) {
   int64_t keys;
   count_tiles<R, KT>(a, &keys);
   a.whole = 0;
   for (share = std::max(share, keys / target);; share += 1 + share / 16) {
-    int64_t units = 0, parts = 0, joins = 0;
+    int64_t units = 0, parts = 0;
     for (int i = 0; i < a.n_seqs; ++i) {
       QuerySeq& s = a.seq[i];
       const int64_t t = std::max(tiles_of<KT>(s.nm) + tiles_of<KT>(s.nt), 1);
       s.splits = (int)((t + share - 1) / share);
-      if (units > INT32_MAX) return -1;
+      if (units > INT32_MAX) return false;
       a.unit0[i] = (int)units;
       s.slot0 = (int)parts;
       const int64_t u = (int64_t)a.h_kv * s.row_tiles * s.splits;
       units += u;
-      if (s.splits > 1) {
-        parts += u;
-        joins += (int64_t)a.h_kv * s.row_tiles;
-      }
+      if (s.splits > 1) parts += u;
     }
-    if (units > INT32_MAX) return -1;
+    if (units > INT32_MAX) return false;
     if (parts <= slots) {
       a.units = (int)units;
-      return joins;
+      return true;
     }
   }
 }
@@ -1304,47 +1370,82 @@ int64_t plan_rounds(Args& a, int64_t slots, int width, double ends, double parti
   return splits == 1 ? 0 : rest;
 }
 
+// The arguments with room for one sequence.
+AttendArgs<1> first_of(const Args& a) {
+  AttendArgs<1> x;
+  x.seq[0] = a.seq[0];
+  x.unit0[0] = a.unit0[0];
+  x.n_seqs = 1; x.h_kv = a.h_kv; x.group = a.group; x.causal = a.causal; x.whole = a.whole; x.units = a.units;
+  x.part_o = a.part_o; x.part_ml = a.part_ml; x.arrived = a.arrived; x.joined = a.joined;
+  return x;
+}
+// The join of the split row tiles.
 template <typename T, int D, int R, int SHARES, int THREADS, int N>
 void join(const AttendArgs<N>& a, int64_t joins, hipStream_t st) {
   constexpr int ROWS = THREADS / (D / 4) / SHARES;
   join_splits<T, D, R, SHARES, THREADS, N><<<dim3((unsigned)joins, R / ROWS), THREADS, 0, st>>>(a);
 }
-
-template <typename T, int D, int R, int N, typename Kernel>
-hipError_t launch(const AttendArgs<N>& a, int64_t joins, Kernel kernel, int threads, int lds, hipStream_t st) {
-  hipError_t e = hipSuccess;
-  if (lds > 65536) e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-  if (e != hipSuccess) return e;
-  kernel<<<a.units, threads, lds, st>>>(a);
-  if ((e = hipGetLastError()) != hipSuccess || joins == 0) return e;
-  int splits = 0;
-  for (int i = 0; i < a.n_seqs; ++i) splits = std::max(splits, a.seq[i].splits);
-  if (splits <= 8) join<T, D, R, 1, 256, N>(a, joins, st);
-  else if (splits <= 32 || R >= 128) join<T, D, R, 4, 256, N>(a, joins, st);
-  else join<T, D, R, 1024 / (D / 4), 1024, N>(a, joins, st);
+template <typename T, typename P, int D, int N, typename Kernel>
+hipError_t launch(const AttendArgs<N>& a, int64_t joins, int splits, Kernel kernel, hipStream_t st) {
+  kernel<<<a.units, 64 * P::WAVES, P::LDS, st>>>(a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || joins == 0) return e;
+  if (splits <= 8) join<T, D, P::R, 1, 256>(a, joins, st);
+  else if (splits <= 32 || P::R >= 128) join<T, D, P::R, 4, 256>(a, joins, st);
+  else join<T, D, P::R, 1024 / (D / 4), 1024>(a, joins, st);
   return hipGetLastError();
 }
-
-// The kernel with room for one sequence, or for all that a launch describes.
-template <typename T, int D, int R, typename One, typename All>
-hipError_t launch(Args& a, void* ws, int64_t joins, One one, All all, int threads, int lds, hipStream_t st) {
-  if (joins < 0) return hipErrorInvalidConfiguration;
+template <typename T, typename P, int D, typename One, typename All>
+hipError_t launch(Args& a, void* ws, int64_t joins, int splits, One one, All all, hipStream_t st) {
   a.part_o = static_cast<float*>(ws);
-  a.part_ml = reinterpret_cast<float2*>(a.part_o + partials<R, D>() * R * D);
-  if (a.n_seqs > 1) return launch<T, D, R, kQueriesPerLaunch>(a, joins, all, threads, lds, st);
-  AttendArgs<1> x;
-  x.seq[0] = a.seq[0];
-  x.unit0[0] = a.unit0[0];
-  x.n_seqs = 1; x.h_kv = a.h_kv; x.group = a.group; x.causal = a.causal; x.whole = a.whole; x.units = a.units;
-  x.part_o = a.part_o; x.part_ml = a.part_ml;
-  return launch<T, D, R, 1>(x, joins, one, threads, lds, st);
+  a.part_ml = reinterpret_cast<float2*>(a.part_o + partials<P::R, D>() * P::R * D);
+  a.arrived = reinterpret_cast<int*>(static_cast<char*>(ws) + kPartBytes);
+  if (a.n_seqs > 1) return launch<T, P, D>(a, joins, splits, all, st);
+  return launch<T, P, D>(first_of(a), joins, splits, one, st);
 }
 
+// Few rows, in shares of at least a key tile for each wavefront.  Units join
+// themselves where that takes one of them `kJoinBatches` rounds of loads at
+// most (its threads have 8 partials of 4 channels on their way each); past
+// that a kernel for it is as fast or faster.  us, with the kernel and without:
+// a row of 7 heads over 1024 keys of width 128 (1 round) 10.8 and 8.7, of 4
+// heads over 32768 keys of width 64 (3) 12.8 and 10.7; 42 rows over 1024 keys
+// of width 128 (4) 13.7 and 15.6.
+constexpr int kJoinBatches = 3;
+template <typename T, typename P, int D, typename One, typename All>
+hipError_t launch_shares(Args& a, void* ws, int64_t target, One one, All all, hipStream_t st) {
+  constexpr int64_t slots = partials<P::R, D>();
+  static_assert(slots <= kMaxPartials, "a counter to a partial");
+  if (!plan_shares<P::R, P::KT>(a, slots, P::WAVES, target)) return hipErrorInvalidConfiguration;
+  int splits = 1;
+  int64_t joins = 0, batches = 0;
+  for (int i = 0; i < a.n_seqs; ++i) {
+    const QuerySeq& s = a.seq[i];
+    if (s.splits == 1) continue;
+    const int64_t items = std::min<int64_t>(P::R, (int64_t)a.group * s.nq) * (D / 4), threads = 64 * P::WAVES;
+    const int64_t passes = (items + threads - 1) / threads, shares = std::max<int64_t>(1, threads / items);
+    joins += (int64_t)a.h_kv * s.row_tiles;
+    splits = std::max(splits, s.splits);
+    batches = std::max(batches, passes * ((s.splits + 8 * shares - 1) / (8 * shares)));
+  }
+  a.joined = batches <= kJoinBatches;
+  return launch<T, P, D>(a, ws, a.joined ? 0 : joins, splits, one, all, st);
+}
+
+// Many rows: units, and a join of the split row tiles.
+template <typename T, typename P, int D, typename One, typename All>
+hipError_t launch_rounds(Args& a, void* ws, int cus, double ends, double partial, One one, All all, hipStream_t st) {
+  const int64_t joins = plan_rounds<P::R, P::KT>(a, partials<P::R, D>(), cus, ends, partial);
+  if (joins < 0) return hipErrorInvalidConfiguration;
+  a.joined = 0;
+  return launch<T, P, D>(a, ws, joins, a.seq[0].splits, one, all, st);
+}
+
+constexpr int kAll = kQueriesPerLaunch;
 template <int D, int NR>
 hipError_t attend_few_rows(Args& a, int cus, void* ws, hipStream_t st) {
   using P = Few<D, NR>;
-  const int64_t joins = plan_shares<P::R, P::KT>(a, partials<P::R, D>(), 4, 3 * cus);
-  return launch<uint16_t, D, P::R>(a, ws, joins, attend_few<D, NR, 1>, attend_few<D, NR, kQueriesPerLaunch>, 256, P::LDS, st);
+  return launch_shares<uint16_t, P, D>(a, ws, 3 * cus, attend_few<D, NR, 1>, attend_few<D, NR, kAll>, st);
 }
 
 template <int D>
@@ -1352,26 +1453,40 @@ hipError_t attend(const AttnDims& dm, Args& a, int cus, void* ws, hipStream_t st
   int64_t rows = 0, keys = 0;
   for (int i = 0; i < a.n_seqs; ++i) rows = std::max(rows, (int64_t)a.group * a.seq[i].nq);
   if (dm.dtype == OMNIMEM_F32) {
-    if (rows > (getenv("OMN_F") ? atoi(getenv("OMN_F")) : 64)) {
-      using P = F32Many<D>;
-      const int64_t joins = plan_rounds<P::R, P::KT>(a, partials<P::R, D>(), cus, 1.0, 0.003);
-      return launch<float, D, P::R>(a, ws, joins, attend_f32_many<D, 1>, attend_f32_many<D, kQueriesPerLaunch>, 256, P::LDS, st);
-    }
-    using P = F32<D>;
-    const int64_t joins = plan_shares<P::R, P::KT>(a, partials<P::R, D>(), 1, 4 * cus);
-    return launch<float, D, P::R>(a, ws, joins, attend_f32<D, 1>, attend_f32<D, kQueriesPerLaunch>, 256, P::LDS, st);
+    // (us of the few-row and the many-row kernel: 48 rows of 4 heads of width 64 over 4096 keys, 8 sequences, 59 and
+    // 61; 84 rows, 4 heads of width 128, one sequence 47 and 32)
+    if (rows <= 64) return launch_shares<float, F32<D>, D>(a, ws, 4 * cus, attend_f32<D, 1>, attend_f32<D, kAll>, st);
+    return launch_rounds<float, F32Many<D>, D>(a, ws, cus, 1.0, 0.003, attend_f32_many<D, 1>, attend_f32_many<D, kAll>, st);
   }
   if (rows <= 16) return attend_few_rows<D, 1>(a, cus, ws, st);
   // Up to 8192 / d rows of every head, and further where that leaves a wavefront at most 896 / d tiles of 32 rows
   // and 128 keys for each compute unit, the few-row kernel.
   count_tiles<32, 128>(a, &keys);
   if (rows <= 8192 / D || keys <= 896 / D * cus) return attend_few_rows<D, 2>(a, cus, ws, st);
-  using P = Many<D>;
-  const int64_t joins = plan_rounds<P::R, P::KT>(a, partials<P::R, D>(), cus, 3.0, 0.03);
-  return launch<uint16_t, D, P::R>(a, ws, joins, attend_many<D, 1>, attend_many<D, kQueriesPerLaunch>, 512, P::LDS, st);
+  return launch_rounds<uint16_t, Many<D>, D>(a, ws, cus, 3.0, 0.03, attend_many<D, 1>, attend_many<D, kAll>, st);
+}
+
+template <typename Kernel>
+hipError_t allow(Kernel kernel, int lds) {
+  return lds <= 65536 ? hipSuccess : hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+}
+template <int D>
+hipError_t prepare() {
+  hipError_t e = allow(attend_f32<D, 1>, F32<D>::LDS);
+  if (e == hipSuccess) e = allow(attend_f32<D, kAll>, F32<D>::LDS);
+  if (e == hipSuccess) e = allow(attend_f32_many<D, 1>, F32Many<D>::LDS);
+  if (e == hipSuccess) e = allow(attend_f32_many<D, kAll>, F32Many<D>::LDS);
+  if (e == hipSuccess) e = allow(attend_few<D, 1, 1>, Few<D, 1>::LDS);
+  if (e == hipSuccess) e = allow(attend_few<D, 1, kAll>, Few<D, 1>::LDS);
+  if (e == hipSuccess) e = allow(attend_few<D, 2, 1>, Few<D, 2>::LDS);
+  if (e == hipSuccess) e = allow(attend_few<D, 2, kAll>, Few<D, 2>::LDS);
+  static_assert(Many<D>::LDS <= 65536, "");
+  return e;
 }
 
 }  // namespace
+
+hipError_t prepare_attend(const AttnDims& dm) { return dm.d == 128 ? prepare<128>() : prepare<64>(); }
 
 hipError_t launch_attend(const AttnDims& dm, AttendArgs<kQueriesPerLaunch>& a, int n, int compute_units, void* ws, hipStream_t st) {
   a.n_seqs = n;

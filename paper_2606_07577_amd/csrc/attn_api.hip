@@ -169,12 +169,15 @@ omnimem_status omnimem_attn_create(const omnimem_attn_config* cfg, omnimem_attn*
     int cus = 0;
     if (hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, attn->device) == hipSuccess && cus > 0)
       attn->compute_units = cus;
-    e = hipMalloc(&attn->workspace, (size_t)kPartBytes);
+    e = hipMalloc(&attn->workspace, (size_t)kPartBytes + kMaxPartials * sizeof(int));
+    if (e == hipSuccess) e = hipMemset(static_cast<char*>(attn->workspace) + kPartBytes, 0, kMaxPartials * sizeof(int));
+    if (e == hipSuccess) e = prepare_attend(attn->dm);
   }
   if (e != hipSuccess) {
     (void)hipGetLastError();
+    (void)hipFree(attn->workspace);
     delete attn;
-    return fail(nullptr, OMNIMEM_ERR_HIP, "workspace allocation: %s", hipGetErrorString(e));
+    return fail(nullptr, OMNIMEM_ERR_HIP, "workspace: %s", hipGetErrorString(e));
   }
   *out = attn;
   return OMNIMEM_OK;

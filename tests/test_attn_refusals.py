@@ -21,12 +21,14 @@ hipError_t hipGetDevice(int* d) { *d = 0; return hipSuccess; }
 hipError_t hipSetDevice(int) { return hipSuccess; }
 hipError_t hipDeviceGetAttribute(int* v, hipDeviceAttribute_t, int) { *v = 256; return hipSuccess; }
 hipError_t hipMalloc(void** p, size_t) { *p = (void*)4096; return hipSuccess; }
+hipError_t hipMemset(void*, int, size_t) { return hipSuccess; }
 hipError_t hipFree(void*) { return hipSuccess; }
 hipError_t hipDeviceSynchronize() { return hipSuccess; }
 hipError_t hipGetLastError() { return hipSuccess; }
 const char* hipGetErrorString(hipError_t) { return ""; }
 }
 namespace omnimem {
+hipError_t prepare_attend(const AttnDims&) { return hipSuccess; }
 hipError_t launch_rotate(const AttnDims&, const RotateArgs<kRotatesPerLaunch>&, int n, hipStream_t) { ++launches; sequences += n; return hipSuccess; }
 hipError_t launch_hold(const AttnDims&, const HeldArgs&, int n, bool, hipStream_t) { ++launches; sequences += n; return hipSuccess; }
 hipError_t launch_attend(const AttnDims&, AttendArgs<kQueriesPerLaunch>&, int n, int, void*, hipStream_t) { ++launches; sequences += n; return hipSuccess; }
