@@ -636,6 +636,7 @@ template <int D, int NR>
 struct Few {
   static constexpr int R = 16 * NR, KT = 128;
   static constexpr int WAVES = 4;
+  static constexpr int STEPS = D * NR == 256 ? 2 : 1;      // a memory tile's, by the registers of two wavefronts a SIMD
   static constexpr int OROW = D + 4;
   static constexpr int VBUF = 32 * D * 2;                  // bytes of a wavefront's tail V rows in LDS
   static constexpr int JOIN = WAVES * R * OROW * 4;
@@ -689,10 +690,10 @@ __device__ inline uint4 load_part(const char* p) {   // 16 or 8 bytes
 }
 
 template <int D, int NR, int N>
-__global__ __launch_bounds__(256, D * NR == 256 ? 1 : 2) void attend_few(AttendArgs<N> a) {
+__global__ __launch_bounds__(256, 2) void attend_few(AttendArgs<N> a) {
   using P = Few<D, NR>;
   using B = MemBlock<D>;
-  constexpr int R = P::R, KT = P::KT, WAVES = P::WAVES, NS = D / 32, NC = D / 16;
+  constexpr int R = P::R, KT = P::KT, WAVES = P::WAVES, NS = D / 32, NC = D / 16, STEPS = P::STEPS, T = 8 / STEPS;
   extern __shared__ __align__(16) char lds[];
   const Unit x = unit_of<R, KT>(a, blockIdx.x);
   const QuerySeq& s = a.seq[x.s];
@@ -723,73 +724,78 @@ __global__ __launch_bounds__(256, D * NR == 256 ? 1 : 2) void attend_few(AttendA
         qf[n][j] = row[n].live ? gload<frag>(q[n] + g * (D / 4) + j * 8) : frag{};
     const char* data = s.mem + x.g * ((int64_t)s.mem_hs * 16);
     const int last_block = tiles_of<kMemRows>(s.nm) - 1;
-    uint4 kc[8], vc[NC];
+    uint4 kc[T], vc[NC];
     uint2 ks, vs;
-    const auto load_k = [&](int t) {
+    // step h of a tile: its 16-row sets T h .., and the rows of V that they are
+    const auto load_k = [&](int t, int h) __attribute__((always_inline)) {
       const char* blk = data + (int64_t)min(t * 4 + (i16 >> 2), last_block) * B::BYTES;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) kc[j] = load_part<D / 8>(blk + (j * 4 + (i16 & 3)) * (D / 2) + g * (D / 8));
+      for (int j = 0; j < T; ++j) kc[j] = load_part<D / 8>(blk + ((h * T + j) * 4 + (i16 & 3)) * (D / 2) + g * (D / 8));
       ks = gload8(blk + B::k_scale(i16 & 3, g * (D / 4) / 32));
     };
-    const auto load_v = [&](int t) {
+    const auto load_v = [&](int t, int h) __attribute__((always_inline)) {
       const char* blk = data + (int64_t)min(t * 4 + g, last_block) * B::BYTES;
 #pragma unroll
-      for (int c = 0; c < NC; ++c) vc[c] = gload16(blk + B::V + (c * 16 + i16) * 16);
+      for (int c = 0; c < NC; ++c) vc[c] = load_part<2 * T>(blk + B::V + (c * 16 + i16) * 16 + h * 2 * T);
       if constexpr (NC == 8) vs = gload8(blk + B::v_scale(i16));
       else vs = make_uint2(gload<uint32_t>(blk + B::v_scale(i16)), 0);
     };
     const int end = min(x.k1, x.mem_tiles);
-    load_k(kti);
-    load_v(kti);
+    load_k(kti, 0);
+    load_v(kti, 0);
     for (; kti < end; kti += WAVES) {
-      floatx4 sc[NR][8];
 #pragma unroll
-      for (int t = 0; t < 8; ++t) {
+      for (int h = 0; h < STEPS; ++h) {
+        const int next_t = h + 1 < STEPS ? kti : kti + WAVES, next_h = (h + 1) % STEPS;
+        floatx4 sc[NR][T];
 #pragma unroll
-        for (int n = 0; n < NR; ++n) sc[n][t] = floatx4{};
-        const float ksc = byte_scale(ks, t);
+        for (int t = 0; t < T; ++t) {
 #pragma unroll
-        for (int j = 0; j < NS; ++j) {
-          const frag kf = __builtin_bit_cast(frag, values8_bf16(word(kc[t], j), ksc));
+          for (int n = 0; n < NR; ++n) sc[n][t] = floatx4{};
+          const float ksc = byte_scale(ks, h * T + t);
 #pragma unroll
-          for (int n = 0; n < NR; ++n) sc[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[n][j], sc[n][t], 0, 0, 0);
+          for (int j = 0; j < NS; ++j) {
+            const frag kf = __builtin_bit_cast(frag, values8_bf16(word(kc[t], j), ksc));
+#pragma unroll
+            for (int n = 0; n < NR; ++n) sc[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[n][j], sc[n][t], 0, 0, 0);
+          }
         }
-      }
-      if (kti + WAVES < end) load_k(kti + WAVES);
-      const int keys = s.nm - kti * KT;
-#pragma unroll
-      for (int n = 0; n < NR; ++n)
-#pragma unroll
-        for (int t = 0; t < 8; ++t) sc[n][t] *= scale;
-      if (keys < KT) {
+        if (next_t < end) load_k(next_t, next_h);
+        const int keys = s.nm - kti * KT;
 #pragma unroll
         for (int n = 0; n < NR; ++n)
 #pragma unroll
-          for (int t = 0; t < 8; ++t)
+          for (int t = 0; t < T; ++t) sc[n][t] *= scale;
+        if (keys < KT) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
-              if (g * 32 + t * 4 + r >= keys) sc[n][t][r] = -INFINITY;
-      }
-      float alpha[NR];
-      weigh<NR, 8>(sc, st, alpha);
-      frag pf[NR][4];
+          for (int n = 0; n < NR; ++n)
 #pragma unroll
-      for (int n = 0; n < NR; ++n)
+            for (int t = 0; t < T; ++t)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) pf[n][j] = pack_weights(sc[n][2 * j], sc[n][2 * j + 1]);
-#pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        const float vsc = byte_scale(vs, c);
-#pragma unroll
-        for (int n = 0; n < NR; ++n) o[n][c] *= alpha[n];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const frag vf = __builtin_bit_cast(frag, values8_bf16(word(vc[c], j), vsc));
-#pragma unroll
-          for (int n = 0; n < NR; ++n) o[n][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[n][j], o[n][c], 0, 0, 0);
+              for (int r = 0; r < 4; ++r)
+                if (g * 32 + (h * T + t) * 4 + r >= keys) sc[n][t][r] = -INFINITY;
         }
+        float alpha[NR];
+        weigh<NR, T>(sc, st, alpha);
+        frag pf[NR][T / 2];
+#pragma unroll
+        for (int n = 0; n < NR; ++n)
+#pragma unroll
+          for (int j = 0; j < T / 2; ++j) pf[n][j] = pack_weights(sc[n][2 * j], sc[n][2 * j + 1]);
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+          const float vsc = byte_scale(vs, c);
+#pragma unroll
+          for (int n = 0; n < NR; ++n) o[n][c] *= alpha[n];
+#pragma unroll
+          for (int j = 0; j < T / 2; ++j) {
+            const frag vf = __builtin_bit_cast(frag, values8_bf16(word(vc[c], j), vsc));
+#pragma unroll
+            for (int n = 0; n < NR; ++n) o[n][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[n][j], o[n][c], 0, 0, 0);
+          }
+        }
+        if (next_t < end) load_v(next_t, next_h);
       }
-      if (kti + WAVES < end) load_v(kti + WAVES);
     }
   }
 
