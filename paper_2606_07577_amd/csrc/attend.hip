@@ -1465,10 +1465,12 @@ hipError_t attend(const AttnDims& dm, Args& a, int cus, void* ws, hipStream_t st
     return launch_rounds<float, F32Many<D>, D>(a, ws, cus, 1.0, 0.003, attend_f32_many<D, 1>, attend_f32_many<D, kAll>, st);
   }
   if (rows <= 16) return attend_few_rows<D, 1>(a, cus, ws, st);
-  // Up to 8192 / d rows of every head, and further where that leaves a wavefront at most 896 / d tiles of 32 rows
-  // and 128 keys for each compute unit, the few-row kernel.
+  // The few-row kernel up to 96 rows of a head, and further where that leaves at most 12 wavefront tiles (32 rows and
+  // 128 keys) for each compute unit.  us, it and the many-row kernel, 4 heads of width 128: 84 rows, 8 sequences of
+  // 32768 memory rows 94 and 125; 112 rows, 8 sequences of 8192 tail rows 93 and 53; 224 rows over 8192 memory rows
+  // (7 tiles a unit) 19 and 26; 448 rows, 8 sequences of 1024 (16) 35 and 32; 700 rows over 8192 (22) 36 and 34.
   count_tiles<32, 128>(a, &keys);
-  if (rows <= 8192 / D || keys <= 896 / D * cus) return attend_few_rows<D, 2>(a, cus, ws, st);
+  if (rows <= 96 || keys <= 12 * cus) return attend_few_rows<D, 2>(a, cus, ws, st);
   return launch_rounds<uint16_t, Many<D>, D>(a, ws, cus, 3.0, 0.03, attend_many<D, 1>, attend_many<D, kAll>, st);
 }
 
