@@ -181,3 +181,103 @@ def test_products_that_are_all_minus_infinity_count_as_none(dtype, nq):
     torch.cuda.synchronize()
     assert (c.out[:, :nq] == 0).all() and torch.isneginf(c.lse[:, :nq]).all()
     attn.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("nq", [1, 20, 130])
+def test_a_negative_scale(dtype, nq):
+    attn = handle(4, 2, 64, dtype)
+    c = Case(attn, torch.Generator(device="cuda").manual_seed(3), 4, 2, 64, dtype, nq, 150, 170, scale=-0.3)
+    attn.omnimem_attend([c.query()])
+    torch.cuda.synchronize()
+    c.check(True)
+    attn.close()
+
+
+def by_torch(q, k, v, scale, causal):
+    """out and lse of q [h_q, n, d] over k, v [h_kv, t, d] in 64 bits on the device, and the sizes of Case.check."""
+    group, n, t = q.shape[0] // k.shape[0], q.shape[1], k.shape[1]
+    q, k, v = q.double(), k.double().repeat_interleave(group, 0), v.double().repeat_interleave(group, 0)
+    s = torch.bmm(q, k.transpose(1, 2).contiguous()) * scale
+    if causal:
+        s.masked_fill_(~torch.ones(n, t, dtype=torch.bool, device="cuda").tril(t - n), float("-inf"))
+    p = torch.softmax(s, -1)
+    reach = torch.bmm(q.abs(), k.abs().transpose(1, 2).contiguous()).amax(-1) * abs(scale)
+    return torch.bmm(p, v), torch.logsumexp(s, -1), torch.bmm(p, v.abs()), reach
+
+
+def check_by_torch(out, lse, ref, d, n):
+    o, l, size, reach = ref
+    half = torch.finfo(out.dtype).eps / 2 if out.dtype == torch.bfloat16 else 0.0
+    tol = size * (2 * (d + 6) * U * reach[..., None] + 2 * (n + 8) * U + half) + (half or U) * o.abs()
+    assert bool(((out.double() - o).abs() <= tol).all())
+    assert bool(((lse.double() - l).abs() <= (d + 6) * U * reach + (n + 8) * U + 2 * U * l.abs()).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("h,nq,nt,d", [(70, 1000, 1000, 64), (67, 513, 700, 128), (9, 1300, 5000, 64)])
+def test_more_row_tiles_than_compute_units(dtype, h, nq, nt, d):
+    """Whole row tiles for each compute unit, and the rest in shares."""
+    g = torch.Generator(device="cuda").manual_seed(h)
+    attn = handle(h, h, d, dtype)
+    q, k, v = (torch.randn(h, n, d, generator=g, device="cuda").to(TORCH[dtype]) for n in (nq, nt, nt))
+    out, lse = torch.zeros_like(q), torch.zeros(h, nq, device="cuda")
+    attn.omnimem_attend([om.make_query(q, out, k, v, lse=lse)])
+    torch.cuda.synchronize()
+    check_by_torch(out, lse, by_torch(q, k, v, d ** -0.5, True), d, nt)
+    attn.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("nq", [1, 9, 40, 150])
+def test_rows_interleaved_over_heads_and_far_apart(dtype, nq):
+    """Keys and values [row][head][d] and query-major queries; then rows and heads whose offsets pass 32 bits."""
+    h_q, h_kv, d, nt = 6, 2, 64, 700
+    g = torch.Generator(device="cuda").manual_seed(nq)
+    td = TORCH[dtype]
+    attn = handle(h_q, h_kv, d, dtype)
+    q = torch.randn(nq, h_q, d, generator=g, device="cuda").to(td).transpose(0, 1)
+    k, v = (torch.randn(nt, h_kv, d, generator=g, device="cuda").to(td).transpose(0, 1) for _ in range(2))
+    ref = by_torch(q, k, v, d ** -0.5, True)
+    out, lse = torch.zeros(nq, h_q, d, device="cuda", dtype=td).transpose(0, 1), torch.zeros(h_q, nq, device="cuda")
+    attn.omnimem_attend([om.make_query(q, out, k, v, lse=lse)])
+    torch.cuda.synchronize()
+    check_by_torch(out, lse, ref, d, nt)
+    elt = torch.finfo(td).bits // 8
+    rows, heads = (7 << 20) // elt, (5 << 30) // elt            # 700 rows of 7 MiB; heads 5 GiB apart
+    buffers = [torch.empty((heads + nt * rows) * elt, dtype=torch.uint8, device="cuda").view(td) for _ in range(2)]
+    far_k, far_v = (b.as_strided((h_kv, nt, d), (heads, rows, 1)) for b in buffers)
+    far_k.copy_(k)
+    far_v.copy_(v)
+    again = torch.zeros_like(out)
+    attn.omnimem_attend([om.make_query(q, again, far_k, far_v)])
+    torch.cuda.synchronize()
+    assert torch.equal(again, out)
+    attn.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("h_q,h_kv,d,nq,nm,nt", [(7, 1, 128, 1, 30000, 9), (4, 1, 64, 1, 40000, 0), (20, 1, 64, 3, 6000, 100),
+                                                 (2, 2, 64, 1, 0, 2500), (16, 1, 128, 1, 2000, 0), (30, 1, 128, 1, 1500, 0)])
+def test_every_way_of_joining(dtype, h_q, h_kv, d, nq, nm, nt):
+    """Splits of few rows that their last unit joins, with one thread to a value or several, and that a kernel joins;
+    against all keys in one share (more rows of the same keys are not split)."""
+    g = torch.Generator(device="cuda").manual_seed(nm)
+    attn = handle(h_q, h_kv, d, dtype)
+    c = Case(attn, g, h_q, h_kv, d, dtype, nq, nm, nt)
+    for _ in range(3):
+        c.out.fill_(7.0)
+        attn.omnimem_attend([c.query()])
+        torch.cuda.synchronize()
+        k, v = (torch.cat([torch.tensor(m, device="cuda"), t[:, :nt].double()], 1) for m, t in zip(c.held, (c.k, c.v)))
+        o, l, size, reach = by_torch(c.q, k, v, c.scale, False)
+        if nt and nq > 1:      # (the causal rule among the tail rows)
+            seen = torch.ones(nq, nm + nt, dtype=torch.bool, device="cuda")
+            seen[:, nm:] = seen[:, nm:].tril(nt - nq)
+            s = torch.bmm(c.q.double(), k.repeat_interleave(h_q // h_kv, 0).transpose(1, 2).contiguous()) * c.scale
+            s.masked_fill_(~seen, float("-inf"))
+            p, l = torch.softmax(s, -1), torch.logsumexp(s, -1)
+            o, size = (torch.bmm(p, x.repeat_interleave(h_q // h_kv, 0)) for x in (v, v.abs()))
+        check_by_torch(c.out[:, :nq], c.lse[:, :nq], (o, l, size, reach), d, nm + nt)
+        assert (c.out[:, nq:] == 7).all()
+    attn.close()

@@ -89,3 +89,28 @@ def test_many_sequences_strides_and_a_block_at_a_time():
         for t, x in zip((back_k, back_v), orc.unpack(want, lengths[i])):
             assert np.array_equal(part(t, i).double().cpu().numpy(), x) and (t[i, lengths[i]:] == 0).all()
     attn.close()
+
+
+def test_offsets_past_32_bits():
+    """Rows and heads whose offsets pass 32 bits, in the rows and in the memory."""
+    h, d, n = 2, 64, 700
+    g = torch.Generator(device="cuda").manual_seed(7)
+    attn = om.Attention(h, h, d)
+    k, v = (torch.randn(h, n, d, generator=g, device="cuda").bfloat16() for _ in range(2))
+    near, near_k, near_v = torch.zeros(om.memory_shape(h, d, n), dtype=torch.uint8, device="cuda"), torch.zeros_like(k), torch.zeros_like(v)
+    attn.omnimem_pack([om.make_held(k, v, near)])
+    attn.omnimem_unpack([om.make_held(near_k, near_v, near)])
+    rows, heads = 7 << 19, 5 << 29                 # 7 MiB, 5 GiB
+    far = [torch.empty(heads + n * rows, dtype=torch.bfloat16, device="cuda").as_strided((h, n, d), (heads, rows, 1)) for _ in range(2)]
+    data = torch.empty((5 << 30) + near.numel(), dtype=torch.uint8, device="cuda").as_strided(near.shape, (5 << 30, near.shape[2], 1))
+    far[0].copy_(k)
+    far[1].copy_(v)
+    attn.omnimem_pack([om.make_held(*far, data)])
+    torch.cuda.synchronize()
+    assert torch.equal(data, near)
+    for t in far:
+        t.zero_()
+    attn.omnimem_unpack([om.make_held(*far, data)])
+    torch.cuda.synchronize()
+    assert torch.equal(far[0], near_k) and torch.equal(far[1], near_v)
+    attn.close()
