@@ -115,6 +115,15 @@ __device__ inline floatx2 shared8(const float* p) {
   const uint64_t v = __hip_atomic_load(reinterpret_cast<const uint64_t*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   return floatx2{__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32))};
 }
+// The larger of a lane's value and that of the lane 32 (16) away.
+__device__ inline float max32(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ inline float max16(float x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
 __device__ inline float log_of(float m, float l) { return l == 0.0f ? -INFINITY : (m + log2f(l)) * kLn2; }
 
 // ---------------------------------------------------------------------------
@@ -436,7 +445,7 @@ __global__ __launch_bounds__(256) void attend_f32(AttendArgs<N> a) {
       sc[r] = wave * 32 + acc_row(r, lane) < limit ? sc[r] * s.scale_log2 : -INFINITY;
       top = fmaxf(top, sc[r]);
     }
-    top = fmaxf(top, __shfl_xor(top, 32));
+    top = max32(top);
     const float m2 = fmaxf(m, top), ref = m2 == -INFINITY ? 0.0f : m2;
     const float alpha = exp2_(m - ref);
     m = m2;
@@ -593,7 +602,7 @@ __global__ __launch_bounds__(256) void attend_f32_many(AttendArgs<N> a) {
         sc[r] = b * 32 + (r >> 2) * 8 + (r & 3) < limit ? sc[r] * s.scale_log2 : -INFINITY;
         top = fmaxf(top, sc[r]);
       }
-      top = fmaxf(top, __shfl_xor(top, 32));
+      top = max32(top);
       if (__any(top > m + 8.0f)) {                         // (see attend_many)
         const float m2 = fmaxf(m, top);
         const float alpha = m2 == -INFINITY ? 1.0f : exp2_(m - m2);
@@ -661,8 +670,7 @@ __device__ inline void weigh(floatx4 (&sc)[NR][N], Stats<NR>& st, float (&alpha)
     float top = -INFINITY;
 #pragma unroll
     for (int t = 0; t < N; ++t) top = fmaxf(fmaxf(fmaxf(top, sc[n][t][0]), fmaxf(sc[n][t][1], sc[n][t][2])), sc[n][t][3]);
-    top = fmaxf(top, __shfl_xor(top, 16));
-    top = fmaxf(top, __shfl_xor(top, 32));
+    top = max32(max16(top));
     const float m2 = fmaxf(st.m[n], top), ref = m2 == -INFINITY ? 0.0f : m2;
     alpha[n] = exp2_(st.m[n] - ref);
     st.m[n] = m2;
@@ -911,7 +919,9 @@ __global__ __launch_bounds__(256, 2) void attend_few(AttendArgs<N> a) {
 
 // ---------------------------------------------------------------------------
 // bf16, many rows (chunks): 256 query rows to a unit, 32 to each of eight
-// wavefronts, against key tiles of 64 rows that they share in LDS.  A step
+// wavefronts, against key tiles of 64 rows that they share in LDS, in four
+// stages (with two, and a barrier every tile, 4096 queries of 28 heads over
+// 20480 rows take 1067 us instead of 1051).  A step
 // multiplies K of the next tile while it turns this tile's scores to weights,
 // and then V of this tile: its MFMAs do not wait for its vector instructions.
 // Tail rows are copied to LDS as they are, and V is transposed as it is read;
@@ -922,7 +932,7 @@ template <int D>
 struct Many {
   static constexpr int R = 256, KT = 64, WAVES = 8;
   static constexpr int TILE = KT * D;                      // elements of a K or V stage
-  static constexpr int LDS = 4 * TILE * 2;
+  static constexpr int LDS = 8 * TILE * 2;                 // four stages of K and of V
   static constexpr int CPR = D / 8;                        // 16-byte chunks per row
   static constexpr int COPIES = CPR / WAVES;               // 1 KiB copies of a tile per wavefront
   static constexpr int NKS = D / 16, NCT = D / 32;
@@ -1034,8 +1044,8 @@ __global__ __launch_bounds__(512, 2) void attend_many(AttendArgs<N> a) {
   constexpr int R = P::R, KT = P::KT, TILE = P::TILE, CPR = P::CPR, NKS = P::NKS, NCT = P::NCT;
   constexpr int W = D / 64;                                // code words per thread and operand of a memory tile
   extern __shared__ __align__(16) char lds[];
-  uint16_t* kbuf = reinterpret_cast<uint16_t*>(lds);       // [2][TILE]
-  uint16_t* vbuf = kbuf + 2 * TILE;
+  uint16_t* kbuf = reinterpret_cast<uint16_t*>(lds);       // [4][TILE]
+  uint16_t* vbuf = kbuf + 4 * TILE;
   // round by round of the chip's 256 compute units, neighbouring units on one XCD
   int u = blockIdx.x;
   if ((u | 255) < a.units) u = (u & ~255) + (u & 7) * 32 + ((u & 255) >> 3);
@@ -1124,7 +1134,7 @@ __global__ __launch_bounds__(512, 2) void attend_many(AttendArgs<N> a) {
     return t < mem_tiles ? nm - t * KT : row.seen - (t - mem_tiles) * KT;
   };
   const auto raise = [&](float top) __attribute__((always_inline)) {                      // largest raw score of the tile to come
-    top = fmaxf(top, __shfl_xor(top, 32)) * scale;
+    top = max32(top) * scale;
     // The sums keep their reference until a score passes it by 8: weights stay below 2^8, and few tiles scale O.
     if (__any(top > m + 8.0f)) {
       const float m2 = fmaxf(m, top);
@@ -1137,14 +1147,18 @@ __global__ __launch_bounds__(512, 2) void attend_many(AttendArgs<N> a) {
   };
 
   if (x.k0 < x.k1) {
+    // Stage of tile t: (t - k0) & 3.  Step t takes K of tile t + 1 and V of tile t, and fetches K of tile t + 3 and V
+    // of tile t + 2; a barrier every second step lies between a fetch and the first step that takes it, and between
+    // the last step that takes a stage and the next fetch into it.
     const int k0 = x.k0, k1 = x.k1;
-    fetch_k(k0, 0);
-    fetch_v(k0, 0);
-    store_k(k0, 0);
-    store_v(k0, 0);
-    if (k0 + 1 < k1) {
-      fetch_k(k0 + 1, 1);
-      store_k(k0 + 1, 1);
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      if (k0 + i < k1) {
+        fetch_k(k0 + i, i);
+        if (i < 2) fetch_v(k0 + i, i);
+        store_k(k0 + i, i);
+        if (i < 2) store_v(k0 + i, i);
+      }
     }
     dma_wait();
     __syncthreads();
@@ -1164,20 +1178,21 @@ __global__ __launch_bounds__(512, 2) void attend_many(AttendArgs<N> a) {
           top = fmaxf(top, s0[b][r]);
         }
       raise(top);
-      __syncthreads();
     }
     const auto step = [&](auto mem, int t, floatx16 (&sc)[2], floatx16 (&next)[2]) __attribute__((always_inline)) {
-      const int st = (t - k0) & 1;                         // (every wavefront is done with K of tile t and V of tile t - 1)
-      if (t + 2 < k1) fetch_k(t + 2, st);
-      if (t + 1 < k1) fetch_v(t + 1, st ^ 1);
+      const int i = t - k0;
+      if (t + 3 < k1) fetch_k(t + 3, (i + 3) & 3);
+      if (t + 2 < k1) fetch_v(t + 2, (i + 2) & 3);
       const int limit = limit_of(t + 1);
-      const float top = many_step<D, decltype(mem)::value>(kbuf + (st ^ 1) * TILE, vbuf + st * TILE, lane, q, sc, next, o, l, m, scale,
-                                                           limit, __any(limit < KT));
+      const float top = many_step<D, decltype(mem)::value>(kbuf + ((i + 1) & 3) * TILE, vbuf + (i & 3) * TILE, lane, q, sc, next, o, l, m,
+                                                           scale, limit, __any(limit < KT));
       if (t + 1 < k1) raise(top);
-      if (t + 2 < k1) store_k(t + 2, st);
-      if (t + 1 < k1) store_v(t + 1, st ^ 1);
-      dma_wait();
-      __syncthreads();
+      if (t + 3 < k1) store_k(t + 3, (i + 3) & 3);
+      if (t + 2 < k1) store_v(t + 2, (i + 2) & 3);
+      if (i & 1) {
+        dma_wait();
+        __syncthreads();
+      }
     };
     const auto steps = [&](auto mem, int t, int end) __attribute__((always_inline)) {     // (two at a time: scores stay where they are)
       for (; t + 1 < end; t += 2) {
@@ -1488,7 +1503,8 @@ hipError_t prepare() {
   if (e == hipSuccess) e = allow(attend_few<D, 1, kAll>, Few<D, 1>::LDS);
   if (e == hipSuccess) e = allow(attend_few<D, 2, 1>, Few<D, 2>::LDS);
   if (e == hipSuccess) e = allow(attend_few<D, 2, kAll>, Few<D, 2>::LDS);
-  static_assert(Many<D>::LDS <= 65536, "");
+  if (e == hipSuccess) e = allow(attend_many<D, 1>, Many<D>::LDS);
+  if (e == hipSuccess) e = allow(attend_many<D, kAll>, Many<D>::LDS);
   return e;
 }
 
