@@ -36,6 +36,29 @@ __device__ inline uint2 gload8(const void* p) {
   return make_uint2(v[0], v[1]);
 }
 
+// C consecutive elements of a row (4 or 8) as they lie in memory, and as fp32.
+template <int C, typename T>
+struct Raw {
+  static constexpr int WORDS = C * (int)sizeof(T) / 4;
+  uint32_t w[WORDS];
+  __device__ inline void load(const T* p) {
+#pragma unroll
+    for (int i = 0; i < WORDS; i += 4) {
+      if constexpr (WORDS == 2) {
+        const uint2 y = gload8(p);
+        w[0] = y.x; w[1] = y.y;
+      } else {
+        const uint4 y = gload16(reinterpret_cast<const uint32_t*>(p) + i);
+        w[i] = y.x; w[i + 1] = y.y; w[i + 2] = y.z; w[i + 3] = y.w;
+      }
+    }
+  }
+  __device__ inline float operator[](int i) const {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
+    return __uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
+  }
+};
+
 // The eight values (fp32) of a word of codes (the conversions give NaN where
 // the scale is kScaleNan).
 __device__ inline void values8(uint32_t w, uint32_t byte, float (&x)[8]) {

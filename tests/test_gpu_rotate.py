@@ -118,3 +118,30 @@ def test_more_sequences_than_a_launch_describes():
     torch.cuda.synchronize()
     assert torch.equal(out, one) and out.abs().sum(-1).gt(0).all()
     attn.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d,neighbours", [(128, False), (64, True)])
+def test_many_tokens_turn_as_few_do(dtype, d, neighbours):
+    """More tokens than go by a workgroup each: against calls of a part of them (fp32 sums in the same order)."""
+    h_q, h_kv, lengths = 5, 1, [2500, 1, 1700, 33]
+    g = torch.Generator(device="cuda").manual_seed(4)
+    attn = om.Attention(h_q, h_kv, d, om.BF16 if dtype == "bf16" else om.F32)
+    w = rows(g, (2, d), dtype)
+    rope = om.make_rope(d, [0.9 ** j for j in range(d // 2 - 8)], axis=[j % 2 for j in range(d // 2 - 8)], neighbours=neighbours,
+                        q_weight=w[0], k_weight=w[1])
+    x = [rows(g, (h_q + 2 * h_kv, n, d), dtype) for n in lengths]
+    pos = [torch.randint(0, 10000, (2, n), generator=g, device="cuda").to(torch.int32) for n in lengths]
+    mod = [torch.randint(0, 2, (n,), generator=g, device="cuda").to(torch.uint8) for n in lengths]
+    many, few = ([torch.full_like(t, 7.0) for t in x] for _ in range(2))
+    m_many, m_few = ([torch.full((n,), 9, dtype=torch.uint8, device="cuda") for n in lengths] for _ in range(2))
+    split = lambda t, a=0, b=None: (t[:h_q, a:b], t[h_q: h_q + h_kv, a:b], t[h_q + h_kv:, a:b])
+    attn.omnimem_rotate(rope, [om.make_projection(*split(t), p, *split(o), m, mo) for t, p, o, m, mo in zip(x, pos, many, mod, m_many)])
+    for t, p, o, m, mo in zip(x, pos, few, mod, m_few):
+        for a in range(0, t.shape[1], 1000):
+            b = min(a + 1000, t.shape[1])
+            attn.omnimem_rotate(rope, [om.make_projection(*split(t, a, b), p[:, a:b], *split(o, a, b), m[a:b], mo[a:b])])
+    torch.cuda.synchronize()
+    for a, b in zip(many + m_many, few + m_few):
+        assert torch.equal(a, b)
+    attn.close()
