@@ -496,19 +496,20 @@ __global__ __launch_bounds__(256) void attend_f32(AttendArgs<N> a) {
 // ---------------------------------------------------------------------------
 template <int D>
 struct F32Many {
-  static constexpr int R = 128, KT = 64, WAVES = 4;
+  static constexpr int R = 128, KT = 4096 / D, WAVES = 4;
   static constexpr int TILE = KT * D;                      // elements of a K or V stage
-  static constexpr int LDS = 4 * TILE * 4;
-  static constexpr int CPR = D / 4, COPIES = CPR / 4;      // 16-byte chunks per row, 1 KiB copies per wavefront
+  static constexpr int LDS = 4 * TILE * 4;                 // 64 KiB: two workgroups to a CU
+  static constexpr int CPR = D / 4, COPIES = 4;            // 16-byte chunks per row, 1 KiB copies per wavefront
   __device__ static inline int k_chunk(int r, int c) { return c ^ (r & (CPR - 1)); }
 };
 
 template <int D, int N>
-__global__ __launch_bounds__(256) void attend_f32_many(AttendArgs<N> a) {
+__global__ __launch_bounds__(256, 2) void attend_f32_many(AttendArgs<N> a) {
   using P = F32Many<D>;
   using M = Mfma<float>;
   using B = MemBlock<D>;
-  constexpr int R = P::R, KT = P::KT, TILE = P::TILE, CPR = P::CPR, NCT = D / 32, W = D / 32;
+  constexpr int R = P::R, KT = P::KT, TILE = P::TILE, CPR = P::CPR, NCT = D / 32;
+  constexpr int W = 2, TPR = 256 / KT, WPC = KT / 8;       // words of codes to a thread, threads to a key, words to a channel
   extern __shared__ __align__(16) char lds[];
   float* kbuf = reinterpret_cast<float*>(lds);             // [2][TILE]
   float* vbuf = kbuf + 2 * TILE;
@@ -540,23 +541,23 @@ __global__ __launch_bounds__(256) void attend_f32_many(AttendArgs<N> a) {
       dma16_opaque_s(tile, (uint32_t)min(r, keys - 1) * rsb + (is_k ? P::k_chunk(r, c) : c) * 16, to + J * 256);
     }
   };
-  // a memory tile on its way: K by rows, 4 threads to one; V by channels, 8 / W threads to one
+  // a memory tile on its way: K by rows, V by channels
   uint32_t kw[W], vw[W], kb = 0, vb = 0;
-  const int krow = tid / 4, vch = tid * W / 8, vt8 = tid * W % 8;
+  const int krow = tid / TPR, kw0 = tid % TPR * W, vch = tid * W / WPC, vw0 = tid * W % WPC;
   const auto fetch = [&](int t, int st) __attribute__((always_inline)) {
     if (t >= mem_tiles) {
       copy(kp, kbuf + st * TILE, t, true);
       copy(vp, vbuf + st * TILE, t, false);
       return;
     }
-    const char* p = data + (int64_t)min(t * 2 + krow / 32, last_block) * B::BYTES;
-    const char* v = data + (int64_t)min(t * 2 + vt8 / 4, last_block) * B::BYTES;
+    const char* p = data + (int64_t)min(t * (KT / 32) + krow / 32, last_block) * B::BYTES;
+    const char* v = data + (int64_t)min(t * (KT / 32) + vw0 / 4, last_block) * B::BYTES;
 #pragma unroll
     for (int j = 0; j < W; ++j) {
-      kw[j] = gload<uint32_t>(p + (krow & 31) * (D / 2) + ((tid & 3) * W + j) * 4);
-      vw[j] = gload<uint32_t>(v + B::V + vch * 16 + (vt8 % 4 + j) * 4);
+      kw[j] = gload<uint32_t>(p + (krow & 31) * (D / 2) + (kw0 + j) * 4);
+      vw[j] = gload<uint32_t>(v + B::V + vch * 16 + (vw0 % 4 + j) * 4);
     }
-    kb = gload<uint8_t>(p + B::k_scale(krow & 31, (tid & 3) * (D / 4) / 32));
+    kb = gload<uint8_t>(p + B::k_scale(krow & 31, kw0 / 4));
     vb = gload<uint8_t>(v + B::v_scale(vch));
   };
   const auto store = [&](int t, int st) __attribute__((always_inline)) {
@@ -567,12 +568,12 @@ __global__ __launch_bounds__(256) void attend_f32_many(AttendArgs<N> a) {
     for (int j = 0; j < W; ++j) {
       float y[8];
       values8(kw[j], kb, y);
-      const int c = ((tid & 3) * W + j) * 2;
+      const int c = (kw0 + j) * 2;
       *reinterpret_cast<floatx4*>(kd + P::k_chunk(krow, c) * 4) = floatx4{y[0], y[1], y[2], y[3]};
       *reinterpret_cast<floatx4*>(kd + P::k_chunk(krow, c + 1) * 4) = floatx4{y[4], y[5], y[6], y[7]};
       values8(vw[j], vb, y);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) vd[((vt8 + j) * 8 + e) * D] = y[e];
+      for (int e = 0; e < 8; ++e) vd[((vw0 + j) * 8 + e) * D] = y[e];
     }
   };
 
@@ -586,24 +587,31 @@ __global__ __launch_bounds__(256) void attend_f32_many(AttendArgs<N> a) {
     const int st = (t - x.k0) & 1;
     if (t + 1 < x.k1) fetch(t + 1, st ^ 1);
     const int limit = (t < mem_tiles ? nm - t * KT : row.seen - (t - mem_tiles) * KT) - half * 4;
+    const bool masked = __any(limit <= KT - 5);            // the tile's last key of this half is KT - 5 behind its first
+    const auto k_quad = [&](int b, int j) __attribute__((always_inline)) {
+      return *reinterpret_cast<const floatx4*>(kbuf + st * TILE + (b * 32 + col) * D + P::k_chunk(b * 32 + col, 2 * j + half) * 4);
+    };
+    // (the key of accumulator register r of this half)
+    const float* vd = vbuf + st * TILE + half * 4 * D + col;
+    const auto v_one = [&](int b, int i) __attribute__((always_inline)) {
+      const int r = i / NCT;
+      return vd[(b * 32 + (r >> 2) * 8 + (r & 3)) * D + i % NCT * 32];
+    };
+    floatx16 sc[KT / 32];
+    float ref;
+    const auto scores = [&](int b, auto&& between) __attribute__((always_inline)) {
+      floatx4 k[3] = {k_quad(b, 0), k_quad(b, 1), {}};
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      const float* kd = kbuf + st * TILE + (b * 32 + col) * D;
-      floatx16 sc = floatx16{};
-#pragma unroll
-      for (int j = 0; j < D / 8; ++j) {
-        const floatx4 k = *reinterpret_cast<const floatx4*>(kd + P::k_chunk(b * 32 + col, 2 * j + half) * 4);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) sc = M::mma(k[e], q[j][e], sc);
+      for (int i = 0; i < D / 2; ++i) {
+        if (i % 4 == 0 && i / 4 + 2 < D / 8) k[(i / 4 + 2) % 3] = k_quad(b, i / 4 + 2);
+        sc[b] = M::mma(k[i / 4 % 3][i % 4], q[i / 4][i % 4], i ? sc[b] : floatx16{});
+        pin(sc[b]);
+        between(i);
       }
-      float top = -INFINITY;
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        sc[r] = b * 32 + (r >> 2) * 8 + (r & 3) < limit ? sc[r] * s.scale_log2 : -INFINITY;
-        top = fmaxf(top, sc[r]);
-      }
+    };
+    const auto reference = [&](float top) __attribute__((always_inline)) {
       top = max32(top);
-      if (__any(top > m + 8.0f)) {                         // (see attend_many)
+      if (__any(top > m + 8.0f)) {                           // (see attend_many)
         const float m2 = fmaxf(m, top);
         const float alpha = m2 == -INFINITY ? 1.0f : exp2_(m - m2);
         m = m2;
@@ -611,18 +619,62 @@ __global__ __launch_bounds__(256) void attend_f32_many(AttendArgs<N> a) {
 #pragma unroll
         for (int c = 0; c < NCT; ++c) o[c] *= alpha;
       }
-      const float ref = m == -INFINITY ? 0.0f : m;
+      ref = m == -INFINITY ? 0.0f : m;
+    };
+    const auto weight = [&](int b, int r) __attribute__((always_inline)) {
+      sc[b][r] = exp2_(sc[b][r] - ref);
+      l += sc[b][r];
+      pin(l);
+    };
+    const auto values = [&](int b, auto&& between) __attribute__((always_inline)) {
+      constexpr int N16 = 16 * NCT, A = 8;
+      float v[A];
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        sc[r] = exp2_(sc[r] - ref);
-        l += sc[r];
+      for (int i = 0; i < A; ++i) v[i] = v_one(b, i);
+#pragma unroll
+      for (int i = 0; i < N16; ++i) {
+        o[i % NCT] = M::mma(v[i % A], sc[b][i / NCT], o[i % NCT]);
+        pin(o[i % NCT]);
+        if (i + A < N16) v[i % A] = v_one(b, i + A);
+        between(i);
       }
-      // (the keys of accumulator register r of this half)
-      const float* vd = vbuf + st * TILE + (b * 32 + half * 4) * D + col;
+    };
+    const auto settle = [&](int b) __attribute__((always_inline)) {
+      sc[b] *= s.scale_log2;
+      if (!masked) return;
 #pragma unroll
-      for (int c = 0; c < NCT; ++c)
+      for (int r = 0; r < 16; ++r)
+        if (b * 32 + (r >> 2) * 8 + (r & 3) >= limit) sc[b][r] = -INFINITY;
+    };
+    const auto all_weights = [&](int b) __attribute__((always_inline)) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) o[c] = M::mma(vd[((r >> 2) * 8 + (r & 3)) * D + c * 32], sc[r], o[c]);
+      for (int r = 0; r < 16; ++r) weight(b, r);
+    };
+    float top = -INFINITY;
+    scores(0, [](int) {});
+    settle(0);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) top = fmaxf(top, sc[0][r]);
+    reference(top);
+    if constexpr (KT == 32) {
+      all_weights(0);
+      values(0, [](int) {});
+    } else {                                               // vector instructions of a block between MFMAs of the other
+      scores(1, [&](int i) __attribute__((always_inline)) {
+#pragma unroll
+        for (int r = i * 32 / D; r < (i + 1) * 32 / D; ++r) weight(0, r);
+      });
+      settle(1);
+      top = -INFINITY;
+      values(0, [&](int i) __attribute__((always_inline)) {
+        if (i % NCT == 0) {
+          top = fmaxf(top, sc[1][i / NCT]);
+          pin(top);
+        }
+      });
+      reference(top);
+      all_weights(1);
+      values(1, [](int) {});
     }
     if (t + 1 < x.k1) store(t + 1, st ^ 1);
     dma_wait();
