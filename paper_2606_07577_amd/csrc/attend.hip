@@ -1157,15 +1157,16 @@ __global__ __launch_bounds__(512, 2) void attend_many(AttendArgs<N> a) {
   };
   const auto fetch_k = [&](int t, int st) __attribute__((always_inline)) {
     if (t >= mem_tiles) { copy(kp, kbuf + st * TILE, t, true); return; }
-    const char* p = data + (int64_t)min(t * 2 + krow / 32, last_block) * B::BYTES;
-    words(p + (krow & 31) * (D / 2) + (tid & 7) * (D / 16), kw);
-    kb = gload<uint8_t>(p + B::k_scale(krow & 31, (tid & 7) * (D / 8) / 32));
+    const char* p = data + (int64_t)min(t * 2 + wave / 4, last_block) * B::BYTES;   // (wavefronts 4 .. have rows 32 ..)
+    words(p + (uint32_t)((krow & 31) * (D / 2) + (tid & 7) * (D / 16)), kw);
+    kb = gload<uint8_t>(p + (uint32_t)B::k_scale(krow & 31, (tid & 7) * (D / 8) / 32));
   };
   const auto fetch_v = [&](int t, int st) __attribute__((always_inline)) {
     if (t >= mem_tiles) { copy(vp, vbuf + st * TILE, t, false); return; }
-    const char* p = data + (int64_t)min(t * 2 + vt8 / 4, last_block) * B::BYTES;
-    words(p + B::V + vch * 16 + vt8 % 4 * 4, vw);
-    vb = gload<uint8_t>(p + B::v_scale(vch));
+    const char* p = data + (int64_t)(t * 2) * B::BYTES;
+    const uint32_t block = vt8 >= 4 && t * 2 < last_block ? B::BYTES : 0;
+    words(p + (block + (uint32_t)(B::V + vch * 16 + vt8 % 4 * 4)), vw);
+    vb = gload<uint8_t>(p + (block + (uint32_t)B::v_scale(vch)));
   };
   const auto store_k = [&](int t, int st) __attribute__((always_inline)) {
     if (t >= mem_tiles) return;
