@@ -91,7 +91,7 @@ bool readable(const omnimem_attn* a, const void* p, int64_t hs, int64_t rs) {
 bool writable(const omnimem_attn* a, const void* p, int64_t heads, int64_t rows, int64_t hs, int64_t rs) {
   const int64_t d = a->cfg.head_dim;
   if (!readable(a, p, hs, rs)) return false;
-  return heads == 1 || rows <= 1 || hs >= (rows - 1) * rs + d || (hs >= d && rs >= (heads - 1) * hs + d);
+  return heads == 1 || hs >= (rows - 1) * rs + d || (hs >= d && rs >= (heads - 1) * hs + d);
 }
 
 const char* kStride = "must be given, 16-byte aligned, strides of whole 16-byte units, row stride >= head_dim";

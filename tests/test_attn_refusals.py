@@ -245,3 +245,17 @@ def test_handles_refuse_descriptors_of_another_layout():
     p._layout = fine._replace(axes=1)
     with pytest.raises(ValueError, match="axes"):
         attn.omnimem_rotate(om.make_rope(64, [0.5] * 8, axis=[0, 1] * 4), [p])
+
+
+def refused(lib, attn, name, kind, fields, more, changes):
+    for change in changes:
+        lib.standin_launches()
+        assert call(lib, attn, name, kind, fields, more=more, **change) == om.ERR_INVALID_ARG, change
+        assert b"sequence 0" in lib.omnimem_attn_last_error(attn) and lib.standin_launches() == 0, change
+
+
+def test_one_row_of_several_heads_needs_a_place_for_each(lib, attn):
+    refused(lib, attn, "omnimem_rotate", om.Projection, dict(projection(attn.elt), n_rows=1), (rope(),),
+            [dict(q_out_head_stride=0), dict(out_head_stride=0), dict(out_head_stride=32)])
+    refused(lib, attn, "omnimem_unpack", om.Held, dict(held(), n_rows=1), (), [dict(kv_head_stride=0)])
+    refused(lib, attn, "omnimem_attend", om.Query, dict(query(), n_queries=1), (1,), [dict(out_head_stride=0)])
