@@ -389,7 +389,8 @@ omnimem_status omnimem_profile_report(omnimem_ctx* ctx, omnimem_kernel_time* out
  * after create, calls on one handle ordered (its workspace is shared by them;
  * so are graphs captured from it, which must not run at the same time).
  * Calls can be captured into graphs: descriptors travel as kernel arguments.
- * The outputs of a call's sequences must not overlap.
+ * The outputs of a call's sequences must not overlap, and an array spans less
+ * than 64 TiB.
  * ------------------------------------------------------------------------- */
 typedef struct {
   int32_t n_q_heads;        /* H_q                                            */

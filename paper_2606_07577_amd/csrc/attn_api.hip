@@ -81,20 +81,23 @@ bool overlap(const Span& a, const Span& b) {
   return true;
 }
 bool same(const Span& a, const Span& b) { return a.base == b.base && (a.hs == b.hs || a.heads == 1) && (a.rs == b.rs || a.rows == 1); }
-// Rows that are read: strides of 16-byte units below 64 GiB, rows of at least d.
-bool readable(const omnimem_attn* a, const void* p, int64_t hs, int64_t rs) {
+// Rows that are read: strides of 16-byte units below 64 GiB, rows of at least
+// d, and no array past 64 TiB (sums of products of strides fit 64 bits).
+constexpr int64_t kMaxSpan = (int64_t)1 << 46;
+bool readable(const omnimem_attn* a, const void* p, int64_t heads, int64_t rows, int64_t hs, int64_t rs) {
   const int64_t e = (int64_t)elt(a);
   return p && aligned(p, 16) && hs >= 0 && rs >= a->cfg.head_dim && hs % (16 / e) == 0 && rs % (16 / e) == 0 &&
-         hs / (16 / e) <= UINT32_MAX && rs / (16 / e) <= UINT32_MAX;
+         hs / (16 / e) <= UINT32_MAX && rs / (16 / e) <= UINT32_MAX &&
+         (double)(heads - 1) * (double)hs + (double)(rows - 1) * (double)rs < (double)(kMaxSpan / e);
 }
 // Rows that are written: each row of each head has its own place.
 bool writable(const omnimem_attn* a, const void* p, int64_t heads, int64_t rows, int64_t hs, int64_t rs) {
   const int64_t d = a->cfg.head_dim;
-  if (!readable(a, p, hs, rs)) return false;
+  if (!readable(a, p, heads, rows, hs, rs)) return false;
   return heads == 1 || hs >= (rows - 1) * rs + d || (hs >= d && rs >= (heads - 1) * hs + d);
 }
 
-const char* kStride = "must be given, 16-byte aligned, strides of whole 16-byte units, row stride >= head_dim";
+const char* kStride = "must be given, 16-byte aligned, strides of whole 16-byte units, row stride >= head_dim, all below 64 TiB";
 
 omnimem_status begin(omnimem_attn* attn, const void* seqs, int32_t n) {
   if (!attn) return fail(nullptr, OMNIMEM_ERR_INVALID_ARG, "null handle");
@@ -112,14 +115,15 @@ omnimem_status check_held(omnimem_attn* attn, const omnimem_held& s, int i, bool
   const int H = attn->cfg.n_kv_heads;
   if (s.n_rows < 0 || s.n_rows > kMaxRows) return bad(attn, i, "n_rows out of range");
   if (s.n_rows == 0) return OMNIMEM_OK;
-  const bool ok = pack ? readable(attn, s.k, s.kv_head_stride, s.kv_row_stride) && readable(attn, s.v, s.kv_head_stride, s.kv_row_stride)
+  const bool ok = pack ? readable(attn, s.k, H, s.n_rows, s.kv_head_stride, s.kv_row_stride) &&
+                             readable(attn, s.v, H, s.n_rows, s.kv_head_stride, s.kv_row_stride)
                        : writable(attn, s.k, H, s.n_rows, s.kv_head_stride, s.kv_row_stride) &&
                              writable(attn, s.v, H, s.n_rows, s.kv_head_stride, s.kv_row_stride);
   if (!ok) return fail(attn, OMNIMEM_ERR_INVALID_ARG, "sequence %d: k and v %s", i, kStride);
   const int64_t bytes = omnimem_memory_bytes(attn->cfg.head_dim, s.n_rows);
   if (!s.data || !aligned(s.data, 16) || s.data_head_stride % 16 || s.data_head_stride < 0 ||
-      (H > 1 && s.data_head_stride < bytes))
-    return bad(attn, i, "data must be given, 16-byte aligned, its head stride a multiple of 16 and at least a head's bytes");
+      s.data_head_stride >= kMaxSpan / 1024 || (H > 1 && s.data_head_stride < bytes))
+    return bad(attn, i, "data must be given, 16-byte aligned, its head stride a multiple of 16, at least a head's bytes and below 64 GiB");
   const Span k = span(attn, s.k, H, s.n_rows, s.kv_head_stride, s.kv_row_stride);
   const Span v = span(attn, s.v, H, s.n_rows, s.kv_head_stride, s.kv_row_stride);
   const Span m = {reinterpret_cast<uintptr_t>(s.data), H, 1, s.data_head_stride, bytes, bytes};
@@ -229,11 +233,12 @@ omnimem_status omnimem_rotate(omnimem_attn* attn, const omnimem_rope* rope, cons
     const omnimem_projection& s = seqs[i];
     if (s.n_rows < 0 || s.n_rows > kMaxRows) return bad(attn, i, "n_rows out of range");
     if (s.n_rows == 0) continue;
-    if (!readable(attn, s.q, s.q_head_stride, s.q_row_stride) || !readable(attn, s.k, s.kv_head_stride, s.kv_row_stride) ||
-        !readable(attn, s.v, s.kv_head_stride, s.kv_row_stride))
+    if (!readable(attn, s.q, c.n_q_heads, s.n_rows, s.q_head_stride, s.q_row_stride) ||
+        !readable(attn, s.k, c.n_kv_heads, s.n_rows, s.kv_head_stride, s.kv_row_stride) ||
+        !readable(attn, s.v, c.n_kv_heads, s.n_rows, s.kv_head_stride, s.kv_row_stride))
       return fail(attn, OMNIMEM_ERR_INVALID_ARG, "sequence %d: q, k and v %s", i, kStride);
-    if (!s.pos || !aligned(s.pos, 4) || s.pos_stride < 0)
-      return bad(attn, i, "pos must be given, 4-byte aligned, its stride >= 0");
+    if (!s.pos || !aligned(s.pos, 4) || s.pos_stride < 0 || s.pos_stride >= kMaxSpan / 16)
+      return bad(attn, i, "pos must be given, 4-byte aligned, its stride >= 0 and below 2^42");
     if (!writable(attn, s.q_out, c.n_q_heads, s.n_rows, s.q_out_head_stride, s.q_out_row_stride) ||
         !writable(attn, s.k_out, c.n_kv_heads, s.n_rows, s.out_head_stride, s.out_row_stride) ||
         !writable(attn, s.v_out, c.n_kv_heads, s.n_rows, s.out_head_stride, s.out_row_stride))
@@ -285,15 +290,15 @@ omnimem_status omnimem_attend(omnimem_attn* attn, const omnimem_query* seqs, int
   const int Hq = c.n_q_heads, H = c.n_kv_heads;
   for (int i = 0; i < n; ++i) {
     const omnimem_query& s = seqs[i];
-    if (s.n_queries < 0 || s.n_queries * attn->dm.group > kMaxRows || s.n_queries > kMaxRows || s.memory_rows < 0 ||
+    if (s.n_queries < 0 || s.n_queries > kMaxRows / attn->dm.group || s.memory_rows < 0 ||
         s.memory_rows > kMaxRows || s.n_tail < 0 || s.n_tail > kMaxRows)
       return bad(attn, i, "n_queries, memory_rows or n_tail out of range");
     if (s.n_queries == 0) continue;
     if (!std::isfinite(s.sm_scale)) return bad(attn, i, "sm_scale is not finite");
-    if (!readable(attn, s.q, s.q_head_stride, s.q_row_stride))
+    if (!readable(attn, s.q, Hq, s.n_queries, s.q_head_stride, s.q_row_stride))
       return fail(attn, OMNIMEM_ERR_INVALID_ARG, "sequence %d: q %s", i, kStride);
-    if (s.n_tail > 0 && (!readable(attn, s.k, s.kv_head_stride, s.kv_row_stride) ||
-                         !readable(attn, s.v, s.kv_head_stride, s.kv_row_stride)))
+    if (s.n_tail > 0 && (!readable(attn, s.k, H, s.n_tail, s.kv_head_stride, s.kv_row_stride) ||
+                         !readable(attn, s.v, H, s.n_tail, s.kv_head_stride, s.kv_row_stride)))
       return fail(attn, OMNIMEM_ERR_INVALID_ARG, "sequence %d: k and v %s", i, kStride);
     if (s.n_tail > 0 && s.kv_row_stride * (int64_t)elt(attn) >= (int64_t)1 << 24)
       return bad(attn, i, "k and v need a row stride below 16 MiB");

@@ -259,3 +259,15 @@ def test_one_row_of_several_heads_needs_a_place_for_each(lib, attn):
             [dict(q_out_head_stride=0), dict(out_head_stride=0), dict(out_head_stride=32)])
     refused(lib, attn, "omnimem_unpack", om.Held, dict(held(), n_rows=1), (), [dict(kv_head_stride=0)])
     refused(lib, attn, "omnimem_attend", om.Query, dict(query(), n_queries=1), (1,), [dict(out_head_stride=0)])
+
+
+def test_strides_that_pass_any_address(lib, attn):
+    far = 1 << 34
+    refused(lib, attn, "omnimem_rotate", om.Projection, dict(projection(attn.elt), n_rows=1 << 30), (rope(),),
+            [dict(q_row_stride=far), dict(kv_row_stride=far), dict(q_out_row_stride=far), dict(out_row_stride=far)])
+    refused(lib, attn, "omnimem_rotate", om.Projection, projection(attn.elt), (rope(),), [dict(pos_stride=1 << 62)])
+    for name in ("omnimem_pack", "omnimem_unpack"):
+        refused(lib, attn, name, om.Held, held(), (), [dict(data_head_stride=1 << 62), dict(kv_row_stride=far, n_rows=1 << 30)])
+    refused(lib, attn, "omnimem_attend", om.Query, query(), (1,),
+            [dict(n_queries=1 << 29, q_row_stride=far), dict(n_queries=1 << 29, out_row_stride=far), dict(n_queries=(1 << 62) + 1),
+             dict(n_tail=1 << 30, kv_head_stride=1 << 50)])
