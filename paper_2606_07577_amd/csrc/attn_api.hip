@@ -151,6 +151,10 @@ omnimem_status hold(omnimem_attn* attn, const omnimem_held* seqs, int32_t n, hip
   return done(attn, e, pack ? "omnimem_pack" : "omnimem_unpack");
 }
 
+float log2_scale(const omnimem_query& s, int d) {
+  return (float)((s.sm_scale != 0.0f ? (double)s.sm_scale : 1.0 / std::sqrt((double)d)) * 1.4426950408889634);
+}
+
 }  // namespace
 
 extern "C" {
@@ -175,6 +179,7 @@ omnimem_status omnimem_attn_create(const omnimem_attn_config* cfg, omnimem_attn*
       attn->compute_units = cus;
     e = hipMalloc(&attn->workspace, (size_t)kPartBytes + kMaxPartials * sizeof(int));
     if (e == hipSuccess) e = hipMemset(static_cast<char*>(attn->workspace) + kPartBytes, 0, kMaxPartials * sizeof(int));
+    if (e == hipSuccess) e = hipDeviceSynchronize();          // (calls come on streams that do not wait for the null stream)
     if (e == hipSuccess) e = prepare_attend(attn->dm);
   }
   if (e != hipSuccess) {
@@ -294,7 +299,7 @@ omnimem_status omnimem_attend(omnimem_attn* attn, const omnimem_query* seqs, int
         s.memory_rows > kMaxRows || s.n_tail < 0 || s.n_tail > kMaxRows)
       return bad(attn, i, "n_queries, memory_rows or n_tail out of range");
     if (s.n_queries == 0) continue;
-    if (!std::isfinite(s.sm_scale)) return bad(attn, i, "sm_scale is not finite");
+    if (!std::isfinite(log2_scale(s, c.head_dim))) return bad(attn, i, "sm_scale times log2(e) is not finite");
     if (!readable(attn, s.q, Hq, s.n_queries, s.q_head_stride, s.q_row_stride))
       return fail(attn, OMNIMEM_ERR_INVALID_ARG, "sequence %d: q %s", i, kStride);
     if (s.n_tail > 0 && (!readable(attn, s.k, H, s.n_tail, s.kv_head_stride, s.kv_row_stride) ||
@@ -313,13 +318,15 @@ omnimem_status omnimem_attend(omnimem_attn* attn, const omnimem_query* seqs, int
       return bad(attn, i, "lse must be 4-byte aligned, its head stride at least n_queries and below 2^32");
     const Span q = span(attn, s.q, Hq, s.n_queries, s.q_head_stride, s.q_row_stride);
     const Span o = span(attn, s.out, Hq, s.n_queries, s.out_head_stride, s.out_row_stride);
-    bool clash = overlap(o, q);
+    const Span lse = {reinterpret_cast<uintptr_t>(s.lse), Hq, 1, s.lse_head_stride * 4, s.n_queries * 4, s.n_queries * 4};
+    const auto written = [&](const Span& x) { return overlap(o, x) || (s.lse && overlap(lse, x)); };
+    bool clash = written(q) || (s.lse && overlap(o, lse));
     if (s.n_tail > 0)
-      clash = clash || overlap(o, span(attn, s.k, H, s.n_tail, s.kv_head_stride, s.kv_row_stride)) ||
-              overlap(o, span(attn, s.v, H, s.n_tail, s.kv_head_stride, s.kv_row_stride));
+      clash = clash || written(span(attn, s.k, H, s.n_tail, s.kv_head_stride, s.kv_row_stride)) ||
+              written(span(attn, s.v, H, s.n_tail, s.kv_head_stride, s.kv_row_stride));
     if (s.memory_rows > 0)
-      clash = clash || overlap(o, {reinterpret_cast<uintptr_t>(s.memory), H, 1, s.memory_head_stride, bytes, bytes});
-    if (clash) return bad(attn, i, "out overlaps q, k, v or the memory");
+      clash = clash || written({reinterpret_cast<uintptr_t>(s.memory), H, 1, s.memory_head_stride, bytes, bytes});
+    if (clash) return bad(attn, i, "out or lse overlaps the other, q, k, v or the memory");
   }
   OnDevice dev(attn->device);
   hipError_t e = dev.err;
@@ -338,8 +345,7 @@ omnimem_status omnimem_attend(omnimem_attn* attn, const omnimem_query* seqs, int
       x.kv_hs = units(s.kv_head_stride); x.kv_rs = units(s.kv_row_stride);
       x.out_hs = units(s.out_head_stride); x.out_rs = units(s.out_row_stride);
       x.mem_hs = (uint32_t)(s.memory_head_stride / 16); x.lse_hs = (uint32_t)s.lse_head_stride;
-      const double scale = s.sm_scale != 0.0f ? (double)s.sm_scale : 1.0 / std::sqrt((double)c.head_dim);
-      x.scale_log2 = (float)(scale * 1.4426950408889634);
+      x.scale_log2 = log2_scale(s, c.head_dim);
       x.nq = (int32_t)s.n_queries; x.nm = (int32_t)s.memory_rows; x.nt = (int32_t)s.n_tail;
     }
     if (m) e = launch_attend(attn->dm, a, m, attn->compute_units, attn->workspace, stream);

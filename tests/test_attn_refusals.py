@@ -271,3 +271,14 @@ def test_strides_that_pass_any_address(lib, attn):
     refused(lib, attn, "omnimem_attend", om.Query, query(), (1,),
             [dict(n_queries=1 << 29, q_row_stride=far), dict(n_queries=1 << 29, out_row_stride=far), dict(n_queries=(1 << 62) + 1),
              dict(n_tail=1 << 30, kv_head_stride=1 << 50)])
+
+
+def test_lse_that_lies_in_another_array(lib, attn):
+    f = query()
+    refused(lib, attn, "omnimem_attend", om.Query, f, (1,),
+            [dict(lse=f["out"]), dict(lse=f["out"] + 64), dict(lse=f["q"] + 4), dict(lse=f["k"]), dict(lse=f["v"] + 128),
+             dict(lse=f["memory"] + 34 * 64 * 4)])
+
+
+def test_a_scale_that_is_no_fp32_in_log2_units(lib, attn):
+    refused(lib, attn, "omnimem_attend", om.Query, query(), (1,), [dict(sm_scale=3.0e38), dict(sm_scale=-3.0e38)])
