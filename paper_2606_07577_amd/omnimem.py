@@ -417,6 +417,11 @@ def _rows(what, *tensors):
             raise ValueError(f"{what} must share shape, strides and type")
 
 
+def _one_device(*tensors):
+    if len({t.device for t in tensors if t is not None}) != 1:
+        raise ValueError("a descriptor's tensors must lie on one device")
+
+
 def _memory(data, rows, k_like=None):
     if data.dtype != torch.uint8 or data.dim() != 3 or data.stride(2) != 1 or data.stride(1) != data.shape[2]:
         raise ValueError("a memory is a uint8 tensor [H_kv, blocks, 34 d], its blocks contiguous")
@@ -468,6 +473,7 @@ def make_projection(q, k, v, pos, q_out, k_out, v_out, modality=None, modality_o
     for m in (modality, modality_out):
         if m is not None and (m.dtype != torch.uint8 or m.dim() != 1 or m.shape[0] < n or m.stride(0) != 1):
             raise TypeError("modality must be contiguous uint8 [>= n]")
+    _one_device(q, k, v, pos, q_out, k_out, v_out, modality, modality_out)
     p = Projection()
     p.q, p.q_head_stride, p.q_row_stride = _ptr(q), q.stride(0), q.stride(1)
     p.k, p.v, p.kv_head_stride, p.kv_row_stride = _ptr(k), _ptr(v), k.stride(0), k.stride(1)
@@ -483,6 +489,7 @@ def make_held(k, v, data):
     """Descriptor of rows k, v [H_kv, n, d] and the memory that holds them: uint8 of memory_shape (or with more blocks)."""
     _rows("k and v", k, v)
     _memory(data, k.shape[1], k)
+    _one_device(k, v, data)
     h = Held()
     h.k, h.v, h.kv_head_stride, h.kv_row_stride = _ptr(k), _ptr(v), k.stride(0), k.stride(1)
     h.data, h.data_head_stride, h.n_rows = _ptr(data), data.stride(0), k.shape[1]
@@ -511,6 +518,7 @@ def make_query(q, out, k=None, v=None, memory=None, memory_rows=0, sm_scale=0.0,
         raise ValueError("memory_rows without a memory")
     if lse is not None and (lse.dtype != torch.float32 or lse.shape != q.shape[:2] or lse.stride(1) != 1):
         raise ValueError("lse must be fp32 [H_q, n], its queries contiguous")
+    _one_device(q, out, k, v, memory, lse)
     x = Query()
     x.q, x.q_head_stride, x.q_row_stride, x.n_queries = _ptr(q), q.stride(0), q.stride(1), q.shape[1]
     x.out, x.out_head_stride, x.out_row_stride = _ptr(out), out.stride(0), out.stride(1)

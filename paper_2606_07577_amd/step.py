@@ -88,9 +88,10 @@ class DeviceStep:
         if self.attn is None:
             self.attn = om.Attention(self.h_q, self.h_kv, self.d, om.BF16 if self.dtype_name == "bf16" else om.F32)
             chunk = [n - c for n, c in zip(self.n, self.n_cache)]
-            self.attn_out = [torch.zeros((c, self.h_q, self.d), device=self.device, dtype=self.tdtype).transpose(0, 1)
-                             for c in chunk]
-            lse = [torch.zeros((self.h_q, c), device=self.device, dtype=torch.float32) for c in chunk]
+            with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream()):
+                self.attn_out = [torch.zeros((c, self.h_q, self.d), device=self.device, dtype=self.tdtype).transpose(0, 1)
+                                 for c in chunk]
+                lse = [torch.zeros((self.h_q, c), device=self.device, dtype=torch.float32) for c in chunk]
             self._queries = om.array_of([om.make_query(self.q[l], self.attn_out[l], self.k[l], self.v[l],
                                                        sm_scale=self.sm_scale[l], lse=lse[l])
                                          for l in range(self.n_layers)])
@@ -207,7 +208,7 @@ class StreamRunner:
         self.fallbacks = 0         # steps compacted out of place for lack of staging rows
         self.keep_working_set = keep_working_set
         self.working_set = None    # [L] of (k, v, modality) copies of the last step's working set
-        self.attn = None           # made by hold() and restore()
+        self.attn = None           # made by hold() or restore()
         self._layers = (om.Layer * n_layers)()
         self._chunks = (om.Chunk * n_layers)()
         self._budget_ready = torch.cuda.Event()
@@ -249,13 +250,12 @@ class StreamRunner:
         are read from (see Reader), a quarter of the cache's bytes to keep
         until the stream goes on (see restore)."""
         budgets = self.finish()
-        if budgets is None:
-            budgets = self._held_budgets()
-        if self.attn is None:
-            self.attn = om.Attention(self.h_q, self.h_kv, self.d, om.BF16 if self.tdtype == torch.bfloat16 else om.F32)
-        data = [torch.empty(om.memory_shape(self.h_kv, self.d, n), dtype=torch.uint8, device=self.device)
-                for n in self.n_cache]
-        self.attn.omnimem_pack(self._held(data), stream)
+        with torch.cuda.stream(self._behind_step(stream)):
+            if budgets is None:
+                budgets = self._held_budgets()
+            data = [torch.empty(om.memory_shape(self.h_kv, self.d, n), dtype=torch.uint8, device=self.device)
+                    for n in self.n_cache]
+            self.attn.omnimem_pack(self._held(data, self.n_cache))
         return HeldMemory(data, list(self.n_cache), [int(b) for b in budgets[:, 0]])
 
     def restore(self, held, stream=None):
@@ -263,18 +263,24 @@ class StreamRunner:
         self.finish()
         if len(held.rows) != self.L or max(held.rows) > self.cache_cap:
             raise ValueError("the memory has another number of layers, or more rows than the caches hold")
-        if self.attn is None:
-            self.attn = om.Attention(self.h_q, self.h_kv, self.d, om.BF16 if self.tdtype == torch.bfloat16 else om.F32)
-        self.n_cache = list(held.rows)
-        self.attn.omnimem_unpack(self._held(held.data), stream)
-        with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream()):
+        with torch.cuda.stream(self._behind_step(stream)):
+            self.attn.omnimem_unpack(self._held(held.data, held.rows))
             for mod, n, visual in zip(self.mbuf[self.cur], held.rows, held.visual):
                 mod[:visual] = 0
                 mod[visual:n] = 1
+        self.n_cache = list(held.rows)
 
-    def _held(self, data):
-        return [om.make_held(self.kbuf[self.cur][l][:, : self.n_cache[l]], self.vbuf[self.cur][l][:, : self.n_cache[l]], data[l])
-                for l in range(self.L)]
+    def _behind_step(self, stream):
+        """The stream (default: the current one) for work on the caches, made to wait for the last step's."""
+        stream = stream if stream is not None else torch.cuda.current_stream()
+        if self._pending_stream is not None and self._pending_stream != stream:
+            stream.wait_stream(self._pending_stream)
+        if self.attn is None:
+            self.attn = om.Attention(self.h_q, self.h_kv, self.d, om.BF16 if self.tdtype == torch.bfloat16 else om.F32)
+        return stream
+
+    def _held(self, data, rows):
+        return [om.make_held(self.kbuf[self.cur][l][:, :n], self.vbuf[self.cur][l][:, :n], data[l]) for l, n in enumerate(rows)]
 
     def _held_budgets(self):
         """Kept visual and audio rows of the caches as they are."""
@@ -460,6 +466,8 @@ class Reader:
         self.tdtype = torch.bfloat16 if dtype == "bf16" else torch.float32
         self.h_q, self.h_kv, self.d, self.cap = h_q, h_kv, d, int(capacity)
         self.memories, self.rope, self.sm_scale = list(memories), rope, float(sm_scale)
+        if not self.memories or len({len(m.data) for m in self.memories}) != 1:
+            raise ValueError("one memory at least, all of one number of layers")
         self.attn = om.Attention(h_q, h_kv, d, om.BF16 if dtype == "bf16" else om.F32)
         n_layers = len(self.memories[0].data)
         shape = (n_layers, len(self.memories), h_kv, self.cap, d)
@@ -474,6 +482,8 @@ class Reader:
         keys and values go behind the stream's tail, and the queries attend to
         its memory and tail.  Returns [H_q, n_b, d] for each stream."""
         new = [x.shape[1] for x in k]
+        if not len(q) == len(k) == len(v) == len(pos) == len(self.memories):
+            raise ValueError(f"q, k, v and pos are lists of {len(self.memories)} streams' tensors")
         if self._new is not None and new != self._new:
             raise ValueError("every layer takes the same numbers of tokens (next() begins the next ones)")
         if any(t + n > self.cap for t, n in zip(self.tail, new)):

@@ -282,3 +282,16 @@ def test_lse_that_lies_in_another_array(lib, attn):
 
 def test_a_scale_that_is_no_fp32_in_log2_units(lib, attn):
     refused(lib, attn, "omnimem_attend", om.Query, query(), (1,), [dict(sm_scale=3.0e38), dict(sm_scale=-3.0e38)])
+
+
+def test_descriptors_refuse_tensors_of_several_devices():
+    t = lambda *s, dtype=torch.bfloat16, device="cpu": torch.zeros(*s, dtype=dtype, device=device)
+    rows = [t(h, 5, 64) for h in (4, 2, 2)]
+    far = [t(h, 5, 64, device="meta") for h in (4, 2, 2)]
+    pos = t(1, 5, dtype=torch.int32)
+    with pytest.raises(ValueError, match="one device"):
+        om.make_projection(*rows, pos, *far)
+    with pytest.raises(ValueError, match="one device"):
+        om.make_held(rows[1], rows[2], t(*om.memory_shape(2, 64, 5), dtype=torch.uint8, device="meta"))
+    with pytest.raises(ValueError, match="one device"):
+        om.make_query(rows[0], rows[0], far[1], far[2])

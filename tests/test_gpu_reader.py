@@ -197,3 +197,68 @@ def test_handles_on_two_streams_at_once():
     assert torch.equal(out, ref)
     for h in handles:
         h.close()
+
+
+def test_a_chunks_attention_first_run_on_another_stream():
+    """What attend() makes at its first call is made on its stream: the current one is behind."""
+    layer = synth.make_layer([5, 2], h_q=4, h_kv=2, d=64, n_cache_v=90, n_cache_a=30, n_frames=2, frame_v=20, frame_a=5,
+                             dup_frac=0.3, head_scale=(0.5, 2.0), dtype="bf16")
+    plain, step = DeviceStep([layer], 80), DeviceStep([layer], 80)
+    plain.attend()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    torch.cuda._sleep(20_000_000)
+    step.attend(side)
+    torch.cuda.synchronize()
+    assert torch.equal(step.attn_out[0], plain.attn_out[0]) and torch.equal(step.lse_in[0], plain.lse_in[0])
+    plain.close()
+    step.close()
+
+
+def test_caches_held_behind_a_step_on_another_stream():
+    layers, h_q, h_kv, d, n = 2, 4, 2, 64, 160
+    g = torch.Generator(device="cuda").manual_seed(7)
+    run = StreamRunner(layers, h_q, h_kv, d, n, 200)
+    side, third = torch.cuda.Stream(), torch.cuda.Stream()
+    chunks = [stream_chunk(g, layers, h_q, h_kv, d, n) for _ in range(3)]
+    torch.cuda.synchronize()
+    run.push(chunks[0], side)
+    run.push(chunks[1], side)
+    held = run.hold(third)                         # (the step's compaction is on the side stream)
+    torch.cuda.synchronize()
+    again = run.hold()
+    torch.cuda.synchronize()
+    assert held.visual == again.visual and all(torch.equal(a, b) for a, b in zip(held.data, again.data))
+    run.push(chunks[2], side)
+    run.restore(held, third)
+    torch.cuda.synchronize()
+    assert run.n_cache == held.rows
+    for l in range(layers):
+        k, v = orc.unpack(held.data[l].cpu().numpy(), held.rows[l])
+        assert np.array_equal(host(run.cache_k(l)), k) and np.array_equal(host(run.cache_v(l)), v)
+    small = HeldMemory([x[:1] for x in held.data], held.rows, held.visual)      # (one KV head instead of two)
+    run.push(chunks[0], side)
+    before = list(run.n_cache)
+    with pytest.raises(ValueError):
+        run.restore(small)
+    assert run.n_cache == before
+    run.close()
+
+
+def test_a_reader_refuses_other_numbers_of_streams():
+    h_q, h_kv, d, n = 2, 1, 64, 3
+    rnd = lambda h: torch.randn(h, n, d, device="cuda").bfloat16()
+    memory = HeldMemory([torch.zeros(om.memory_shape(h_kv, d, 0), dtype=torch.uint8, device="cuda")], [0], [0])
+    rope = om.make_rope(d, [0.5 ** j for j in range(32)])
+    pos = torch.zeros(1, n, dtype=torch.int32, device="cuda")
+    reader = Reader([memory, memory], h_q, h_kv, d, rope, 8)
+    for streams in (0, 1, 3):
+        with pytest.raises(ValueError, match="2 streams"):
+            reader.layer(0, [rnd(h_q)] * streams, [rnd(h_kv)] * streams, [rnd(h_kv)] * streams, [pos] * streams)
+    outs = reader.layer(0, [rnd(h_q)] * 2, [rnd(h_kv)] * 2, [rnd(h_kv)] * 2, [pos] * 2)
+    torch.cuda.synchronize()
+    assert len(outs) == 2 and all(torch.isfinite(o.float()).all() for o in outs)
+    reader.close()
+    for memories in ([], [memory, HeldMemory(memory.data * 2, [0, 0], [0, 0])]):
+        with pytest.raises(ValueError):
+            Reader(memories, h_q, h_kv, d, rope, 8)
