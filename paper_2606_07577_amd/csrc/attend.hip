@@ -693,8 +693,8 @@ __global__ __launch_bounds__(256, 2) void attend_f32_many(AttendArgs<N> a) {
 
 // ---------------------------------------------------------------------------
 // bf16, few rows (single tokens, short questions): 16 NR query rows to a unit.
-// Its key tiles of 128 rows go round the wavefronts, each with sums of its own.  A memory tile goes from HBM to registers and from there to the
-// MFMAs: lane (i, g) = (lane % 16, lane / 16) reads a quarter of K row i of
+// Its key tiles of 128 rows go round the wavefronts, each with sums of its own.
+// A memory tile goes from HBM to registers and from there to the MFMAs: lane (i, g) = (lane % 16, lane / 16) reads a quarter of K row i of
 // eight 16-row sets, and channel i's 32 rows of V block g, 16 bytes each; the
 // sets are chosen (rows 4 T .. 4 T + 3 of each of the four blocks) so that
 // set T's scores in lane (query, g) are those of V's rows 4 T .. of block g.
@@ -1525,6 +1525,32 @@ hipError_t attend_few_rows(Args& a, int cus, void* ws, hipStream_t st) {
   return launch_shares<uint16_t, P, D>(a, ws, 3 * cus, attend_few<D, NR, 1>, attend_few<D, NR, kAll>, st);
 }
 
+// A call whose largest sequence wants the many-row kernel has its sequences of
+// up to `rows` query rows of a head taken out, for a launch of their own before
+// it, if one of them has more keys than any other (its unit would end last) or
+// they have more than 16 key tiles for each compute unit.  us, in one launch and
+// in two, beside a chunk of 512 queries of 28 heads over 4608 keys: 7 tokens
+// over 8292 keys 88 and 69, one over 1100 53 and 64; beside 2048 queries over
+// 6144: 31 tokens over 16484 411 and 240, over 4196 (31 tiles a CU) 214 and
+// 192, 8 over 4196 (8) 163 and 176; beside 200 queries of 16 heads over 4296: 6
+// prompts of 10 over 4173 (6) 30 and 38.
+template <int R, int KT>
+Args take_few(Args& a, int rows, int cus) {
+  Args few = a, many = a;
+  few.n_seqs = many.n_seqs = 0;
+  int64_t longest[2] = {0, 0}, tiles;
+  for (int i = 0; i < a.n_seqs; ++i) {
+    const QuerySeq& s = a.seq[i];
+    const bool is_few = (int64_t)a.group * s.nq <= rows;
+    Args& to = is_few ? few : many;
+    to.seq[to.n_seqs++] = s;
+    longest[is_few] = std::max(longest[is_few], (int64_t)s.nm + s.nt);
+  }
+  count_tiles<R, KT>(few, &tiles);
+  if (longest[1] > longest[0] || tiles > 16 * cus) a = many; else few.n_seqs = 0;
+  return few;
+}
+
 template <int D>
 hipError_t attend(const AttnDims& dm, Args& a, int cus, void* ws, hipStream_t st) {
   int64_t rows = 0, keys = 0;
@@ -1533,6 +1559,11 @@ hipError_t attend(const AttnDims& dm, Args& a, int cus, void* ws, hipStream_t st
     // (us of the few-row and the many-row kernel: 48 rows of 4 heads of width 64 over 4096 keys, 8 sequences, 59 and
     // 61; 84 rows, 4 heads of width 128, one sequence 47 and 32)
     if (rows <= 64) return launch_shares<float, F32<D>, D>(a, ws, 4 * cus, attend_f32<D, 1>, attend_f32<D, kAll>, st);
+    Args few = take_few<F32Many<D>::R, F32Many<D>::KT>(a, 64, cus);
+    if (few.n_seqs > 0) {
+      const hipError_t e = attend<D>(dm, few, cus, ws, st);
+      if (e != hipSuccess) return e;
+    }
     return launch_rounds<float, F32Many<D>, D>(a, ws, cus, 1.0, 0.003, attend_f32_many<D, 1>, attend_f32_many<D, kAll>, st);
   }
   if (rows <= 16) return attend_few_rows<D, 1>(a, cus, ws, st);
@@ -1542,6 +1573,11 @@ hipError_t attend(const AttnDims& dm, Args& a, int cus, void* ws, hipStream_t st
   // (7 tiles a unit) 19 and 26; 448 rows, 8 sequences of 1024 (16) 35 and 32; 700 rows over 8192 (22) 36 and 34.
   count_tiles<32, 128>(a, &keys);
   if (rows <= 96 || keys <= 12 * cus) return attend_few_rows<D, 2>(a, cus, ws, st);
+  Args few = take_few<Many<D>::R, Many<D>::KT>(a, 96, cus);
+  if (few.n_seqs > 0) {
+    const hipError_t e = attend<D>(dm, few, cus, ws, st);
+    if (e != hipSuccess) return e;
+  }
   return launch_rounds<uint16_t, Many<D>, D>(a, ws, cus, 3.0, 0.03, attend_many<D, 1>, attend_many<D, kAll>, st);
 }
 

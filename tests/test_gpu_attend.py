@@ -281,3 +281,18 @@ def test_every_way_of_joining(dtype, h_q, h_kv, d, nq, nm, nt):
         check_by_torch(c.out[:, :nq], c.lse[:, :nq], (o, l, size, reach), d, nm + nt)
         assert (c.out[:, nq:] == 7).all()
     attn.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("chunk,others", [((2600, 0, 2600), [(1, 3000, 5), (9, 40, 0), (0, 0, 5), (200, 0, 300), (1, 0, 2700)]),
+                                          ((700, 0, 2300), [(1, 2200, 3)] * 31), ((2600, 0, 2600), [(1, 100, 5), (3, 0, 7)])])
+def test_chunks_and_tokens_in_one_call(dtype, chunk, others):
+    """A chunk beside tokens with more keys than it, beside many tokens, and beside a few that go with it."""
+    attn = handle(4, 4, 64, dtype)
+    g = torch.Generator(device="cuda").manual_seed(chunk[0])
+    cases = [Case(attn, g, 4, 4, 64, dtype, *s) for s in [*others[:2], chunk, *others[2:]]]
+    attn.omnimem_attend([c.query() for c in cases])
+    torch.cuda.synchronize()
+    for c in cases:
+        c.check(True)
+    attn.close()
