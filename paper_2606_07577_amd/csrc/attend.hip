@@ -366,15 +366,32 @@ __device__ inline void write_rows(const AttendArgs<N>& a, const QuerySeq& s, con
 }
 
 // ---------------------------------------------------------------------------
-// fp32, few rows: 32 query rows to a unit; the four wavefronts take 32 keys
-// each of a tile of 128 in LDS, and join their sums at the end.
+// fp32, few rows: 32 query rows to a unit, whose key tiles of 32 rows go round
+// the four wavefronts, each with sums of its own that are joined at the end.  A
+// tile goes from memory to registers and from there to the MFMAs: lane (i, h) =
+// (lane % 32, lane / 32) reads channels 8 j + 4 h .. of K row i, and of V
+// channel i of every 32 the rows that its weights are of, 8 e + 4 h .. of a
+// memory block's codes (16 bytes have a channel's 32 rows).  The next tile's K
+// is on its way during the weights and V's products, V during K's.  The MFMAs
+// bound a long cache (32 rows at least, of which a token has a head's queries:
+// 8 sequences of 7 rows and 4 heads of width 128 over 4096 tail rows, 134 MB,
+// 48 us, 2.8 TB/s), latency a short one (7 rows over 4096 memory rows 16 us).
+// With two units to a compute unit 27, 48 and 52 us where one and four take 30,
+// 38 and 57 and 28, 57 and 57 (8 sequences: 4 rows of width 64 over 4096 memory
+// rows; 7 of width 128 over 4096 tail rows, and memory rows).
 // ---------------------------------------------------------------------------
 template <int D>
 struct F32 {
-  static constexpr int R = 32, KT = 128, WAVES = 4;
+  static constexpr int R = 32, KT = 32, WAVES = 4;
   static constexpr int ROW = D + 4;                        // padded LDS row
-  static constexpr int LDS = 2 * KT * ROW * 4 + 4 * R * 8 + (int)sizeof(Joint);
+  static constexpr int LDS = 4 * R * ROW * 4 + 4 * R * 8 + (int)sizeof(Joint);
 };
+// Four values of a word of codes: the low or (h) high half.
+__device__ inline floatx4 values4(uint32_t w, int h, uint32_t byte) {
+  const float s = scale_of(byte);
+  const floatx2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w >> (16 * h), s, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w >> (16 * h), s, 1);
+  return floatx4{a[0], a[1], b[0], b[1]};
+}
 
 template <int D, int N>
 __global__ __launch_bounds__(256) void attend_f32(AttendArgs<N> a) {
@@ -383,94 +400,127 @@ __global__ __launch_bounds__(256) void attend_f32(AttendArgs<N> a) {
   constexpr int R = P::R, KT = P::KT, ROW = P::ROW, NCT = D / 32;
   using B = MemBlock<D>;
   extern __shared__ __align__(16) char lds[];
-  float* kt = reinterpret_cast<float*>(lds);
-  float* vt = kt + KT * ROW;
-  float2* ml = reinterpret_cast<float2*>(vt + KT * ROW);   // [4][R]
+  float* ob = reinterpret_cast<float*>(lds);               // [4][R][ROW]
+  float2* ml = reinterpret_cast<float2*>(ob + 4 * R * ROW); // [4][R]
   Joint* joint = reinterpret_cast<Joint*>(ml + 4 * R);
   const Unit x = unit_of<R, KT>(a, blockIdx.x);
   const QuerySeq& s = a.seq[x.s];
   const int lane = threadIdx.x & 63, wave = wave_id(), half = lane >> 5, col = lane & 31;
   const Row row = row_of(a, s, x, x.rt * R + col);
-  const float* q = static_cast<const float*>(s.q) + row.h * elems(s.q_hs, 4) + row.i * elems(s.q_rs, 4);
-  const int64_t kv_rs = elems(s.kv_rs, 4);
-  float qf[D / 2];
+  const float* qp = static_cast<const float*>(s.q) + row.h * elems(s.q_hs, 4) + row.i * elems(s.q_rs, 4);
+  floatx4 q[D / 8];
 #pragma unroll
-  for (int ks = 0; ks < D / 2; ++ks) qf[ks] = row.live ? gload<float>(q + ks * 2 + half) : 0.0f;
+  for (int j = 0; j < D / 8; ++j) q[j] = row.live ? gload<floatx4>(qp + 8 * j + 4 * half) : floatx4{};
+  const uint32_t rsb = s.kv_rs * 16u;                      // row stride in bytes, below 2^24
+  const char* kp = static_cast<const char*>(s.k) + x.g * ((int64_t)s.kv_hs * 16);
+  const char* vp = static_cast<const char*>(s.v) + x.g * ((int64_t)s.kv_hs * 16);
+  const char* data = s.mem + x.g * ((int64_t)s.mem_hs * 16);
+  const int mem_tiles = x.mem_tiles, nt = s.nt, nm = s.nm;
+
+  uint4 kr[D / 8];                                         // a tile's rows, or (the first) codes
+  uint32_t vr[16 * NCT], kb[NCT], vb[NCT];
+  const auto load_k = [&](int t) __attribute__((always_inline)) {
+    if (t < mem_tiles) {
+      const char* block = data + (int64_t)t * B::BYTES;
+#pragma unroll
+      for (int j = 0; j < NCT; ++j) {
+        kr[j] = gload16(block + (uint32_t)(col * (D / 2) + j * 16));
+        kb[j] = gload<uint8_t>(block + (uint32_t)B::k_scale(col, j));
+      }
+    } else {
+      const int key0 = (t - mem_tiles) * KT;
+      const char* tile = kp + (int64_t)key0 * rsb;
+      const uint32_t at = (uint32_t)min(col, nt - key0 - 1) * rsb + half * 16;
+#pragma unroll
+      for (int j = 0; j < D / 8; ++j) kr[j] = gload16(tile + (at + j * 32));
+    }
+    asm volatile("" ::: "memory");
+  };
+  const auto load_v = [&](int t) __attribute__((always_inline)) {
+    if (t < mem_tiles) {
+      const char* block = data + (int64_t)t * B::BYTES;
+#pragma unroll
+      for (int c = 0; c < NCT; ++c) {
+        const uint4 w = gload16(block + (uint32_t)(B::V + (c * 32 + col) * 16));
+        vr[c * 16] = w.x; vr[c * 16 + 1] = w.y; vr[c * 16 + 2] = w.z; vr[c * 16 + 3] = w.w;
+        vb[c] = gload<uint8_t>(block + (uint32_t)B::v_scale(c * 32 + col));
+      }
+    } else {
+      const int key0 = (t - mem_tiles) * KT;
+      const char* tile = vp + (int64_t)key0 * rsb;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const uint32_t at = (uint32_t)min((r >> 2) * 8 + half * 4 + (r & 3), nt - key0 - 1) * rsb + col * 4;
+#pragma unroll
+        for (int c = 0; c < NCT; ++c) vr[c * 16 + r] = gload<uint32_t>(tile + (at + c * 128));
+      }
+    }
+    asm volatile("" ::: "memory");
+  };
 
   floatx16 o[NCT];
 #pragma unroll
   for (int c = 0; c < NCT; ++c) o[c] = floatx16{};
   float m = -INFINITY, l = 0.0f;
-
-  for (int kti = x.k0; kti < x.k1; ++kti) {
-    __syncthreads();
-    const bool in_mem = kti < x.mem_tiles;
-    const int key0 = (in_mem ? kti : kti - x.mem_tiles) * KT;
-    const int keys = min(KT, (in_mem ? s.nm : s.nt) - key0);
-    if (in_mem) {
-      const char* data = s.mem + x.g * ((int64_t)s.mem_hs * 16) + (int64_t)(key0 / kMemRows) * B::BYTES;
-      const int blocks = (keys + kMemRows - 1) / kMemRows;
-      for (int e = threadIdx.x; e < KT * D / 8; e += 256) {
-        const int t = e / (D / 8), c8 = e % (D / 8), b = t / kMemRows;
-        float y[8] = {};
-        if (b < blocks) {
-          const char* blk = data + (int64_t)b * B::BYTES;
-          values8(gload<uint32_t>(blk + (t % kMemRows) * (D / 2) + c8 * 4), gload<uint8_t>(blk + B::k_scale(t % kMemRows, c8 >> 2)), y);
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) kt[t * ROW + c8 * 8 + j] = y[j];
-      }
-      for (int e = threadIdx.x; e < KT * D / 8; e += 256) {
-        const int c = e % D, t8 = e / D, b = t8 / 4;
-        float y[8] = {};
-        if (b < blocks) {
-          const char* blk = data + (int64_t)b * B::BYTES;
-          values8(gload<uint32_t>(blk + B::V + c * 16 + (t8 & 3) * 4), gload<uint8_t>(blk + B::v_scale(c)), y);
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) vt[(t8 * 8 + j) * ROW + c] = y[j];
-      }
-    } else {
-      const float* k = static_cast<const float*>(s.k) + x.g * elems(s.kv_hs, 4) + key0 * kv_rs;
-      const float* v = static_cast<const float*>(s.v) + x.g * elems(s.kv_hs, 4) + key0 * kv_rs;
-      for (int e = threadIdx.x; e < KT * D / 4; e += 256) {
-        const int t = e / (D / 4), c = e % (D / 4) * 4;
-        const uint4 z = make_uint4(0, 0, 0, 0);
-        *reinterpret_cast<uint4*>(kt + t * ROW + c) = t < keys ? gload16(k + t * kv_rs + c) : z;
-        *reinterpret_cast<uint4*>(vt + t * ROW + c) = t < keys ? gload16(v + t * kv_rs + c) : z;
-      }
-    }
-    __syncthreads();
+  const auto step = [&](auto mem, int t) __attribute__((always_inline)) {
     floatx16 sc = floatx16{};
 #pragma unroll
-    for (int ks = 0; ks < D / 2; ++ks) sc = M::mma(kt[(wave * 32 + col) * ROW + ks * 2 + half], qf[ks], sc);
-    const int limit = in_mem ? (row.live ? keys : 0) : row.seen - key0;
+    for (int j = 0; j < D / 8; ++j) {
+      floatx4 k;
+      if constexpr (decltype(mem)::value)
+        k = values4(j % 4 == 0 ? kr[j / 4].x : j % 4 == 1 ? kr[j / 4].y : j % 4 == 2 ? kr[j / 4].z : kr[j / 4].w, half, kb[j / 4]);
+      else
+        k = __builtin_bit_cast(floatx4, kr[j]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sc = M::mma(k[e], q[j][e], sc);
+    }
+    if (t + 4 < x.k1) load_k(t + 4);
+    const int limit = (decltype(mem)::value ? nm - t * KT : row.seen - (t - mem_tiles) * KT) - half * 4;
     float top = -INFINITY;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      sc[r] = wave * 32 + acc_row(r, lane) < limit ? sc[r] * s.scale_log2 : -INFINITY;
+      sc[r] = (r >> 2) * 8 + (r & 3) < limit ? sc[r] * s.scale_log2 : -INFINITY;
       top = fmaxf(top, sc[r]);
     }
     top = max32(top);
-    const float m2 = fmaxf(m, top), ref = m2 == -INFINITY ? 0.0f : m2;
-    const float alpha = exp2_(m - ref);
-    m = m2;
-    float sum = 0.0f;
+    if (__any(top > m + 8.0f)) {                           // (see attend_many)
+      const float m2 = fmaxf(m, top);
+      const float alpha = m2 == -INFINITY ? 1.0f : exp2_(m - m2);
+      m = m2;
+      l *= alpha;
+#pragma unroll
+      for (int c = 0; c < NCT; ++c) o[c] *= alpha;
+    }
+    const float ref = m == -INFINITY ? 0.0f : m;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       sc[r] = exp2_(sc[r] - ref);
-      sum += sc[r];
+      l += sc[r];
     }
-    l = l * alpha + sum;
 #pragma unroll
-    for (int c = 0; c < NCT; ++c) {
-      o[c] *= alpha;
-      // (the keys of accumulator register r of this half)
-      const float* vp = vt + (wave * 32 + half * 4) * ROW + c * 32 + col;
+    for (int e = 0; e < 4; ++e) {
+      floatx4 v[NCT];
 #pragma unroll
-      for (int r = 0; r < 16; ++r) o[c] = M::mma(vp[((r >> 2) * 8 + (r & 3)) * ROW], sc[r], o[c]);
+      for (int c = 0; c < NCT; ++c) {
+        if constexpr (decltype(mem)::value) v[c] = values4(vr[c * 16 + e], half, vb[c]);
+        else
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v[c][i] = __uint_as_float(vr[c * 16 + e * 4 + i]);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int c = 0; c < NCT; ++c) o[c] = M::mma(v[c][i], sc[e * 4 + i], o[c]);
     }
+    if (t + 4 < x.k1) load_v(t + 4);
+  };
+  int t = x.k0 + wave;
+  if (t < x.k1) {
+    load_k(t);
+    load_v(t);
   }
+  for (; t < min(mem_tiles, x.k1); t += 4) step(std::true_type{}, t);
+  for (; t < x.k1; t += 4) step(std::false_type{}, t);
   l += __shfl_xor(l, 32);
 
   // join the four wavefronts
@@ -484,7 +534,6 @@ __global__ __launch_bounds__(256) void attend_f32(AttendArgs<N> a) {
   float total = 0.0f;
 #pragma unroll
   for (int w = 0; w < 4; ++w) total += ml[w * R + col].y * exp2_(ml[w * R + col].x - ref);
-  float* ob = kt;                                  // [4][R][ROW], the tiles are done with
 #pragma unroll
   for (int c = 0; c < NCT; ++c)
 #pragma unroll
@@ -497,8 +546,13 @@ __global__ __launch_bounds__(256) void attend_f32(AttendArgs<N> a) {
 
 // ---------------------------------------------------------------------------
 // fp32, many rows: 128 query rows to a unit, 32 to each wavefront, against key
-// tiles of 64 rows in two LDS stages.  The MFMA's rate bounds it (a quarter of
-// the vector unit's work for each), so a step is in the plain order.
+// tiles of 64 rows (d = 128: 32) in two LDS stages.  The MFMA's rate bounds it:
+// two workgroups to a CU, accumulators in the registers that the vector
+// instructions use (256 of them: with more allowed, the compiler keeps
+// accumulators apart and moves them), and vector instructions between MFMAs.
+// 8 x 1600 queries of 16 heads of width 64 over 8256 rows 3390 us, 127 TFLOP/s
+// of the 154 that a large product reaches; 2800 of 28 heads of width 128 over
+// 8256 2500 us, 131.  With a workgroup to a CU and the moves 3756 and 2857.
 // ---------------------------------------------------------------------------
 template <int D>
 struct F32Many {
@@ -694,10 +748,14 @@ __global__ __launch_bounds__(256, 2) void attend_f32_many(AttendArgs<N> a) {
 // ---------------------------------------------------------------------------
 // bf16, few rows (single tokens, short questions): 16 NR query rows to a unit.
 // Its key tiles of 128 rows go round the wavefronts, each with sums of its own.
-// A memory tile goes from HBM to registers and from there to the MFMAs: lane (i, g) = (lane % 16, lane / 16) reads a quarter of K row i of
-// eight 16-row sets, and channel i's 32 rows of V block g, 16 bytes each; the
-// sets are chosen (rows 4 T .. 4 T + 3 of each of the four blocks) so that
-// set T's scores in lane (query, g) are those of V's rows 4 T .. of block g.
+// A memory tile goes from HBM to registers and from there to the MFMAs: lane
+// (i, g) = (lane % 16, lane / 16) reads a quarter of K row i of eight 16-row
+// sets, and channel i's 32 rows of V block g, 16 bytes each; the sets are chosen
+// (rows 4 T .. 4 T + 3 of each of the four blocks) so that set T's scores in
+// lane (query, g) are those of V's rows 4 T .. of block g.  HBM bounds it on
+// many long caches (32 tokens of 28 heads over up to 16384 rows, 164 MB, 43 us:
+// 3.8 TB/s), latency and the join on one (40256 rows, 22 MB: 9 us and a join of
+// 5) and on short ones (219 rows: 6 us).
 // ---------------------------------------------------------------------------
 template <int D, int NR>
 struct Few {
@@ -1022,7 +1080,9 @@ __device__ inline frag v_frag(const uint16_t* vd, int lane, int i) {   // i-th: 
 }
 
 // Weights of the 16-key steps of a tile from their scores, one value at a time
-// (value e of 32 is of step e / 8).
+// (value e of 32 is of step e / 8).  They are rounded to bf16 for the second
+// product, half a step or 2^-8 of each at most, as its matrix cores have eight
+// times the rate of fp32's; their sum takes them as they are.
 struct Weights {
   uint32_t w[4][4];
   float even;
@@ -1556,9 +1616,10 @@ hipError_t attend(const AttnDims& dm, Args& a, int cus, void* ws, hipStream_t st
   int64_t rows = 0, keys = 0;
   for (int i = 0; i < a.n_seqs; ++i) rows = std::max(rows, (int64_t)a.group * a.seq[i].nq);
   if (dm.dtype == OMNIMEM_F32) {
-    // (us of the few-row and the many-row kernel: 48 rows of 4 heads of width 64 over 4096 keys, 8 sequences, 59 and
-    // 61; 84 rows, 4 heads of width 128, one sequence 47 and 32)
-    if (rows <= 64) return launch_shares<float, F32<D>, D>(a, ws, 4 * cus, attend_f32<D, 1>, attend_f32<D, kAll>, st);
+    // (us of the few-row and the many-row kernel, 4 heads: 64 rows of width 64 over 4096 memory rows 19 and 21, 8
+    // sequences 48 and 54; 96 rows 24 and 21, 62 and 55; 63 rows of width 128 over 4096 tail rows, 8 sequences, 72 and
+    // 89; 84 rows 132 and 90)
+    if (rows <= 64) return launch_shares<float, F32<D>, D>(a, ws, 2 * cus, attend_f32<D, 1>, attend_f32<D, kAll>, st);
     Args few = take_few<F32Many<D>::R, F32Many<D>::KT>(a, 64, cus);
     if (few.n_seqs > 0) {
       const hipError_t e = attend<D>(dm, few, cus, ws, st);
