@@ -27,6 +27,8 @@ __device__ inline int tail_seen(const QuerySeq& s, int causal, int i) {
 template <int KT>
 __host__ __device__ inline int tiles_of(int rows) { return (int)(((int64_t)rows + KT - 1) / KT); }
 
+constexpr int kFewWaves = 4;     // wavefronts to a workgroup of the few-row kernels
+
 // ---------------------------------------------------------------------------
 // Work of a unit.  Within a sequence the KV heads go fastest and the last row
 // tiles, which see the most, come first: a causal tail's long units begin
@@ -52,7 +54,7 @@ __device__ inline int seq_of(const int32_t (&first)[N], int n, int u) {
   const int v = lane < n ? first[lane] : INT32_MAX;
   return uniform(__popcll(__ballot(v <= u)) - 1);
 }
-template <int R, int KT, int N>
+template <int R, int KT, int WAVES, int N>      // WAVES: that go through the key tiles in turn
 __device__ inline Unit unit_of(const AttendArgs<N>& a, int u) {
   Unit x;
   int tile;
@@ -84,8 +86,14 @@ __device__ inline Unit unit_of(const AttendArgs<N>& a, int u) {
   x.mem_tiles = tiles_of<KT>(s.nm);
   const int last = (min((x.rt + 1) * R, x.rows) - 1) / a.group;
   const int tiles = x.mem_tiles + tiles_of<KT>(tail_seen(s, a.causal, last));
-  x.k0 = (int)((int64_t)tiles * x.split / x.splits);
-  x.k1 = (int)((int64_t)tiles * (x.split + 1) / x.splits);
+  if constexpr (WAVES == 1) {
+    x.k0 = (int)((int64_t)tiles * x.split / x.splits);
+    x.k1 = (int)((int64_t)tiles * (x.split + 1) / x.splits);
+  } else {                   // as many for each wavefront
+    const int64_t share = ((tiles + x.splits - 1) / x.splits + WAVES - 1) / WAVES * WAVES;
+    x.k0 = (int)min((int64_t)tiles, share * x.split);
+    x.k1 = (int)min((int64_t)tiles, share * (x.split + 1));
+  }
   return x;
 }
 
@@ -375,10 +383,8 @@ __device__ inline void write_rows(const AttendArgs<N>& a, const QuerySeq& s, con
 // is on its way during the weights and V's products, V during K's.  The MFMAs
 // bound a long cache (32 rows at least, of which a token has a head's queries:
 // 8 sequences of 7 rows and 4 heads of width 128 over 4096 tail rows, 134 MB,
-// 48 us, 2.8 TB/s), latency a short one (7 rows over 4096 memory rows 16 us).
-// With two units to a compute unit 27, 48 and 52 us where one and four take 30,
-// 38 and 57 and 28, 57 and 57 (8 sequences: 4 rows of width 64 over 4096 memory
-// rows; 7 of width 128 over 4096 tail rows, and memory rows).
+// 38 us, 3.6 TB/s; over memory rows 36), latency a short one (7 rows over 4096
+// memory rows 16 us).
 // ---------------------------------------------------------------------------
 template <int D>
 struct F32 {
@@ -403,7 +409,7 @@ __global__ __launch_bounds__(256) void attend_f32(AttendArgs<N> a) {
   float* ob = reinterpret_cast<float*>(lds);               // [4][R][ROW]
   float2* ml = reinterpret_cast<float2*>(ob + 4 * R * ROW); // [4][R]
   Joint* joint = reinterpret_cast<Joint*>(ml + 4 * R);
-  const Unit x = unit_of<R, KT>(a, blockIdx.x);
+  const Unit x = unit_of<R, KT, kFewWaves>(a, blockIdx.x);
   const QuerySeq& s = a.seq[x.s];
   const int lane = threadIdx.x & 63, wave = wave_id(), half = lane >> 5, col = lane & 31;
   const Row row = row_of(a, s, x, x.rt * R + col);
@@ -573,7 +579,7 @@ __global__ __launch_bounds__(256, 2) void attend_f32_many(AttendArgs<N> a) {
   extern __shared__ __align__(16) char lds[];
   float* kbuf = reinterpret_cast<float*>(lds);             // [2][TILE]
   float* vbuf = kbuf + 2 * TILE;
-  const Unit x = unit_of<R, KT>(a, blockIdx.x);
+  const Unit x = unit_of<R, KT, 1>(a, blockIdx.x);
   const QuerySeq& s = a.seq[x.s];
   const int tid = threadIdx.x, lane = tid & 63, wave = wave_id(), half = lane >> 5, col = lane & 31;
   const Row row = row_of(a, s, x, x.rt * R + wave * 32 + col);
@@ -753,9 +759,9 @@ __global__ __launch_bounds__(256, 2) void attend_f32_many(AttendArgs<N> a) {
 // sets, and channel i's 32 rows of V block g, 16 bytes each; the sets are chosen
 // (rows 4 T .. 4 T + 3 of each of the four blocks) so that set T's scores in
 // lane (query, g) are those of V's rows 4 T .. of block g.  HBM bounds it on
-// many long caches (32 tokens of 28 heads over up to 16384 rows, 164 MB, 43 us:
-// 3.8 TB/s), latency and the join on one (40256 rows, 22 MB: 9 us and a join of
-// 5) and on short ones (219 rows: 6 us).
+// many long caches (32 tokens of 28 heads over up to 16384 rows, 164 MB, 39 us:
+// 4.3 TB/s), latency and the join on one (40256 rows, 22 MB: 14 us, 5 of them the
+// join) and on short ones (219 rows: 6 us).
 // ---------------------------------------------------------------------------
 template <int D, int NR>
 struct Few {
@@ -819,7 +825,7 @@ __global__ __launch_bounds__(256, 2) void attend_few(AttendArgs<N> a) {
   using B = MemBlock<D>;
   constexpr int R = P::R, KT = P::KT, WAVES = P::WAVES, NS = D / 32, NC = D / 16, STEPS = P::STEPS, T = 8 / STEPS;
   extern __shared__ __align__(16) char lds[];
-  const Unit x = unit_of<R, KT>(a, blockIdx.x);
+  const Unit x = unit_of<R, KT, kFewWaves>(a, blockIdx.x);
   const QuerySeq& s = a.seq[x.s];
   const int lane = threadIdx.x & 63, wave = wave_id(), g = lane >> 4, i16 = lane & 15;
   Row row[NR];
@@ -1164,7 +1170,7 @@ __global__ __launch_bounds__(512, 2) void attend_many(AttendArgs<N> a) {
   extern __shared__ __align__(16) char lds[];
   uint16_t* kbuf = reinterpret_cast<uint16_t*>(lds);       // [4][TILE]
   uint16_t* vbuf = kbuf + 4 * TILE;
-  const Unit x = unit_of<R, KT>(a, blockIdx.x);
+  const Unit x = unit_of<R, KT, 1>(a, blockIdx.x);
   const QuerySeq& s = a.seq[x.s];
   const int tid = threadIdx.x, lane = tid & 63, wave = wave_id(), half = lane >> 5, col = lane & 31;
   const float scale = fabsf(s.scale_log2);
@@ -1444,32 +1450,61 @@ int64_t count_tiles(Args& a, int64_t* keys) {
   return n;
 }
 
-// Key tiles in shares of about `share`, or as many more as leave about
-// `target` units, or no more partials than the workspace holds.
+// Few rows: key tiles in shares of a multiple of kFewWaves, the same number to
+// each of a workgroup's wavefronts.  A compute unit has its workgroups side by
+// side, so a call takes as long as the fullest one: for each of some k the
+// smallest shares of which a compute unit has at most k, and of those the ones
+// with the least key tiles on the fullest, k - 1 average shares and the largest
+// one, and 6 tiles' time to begin and end each.  us, with these and with shares
+// of the keys over three times the compute units: 32 tokens over 200 to 16384
+// rows 33 and 37, over 16384 50 and 56, 8 over up to 8192 11.5 and 13.4, 100 over
+// up to 8000 73 and 90, 7 prompts of 45 over up to 4096 (width 64) 16 and 20.
+struct Shares {
+  int64_t units = 0, parts = 0, tiles = 0, largest = 0;
+};
 template <int R, int KT>
-bool plan_shares(Args& a, int64_t slots, int64_t share, int64_t target) {
-  int64_t keys;
+Shares set_shares(Args& a, int64_t share) {
+  Shares x;
+  for (int i = 0; i < a.n_seqs; ++i) {
+    QuerySeq& s = a.seq[i];
+    const int64_t t = std::max(tiles_of<KT>(s.nm) + tiles_of<KT>(s.nt), 1), heads = (int64_t)a.h_kv * s.row_tiles;
+    s.splits = (int)((t + share - 1) / share);
+    a.unit0[i] = (int)x.units;
+    s.slot0 = (int)x.parts;
+    x.units += heads * s.splits;
+    if (s.splits > 1) x.parts += heads * s.splits;
+    x.tiles += heads * t;
+    x.largest = std::max(x.largest, (t + s.splits - 1) / s.splits);
+    if (x.units > INT32_MAX) break;
+  }
+  return x;
+}
+template <int R, int KT>
+bool plan_shares(Args& a, int64_t slots, int cus) {
+  int64_t keys, most = 1;
   count_tiles<R, KT>(a, &keys);
   a.whole = 0;
-  for (share = std::max(share, keys / target);; share += 1 + share / 16) {
-    int64_t units = 0, parts = 0;
-    for (int i = 0; i < a.n_seqs; ++i) {
-      QuerySeq& s = a.seq[i];
-      const int64_t t = std::max(tiles_of<KT>(s.nm) + tiles_of<KT>(s.nt), 1);
-      s.splits = (int)((t + share - 1) / share);
-      if (units > INT32_MAX) return false;
-      a.unit0[i] = (int)units;
-      s.slot0 = (int)parts;
-      const int64_t u = (int64_t)a.h_kv * s.row_tiles * s.splits;
-      units += u;
-      if (s.splits > 1) parts += u;
+  for (int i = 0; i < a.n_seqs; ++i) most = std::max(most, (int64_t)tiles_of<KT>(a.seq[i].nm) + tiles_of<KT>(a.seq[i].nt));
+  int64_t best = (most + kFewWaves - 1) / kFewWaves, high = best;   // in kFewWaves tiles: no split
+  double least = 1e30;
+  for (int k : {1, 2, 3, 4, 6, 8}) {
+    int64_t low = 1;
+    if (set_shares<R, KT>(a, high * kFewWaves).units > (int64_t)k * cus) continue;
+    while (low < high) {
+      const int64_t mid = (low + high) / 2;
+      if (set_shares<R, KT>(a, mid * kFewWaves).units <= (int64_t)k * cus) high = mid; else low = mid + 1;
     }
-    if (units > INT32_MAX) return false;
-    if (parts <= slots) {
-      a.units = (int)units;
-      return true;
+    const Shares x = set_shares<R, KT>(a, high * kFewWaves);
+    const double n = (double)((x.units + cus - 1) / cus), cost = (n - 1) * x.tiles / x.units + x.largest + 6 * n;
+    if (x.parts <= slots && cost < least) {
+      least = cost;
+      best = high;
     }
+    if (high == 1) break;
   }
+  const Shares x = set_shares<R, KT>(a, best * kFewWaves);
+  a.units = (int)x.units;
+  return x.units <= INT32_MAX;
 }
 
 // As many whole row tiles as fill the chip a number of times, and the rest in
@@ -1550,10 +1585,11 @@ hipError_t launch(Args& a, void* ws, int64_t joins, int splits, One one, All all
 // of width 128 (4) 13.7 and 15.6.
 constexpr int kJoinBatches = 3;
 template <typename T, typename P, int D, typename One, typename All>
-hipError_t launch_shares(Args& a, void* ws, int64_t target, One one, All all, hipStream_t st) {
+hipError_t launch_shares(Args& a, void* ws, int cus, One one, All all, hipStream_t st) {
   constexpr int64_t slots = partials<P::R, D>();
   static_assert(slots <= kMaxPartials, "a counter to a partial");
-  if (!plan_shares<P::R, P::KT>(a, slots, P::WAVES, target)) return hipErrorInvalidConfiguration;
+  static_assert(P::WAVES == kFewWaves, "shares for the workgroup's wavefronts");
+  if (!plan_shares<P::R, P::KT>(a, slots, cus)) return hipErrorInvalidConfiguration;
   int splits = 1;
   int64_t joins = 0, batches = 0;
   for (int i = 0; i < a.n_seqs; ++i) {
@@ -1582,7 +1618,7 @@ constexpr int kAll = kQueriesPerLaunch;
 template <int D, int NR>
 hipError_t attend_few_rows(Args& a, int cus, void* ws, hipStream_t st) {
   using P = Few<D, NR>;
-  return launch_shares<uint16_t, P, D>(a, ws, 3 * cus, attend_few<D, NR, 1>, attend_few<D, NR, kAll>, st);
+  return launch_shares<uint16_t, P, D>(a, ws, cus, attend_few<D, NR, 1>, attend_few<D, NR, kAll>, st);
 }
 
 // A call whose largest sequence wants the many-row kernel has its sequences of
@@ -1619,7 +1655,7 @@ hipError_t attend(const AttnDims& dm, Args& a, int cus, void* ws, hipStream_t st
     // (us of the few-row and the many-row kernel, 4 heads: 64 rows of width 64 over 4096 memory rows 19 and 21, 8
     // sequences 48 and 54; 96 rows 24 and 21, 62 and 55; 63 rows of width 128 over 4096 tail rows, 8 sequences, 72 and
     // 89; 84 rows 132 and 90)
-    if (rows <= 64) return launch_shares<float, F32<D>, D>(a, ws, 2 * cus, attend_f32<D, 1>, attend_f32<D, kAll>, st);
+    if (rows <= 64) return launch_shares<float, F32<D>, D>(a, ws, cus, attend_f32<D, 1>, attend_f32<D, kAll>, st);
     Args few = take_few<F32Many<D>::R, F32Many<D>::KT>(a, 64, cus);
     if (few.n_seqs > 0) {
       const hipError_t e = attend<D>(dm, few, cus, ws, st);
