@@ -1622,7 +1622,7 @@ hipError_t attend_few_rows(Args& a, int cus, void* ws, hipStream_t st) {
 }
 
 // A call whose largest sequence wants the many-row kernel has its sequences of
-// up to `rows` query rows of a head taken out, for a launch of their own before
+// up to `rows` query rows of a head (which never take it) taken out, for a launch of their own before
 // it, if one of them has more keys than any other (its unit would end last) or
 // they have more than 16 key tiles for each compute unit.  us, in one launch and
 // in two, beside a chunk of 512 queries of 28 heads over 4608 keys: 7 tokens
@@ -1647,16 +1647,25 @@ Args take_few(Args& a, int rows, int cus) {
   return few;
 }
 
+constexpr int kAlwaysFew = 64;   // query rows of a head that never take a many-row kernel
 template <int D>
 hipError_t attend(const AttnDims& dm, Args& a, int cus, void* ws, hipStream_t st) {
-  int64_t rows = 0, keys = 0;
-  for (int i = 0; i < a.n_seqs; ++i) rows = std::max(rows, (int64_t)a.group * a.seq[i].nq);
+  int64_t rows = 0, memory = 0, tail = 0;
+  for (int i = 0; i < a.n_seqs; ++i) {
+    const QuerySeq& s = a.seq[i];
+    const int64_t r = (int64_t)a.group * s.nq, tiles = a.h_kv * ((r + 31) / 32);
+    rows = std::max(rows, r);
+    memory += tiles * tiles_of<128>(s.nm);
+    tail += tiles * tiles_of<128>(s.nt);
+  }
   if (dm.dtype == OMNIMEM_F32) {
-    // (us of the few-row and the many-row kernel, 4 heads: 64 rows of width 64 over 4096 memory rows 19 and 21, 8
-    // sequences 48 and 54; 96 rows 24 and 21, 62 and 55; 63 rows of width 128 over 4096 tail rows, 8 sequences, 72 and
-    // 89; 84 rows 132 and 90)
-    if (rows <= 64) return launch_shares<float, F32<D>, D>(a, ws, cus, attend_f32<D, 1>, attend_f32<D, kAll>, st);
-    Args few = take_few<F32Many<D>::R, F32Many<D>::KT>(a, 64, cus);
+    // The few-row kernel where its tiles of 32 rows hold at most 3/4 as many as the other's of 128, up to 192.  us, it
+    // and the many-row kernel, 4 heads, 8 sequences of 32768 memory rows of width 64: 64 rows 232 and 329, 84 287 and
+    // 330, 112 450 and 330, 168 548 and 644; of 8192 tail rows of width 128: 116 and 170, 181 and 171, 212 and 172, 328
+    // and 314; one of 8192 memory rows of width 128: 27 and 36, 32 and 36, 38 and 37, 47 and 53.
+    if (rows <= 96 || (rows > 128 && rows <= 192))
+      return launch_shares<float, F32<D>, D>(a, ws, cus, attend_f32<D, 1>, attend_f32<D, kAll>, st);
+    Args few = take_few<F32Many<D>::R, F32Many<D>::KT>(a, kAlwaysFew, cus);
     if (few.n_seqs > 0) {
       const hipError_t e = attend<D>(dm, few, cus, ws, st);
       if (e != hipSuccess) return e;
@@ -1664,13 +1673,14 @@ hipError_t attend(const AttnDims& dm, Args& a, int cus, void* ws, hipStream_t st
     return launch_rounds<float, F32Many<D>, D>(a, ws, cus, 1.0, 0.003, attend_f32_many<D, 1>, attend_f32_many<D, kAll>, st);
   }
   if (rows <= 16) return attend_few_rows<D, 1>(a, cus, ws, st);
-  // The few-row kernel up to 96 rows of a head, and further where that leaves at most 12 wavefront tiles (32 rows and
-  // 128 keys) for each compute unit.  us, it and the many-row kernel, 4 heads of width 128: 84 rows, 8 sequences of
-  // 32768 memory rows 94 and 125; 112 rows, 8 sequences of 8192 tail rows 93 and 53; 224 rows over 8192 memory rows
-  // (7 tiles a unit) 19 and 26; 448 rows, 8 sequences of 1024 (16) 35 and 32; 700 rows over 8192 (22) 36 and 34.
-  count_tiles<32, 128>(a, &keys);
-  if (rows <= 96 || keys <= 12 * cus) return attend_few_rows<D, 2>(a, cus, ws, st);
-  Args few = take_few<Many<D>::R, Many<D>::KT>(a, 96, cus);
+  // The few-row kernel up to 64 rows of a head, to 128 over memories (whose codes it reads again for each 32 rows at a
+  // quarter of tail rows' cost), and where that leaves at most 40 tiles (32 rows and 128 memory rows, or 64 tail rows)
+  // to a compute unit.  us, it and the many-row kernel, 4 heads of width 128: 56 rows, 8 sequences of 32768 memory rows
+  // 61 and 120, of 8192 tail rows 37 and 50; 84 rows 83 and 122, 59 and 53 (48 tiles); 112 rows 105 and 125, 60 and 53
+  // (64); 168 rows 137 and 130 (193), 74 and 55 (96); 448 rows over 8192 memory rows 24 and 34 (14), 8 sequences of 1024
+  // tail rows 31 and 33 (28); 700 rows over 8192 33 and 35 (22), over 32768 73 and 65 (88).
+  if (rows <= kAlwaysFew || (rows <= 128 && memory >= tail) || memory + 2 * tail <= 40 * cus) return attend_few_rows<D, 2>(a, cus, ws, st);
+  Args few = take_few<Many<D>::R, Many<D>::KT>(a, kAlwaysFew, cus);
   if (few.n_seqs > 0) {
     const hipError_t e = attend<D>(dm, few, cus, ws, st);
     if (e != hipSuccess) return e;

@@ -296,3 +296,30 @@ def test_chunks_and_tokens_in_one_call(dtype, chunk, others):
     for c in cases:
         c.check(True)
     attn.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_many_tokens_beside_a_chunk_with_more_keys(dtype):
+    attn = handle(4, 4, 64, dtype)
+    g = torch.Generator(device="cuda").manual_seed(5)
+    cases = [Case(attn, g, 4, 4, 64, dtype, *s) for s in [(2600, 0, 2600)] + [(1, 2200, 3)] * 31]
+    attn.omnimem_attend([c.query() for c in cases])
+    torch.cuda.synchronize()
+    for c in cases:
+        c.check(True)
+    attn.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("nq", [17, 24, 25, 32, 33, 47, 48, 49])
+def test_rows_about_the_limits_of_the_few_row_kernels(dtype, nq):
+    """64, 96, 128 and 192 rows of a head, over a memory and over tail rows, in batches that fill the chip."""
+    attn = handle(8, 2, 64, dtype)
+    g = torch.Generator(device="cuda").manual_seed(nq)
+    for nm, nt in ((3000, nq), (0, 3000)):
+        cases = [Case(attn, g, 8, 2, 64, dtype, nq, nm, nt, lse=i == 0) for i in range(9)]
+        attn.omnimem_attend([c.query() for c in cases])
+        torch.cuda.synchronize()
+        for c in cases:
+            c.check(True)
+    attn.close()
