@@ -1622,14 +1622,13 @@ hipError_t attend_few_rows(Args& a, int cus, void* ws, hipStream_t st) {
 }
 
 // A call whose largest sequence wants the many-row kernel has its sequences of
-// up to `rows` query rows of a head (which never take it) taken out, for a launch of their own before
-// it, if one of them has more keys than any other (its unit would end last) or
-// they have more than 16 key tiles for each compute unit.  us, in one launch and
-// in two, beside a chunk of 512 queries of 28 heads over 4608 keys: 7 tokens
-// over 8292 keys 88 and 69, one over 1100 53 and 64; beside 2048 queries over
-// 6144: 31 tokens over 16484 411 and 240, over 4196 (31 tiles a CU) 214 and
-// 192, 8 over 4196 (8) 163 and 176; beside 200 queries of 16 heads over 4296: 6
-// prompts of 10 over 4173 (6) 30 and 38.
+// up to `rows` query rows of a head (which never take it) taken out, for a
+// launch of their own before it, if one of them has more keys than any other
+// (its unit would end last) or they have more than 16 key tiles for each compute
+// unit.  us, in one launch and in two, beside a chunk of 512 queries of 28 heads
+// over 4608 keys: 7 tokens over 8292 keys 88 and 65, one over 1100 54 and 62;
+// beside 2048 queries over 6144: 31 tokens over 16484 411 and 230, over 4196 (31
+// tiles a CU) 214 and 189, 8 over 4196 (8) 164 and 176.
 template <int R, int KT>
 Args take_few(Args& a, int rows, int cus) {
   Args few = a, many = a;
