@@ -12,6 +12,7 @@ import math
 import os
 import typing
 
+import numpy as np
 import torch
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -400,6 +401,15 @@ def array_of(descriptors):
     arr = (type(descriptors[0]) * len(descriptors))(*descriptors)
     arr._layouts = {d._layout for d in descriptors if hasattr(d, "_layout")}
     return arr
+
+
+def columns_of(array):
+    """A numpy structured view of a ctypes array of descriptors: array[i].f is columns["f"][i]."""
+    kind = array._type_
+    dtype = np.dtype({"names": [name for name, _ in kind._fields_],
+                      "formats": ["u8" if t is ctypes.c_void_p else np.dtype(t) for _, t in kind._fields_],
+                      "offsets": [getattr(kind, name).offset for name, _ in kind._fields_], "itemsize": ctypes.sizeof(kind)})
+    return np.frombuffer(array, dtype=dtype)
 
 
 def memory_shape(n_kv_heads, head_dim, rows):

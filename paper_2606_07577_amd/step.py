@@ -6,6 +6,8 @@ owns the output buffers and runs the four stages on a stream.
 """
 from __future__ import annotations
 
+import contextlib
+
 import numpy as np
 import torch
 
@@ -459,50 +461,112 @@ class Reader:
     A model calls layer() for each of its layers with the projections of the
     streams' next tokens (a prompt's, or one each), in order, and next() after
     the last layer.  `capacity`: tail rows of a stream.
+
+    The calls' descriptors are made once; layer() sets what changes.  Where
+    every stream has the same number of tokens it takes the streams' tensors
+    stacked, at a host cost that does not grow with them (lists: some
+    microseconds for each stream).
     """
 
     def __init__(self, memories, h_q, h_kv, d, rope, capacity, dtype="bf16", device="cuda", sm_scale=0.0):
-        self.device = torch.device(device)
         self.tdtype = torch.bfloat16 if dtype == "bf16" else torch.float32
         self.h_q, self.h_kv, self.d, self.cap = h_q, h_kv, d, int(capacity)
         self.memories, self.rope, self.sm_scale = list(memories), rope, float(sm_scale)
         if not self.memories or len({len(m.data) for m in self.memories}) != 1:
             raise ValueError("one memory at least, all of one number of layers")
+        n_layers, streams, elt = len(self.memories[0].data), len(self.memories), self.tdtype.itemsize
         self.attn = om.Attention(h_q, h_kv, d, om.BF16 if dtype == "bf16" else om.F32)
-        n_layers = len(self.memories[0].data)
-        shape = (n_layers, len(self.memories), h_kv, self.cap, d)
-        self.k, self.v = (torch.zeros(shape, device=self.device, dtype=self.tdtype) for _ in range(2))
-        self.tail = [0] * len(self.memories)     # tail rows of each stream
+        shape = (n_layers, streams, h_kv, self.cap, d)
+        self.k, self.v = (torch.zeros(shape, device=device, dtype=self.tdtype) for _ in range(2))
+        self.device = self.k.device
+        self.tail = [0] * streams                # tail rows of each stream
         self._new = None                         # and those that the current tokens add
+        layouts = {om._Layout(h_q, h_kv, d, self.tdtype, self.device.index, rope.n_axes)}
+        self._rows = (om.Projection * streams)()
+        self._rows._layouts = layouts
+        row = self._row = om.columns_of(self._rows)
+        row["q_out_head_stride"], row["q_out_row_stride"] = d, h_q * d
+        row["out_head_stride"], row["out_row_stride"] = self.k.stride(2), d
+        self._queries, self._query = [], []
+        at = np.arange(n_layers * streams, dtype=np.uint64).reshape(n_layers, streams) * np.uint64(h_kv * self.cap * d * elt)
+        self._k_at, self._v_at = at + np.uint64(self.k.data_ptr()), at + np.uint64(self.v.data_ptr())
+        for l in range(n_layers):
+            queries = (om.Query * streams)()
+            queries._layouts = layouts
+            x = om.columns_of(queries)
+            x["q_head_stride"] = x["out_head_stride"] = d
+            x["q_row_stride"] = x["out_row_stride"] = h_q * d
+            x["k"], x["v"] = self._k_at[l], self._v_at[l]
+            x["kv_head_stride"], x["kv_row_stride"], x["sm_scale"] = self.k.stride(2), d, self.sm_scale
+            for b, m in enumerate(self.memories):
+                if m.rows[l]:
+                    om._memory(m.data[l], m.rows[l], self.k[l, b])
+                    if m.data[l].device != self.device:
+                        raise ValueError("the memories must lie on the reader's device")
+                    queries[b].memory, queries[b].memory_head_stride = m.data[l].data_ptr(), m.data[l].stride(0)
+                    queries[b].memory_rows = m.rows[l]
+            self._queries.append(queries)
+            self._query.append(x)
+
+    def _columns(self, what, x, heads, last):
+        """Pointers, strides and sizes of the streams' tensors x [heads, n, last] (pos: [axes, n], `last` None): a list
+        of them, or the tensors stacked."""
+        stacked = isinstance(x, torch.Tensor)
+        dims, dtype = (2, torch.int32) if last is None else (3, self.tdtype)
+        if len(x) != len(self.memories):
+            raise ValueError(f"q, k, v and pos are lists of {len(self.memories)} streams' tensors, or those stacked")
+        for t in (x,) if stacked else x:
+            lead = t.dim() - dims
+            if (lead != int(stacked) or t.dtype != dtype or t.device != self.device or (t.stride(-1) != 1 and t.shape[-1] > 1) or
+                    (t.shape[lead] < heads if last is None else (t.shape[lead], t.shape[-1]) != (heads, last))):
+                raise ValueError(f"{what}: tensors of the reader's device, heads, width and type (positions int32) with "
+                                 "their last axis contiguous")
+        if stacked:
+            count = len(x)
+            ptr = np.uint64(x.data_ptr()) + np.arange(count, dtype=np.uint64) * np.uint64(x.stride(0) * x.element_size())
+            return ptr, x.stride(1), x.stride(2), [x.shape[2]] * count
+        return ([t.data_ptr() for t in x], [t.stride(0) for t in x], [t.stride(1) for t in x], [t.shape[1] for t in x])
 
     def layer(self, l, q, k, v, pos, stream=None):
         """One layer of the streams' next tokens: for each stream b q[b] [H_q,
         n_b, d], k[b] and v[b] [H_kv, n_b, d] as projected, and their positions
         pos[b] int32 [axes, n_b].  Keys and queries are normalised and rotated,
         keys and values go behind the stream's tail, and the queries attend to
-        its memory and tail.  Returns [H_q, n_b, d] for each stream."""
-        new = [x.shape[1] for x in k]
-        if not len(q) == len(k) == len(v) == len(pos) == len(self.memories):
-            raise ValueError(f"q, k, v and pos are lists of {len(self.memories)} streams' tensors")
+        its memory and tail.  Returns [H_q, n_b, d] for each stream.  Each of
+        the four is a list, or the streams' tensors stacked; with q stacked the
+        result is [streams, H_q, n, d]."""
+        qp, qh, qr, new = self._columns("q", q, self.h_q, self.d)
+        kp, kh, kr, nk = self._columns("k", k, self.h_kv, self.d)
+        vp, vh, vr, nv = self._columns("v", v, self.h_kv, self.d)
+        pp, ps, _, np_ = self._columns("pos", pos, self.rope.n_axes, None)
+        if not new == nk == nv == np_:
+            raise ValueError("q, k, v and pos have different numbers of tokens")
+        if np.any(np.not_equal(kh, vh)) or np.any(np.not_equal(kr, vr)):
+            raise ValueError("k and v must share their strides")
         if self._new is not None and new != self._new:
             raise ValueError("every layer takes the same numbers of tokens (next() begins the next ones)")
         if any(t + n > self.cap for t, n in zip(self.tail, new)):
             raise ValueError(f"more than {self.cap} tail rows")
         self._new = new
-        rows, queries, outs, rotated = [], [], [], []   # (rotated: the queries, kept until the calls are queued)
-        with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream()):
-            for b, (t, n) in enumerate(zip(self.tail, new)):
-                q_rot = torch.empty((n, self.h_q, self.d), device=self.device, dtype=self.tdtype).transpose(0, 1)
-                out = torch.empty_like(q_rot)
-                kc, vc, mem = self.k[l, b], self.v[l, b], self.memories[b]
-                rows.append(om.make_projection(q[b], k[b], v[b], pos[b], q_rot, kc[:, t: t + n], vc[:, t: t + n]))
-                queries.append(om.make_query(q_rot, out, kc[:, : t + n], vc[:, : t + n], mem.data[l] if mem.rows[l] else None,
-                                             mem.rows[l], self.sm_scale))
-                outs.append(out)
-                rotated.append(q_rot)
-        self.attn.omnimem_rotate(self.rope, rows, stream)
-        self.attn.omnimem_attend(queries, True, stream)
-        return outs
+        total, elt = sum(new), self.tdtype.itemsize
+        with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
+            rotated, out = (torch.empty((total, self.h_q, self.d), device=self.device, dtype=self.tdtype) for _ in range(2))
+        first = np.cumsum([0] + new)
+        at = first[:-1].astype(np.uint64) * np.uint64(self.h_q * self.d * elt)
+        tail = np.array(self.tail, dtype=np.uint64) * np.uint64(self.d * elt)
+        row, query = self._row, self._query[l]
+        row["q"], row["q_head_stride"], row["q_row_stride"] = qp, qh, qr
+        row["k"], row["v"], row["kv_head_stride"], row["kv_row_stride"] = kp, vp, kh, kr
+        row["pos"], row["pos_stride"], row["n_rows"] = pp, ps, new
+        row["q_out"] = query["q"] = at + np.uint64(rotated.data_ptr())
+        row["k_out"], row["v_out"] = self._k_at[l] + tail, self._v_at[l] + tail
+        query["out"], query["n_queries"] = at + np.uint64(out.data_ptr()), new
+        query["n_tail"] = np.add(self.tail, new)
+        self.attn.omnimem_rotate(self.rope, self._rows, stream)
+        self.attn.omnimem_attend(self._queries[l], True, stream)
+        if isinstance(q, torch.Tensor):
+            return out.view(len(new), -1, self.h_q, self.d).transpose(1, 2) if total else out.new_empty((len(new), self.h_q, 0, self.d))
+        return [out[i: j].transpose(0, 1) for i, j in zip(first[:-1], first[1:])]
 
     def next(self):
         """The tokens of the last layer() calls are part of the tails."""

@@ -262,3 +262,43 @@ def test_a_reader_refuses_other_numbers_of_streams():
     for memories in ([], [memory, HeldMemory(memory.data * 2, [0, 0], [0, 0])]):
         with pytest.raises(ValueError):
             Reader(memories, h_q, h_kv, d, rope, 8)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_reader_takes_the_streams_stacked(dtype):
+    """A fused projection's heads of all streams, stacked, give what the streams' tensors in lists give, bit by bit."""
+    h_q, h_kv, d, streams, layers, td = 4, 2, 64, 3, 2, torch.bfloat16 if dtype == "bf16" else torch.float32
+    g = torch.Generator(device="cuda").manual_seed(11)
+    attn = om.Attention(h_q, h_kv, d, om.BF16 if dtype == "bf16" else om.F32)
+    memories = []
+    for rows in ([100, 0], [33, 64], [0, 7]):
+        data = [torch.zeros(om.memory_shape(h_kv, d, n), dtype=torch.uint8, device="cuda") for n in rows]
+        kv = [torch.randn(2, h_kv, n, d, generator=g, device="cuda").to(td) for n in rows]
+        attn.omnimem_pack([om.make_held(x[0], x[1], m) for x, m, n in zip(kv, data, rows) if n])
+        torch.cuda.synchronize()
+        memories.append(HeldMemory(data, rows, rows))
+    rope = om.make_rope(d, [0.7 ** j for j in range(16)], axis=[j % 2 for j in range(16)])
+    lists, stacked = (Reader(memories, h_q, h_kv, d, rope, 16, dtype=dtype) for _ in range(2))
+    side = torch.cuda.Stream()
+    for n in (5, 1, 1):
+        for l in range(layers):
+            x = torch.randn(streams, n, h_q + 2 * h_kv, d, generator=g, device="cuda").to(td).transpose(1, 2)
+            q, k, v = x[:, :h_q], x[:, h_q: h_q + h_kv], x[:, h_q + h_kv:]
+            pos = torch.randint(0, 900, (streams, 2, n), generator=g, device="cuda").to(torch.int32)
+            torch.cuda.synchronize()
+            want = lists.layer(l, list(q), list(k), list(v), list(pos))
+            got = stacked.layer(l, q, k, v, pos, side)
+            torch.cuda.synchronize()
+            assert got.shape == (streams, h_q, n, d) and all(torch.equal(a, b) for a, b in zip(want, got))
+        lists.next()
+        stacked.next()
+    assert torch.equal(lists.k, stacked.k) and torch.equal(lists.v, stacked.v) and lists.tail == stacked.tail == [7] * 3
+    good = dict(q=q, k=k, v=v, pos=pos)
+    for change in (dict(q=q[:2]), dict(q=q[:, :3]), dict(q=q.double()), dict(q=q[0]), dict(k=k.cpu()), dict(v=v[..., :32]),
+                   dict(pos=pos[:, :1]), dict(pos=pos.long()), dict(q=torch.cat([q, q], 2)), dict(v=v.contiguous()),
+                   dict(q=q.transpose(2, 3).contiguous().transpose(2, 3).expand(-1, -1, 5, -1))):
+        with pytest.raises(ValueError):
+            stacked.layer(0, **{**good, **change})
+    lists.close()
+    stacked.close()
+    attn.close()
