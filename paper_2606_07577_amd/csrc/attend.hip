@@ -1658,11 +1658,12 @@ hipError_t attend(const AttnDims& dm, Args& a, int cus, void* ws, hipStream_t st
     tail += tiles * tiles_of<128>(s.nt);
   }
   if (dm.dtype == OMNIMEM_F32) {
-    // The few-row kernel where its tiles of 32 rows hold at most 3/4 as many as the other's of 128, up to 192.  us, it
-    // and the many-row kernel, 4 heads, 8 sequences of 32768 memory rows of width 64: 64 rows 232 and 329, 84 287 and
-    // 330, 112 450 and 330, 168 548 and 644; of 8192 tail rows of width 128: 116 and 170, 181 and 171, 212 and 172, 328
-    // and 314; one of 8192 memory rows of width 128: 27 and 36, 32 and 36, 38 and 37, 47 and 53.
-    if (rows <= 96 || (rows > 128 && rows <= 192))
+    // The few-row kernel up to 96 rows, to 192 over memories if the other's tiles of 128 would have a half more rows, and
+    // where its tiles (32 rows and 128 keys) are at most 3 to a compute unit.  us, it and the many-row kernel, 4 heads,
+    // 8 sequences of 32768 memory rows of width 64: 64 rows 232 and 329, 84 287 and 330, 112 450 and 330, 168 548 and 644;
+    // of 8192 tail rows of width 128: 116 and 170, 181 and 171, 212 and 172, 328 and 314; one of 1500 tail rows of width
+    // 64: 320 rows 17 and 23 (2 tiles), 500 19 and 22 (3), 1332 34 and 36 (8); of width 128: 25 and 28, 30 and 31, 65 and 57.
+    if (rows <= 96 || (rows > 128 && rows <= 192 && memory >= tail) || memory + tail <= 3 * cus)
       return launch_shares<float, F32<D>, D>(a, ws, cus, attend_f32<D, 1>, attend_f32<D, kAll>, st);
     Args few = take_few<F32Many<D>::R, F32Many<D>::KT>(a, kAlwaysFew, cus);
     if (few.n_seqs > 0) {
