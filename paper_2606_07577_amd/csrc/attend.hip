@@ -490,9 +490,8 @@ __global__ __launch_bounds__(256) void attend_f32(AttendArgs<N> a) {
     }
     top = max32(top);
     if (__any(top > m + 8.0f)) {                           // (see attend_many)
-      const float m2 = fmaxf(m, top);
-      const float alpha = m2 == -INFINITY ? 1.0f : exp2_(m - m2);
-      m = m2;
+      const float alpha = top > m + 8.0f ? exp2_(m - top) : 1.0f;
+      m = top > m + 8.0f ? top : m;
       l *= alpha;
 #pragma unroll
       for (int c = 0; c < NCT; ++c) o[c] *= alpha;
@@ -678,9 +677,8 @@ __global__ __launch_bounds__(256, 2) void attend_f32_many(AttendArgs<N> a) {
     const auto reference = [&](float top) __attribute__((always_inline)) {
       top = max32(top);
       if (__any(top > m + 8.0f)) {                           // (see attend_many)
-        const float m2 = fmaxf(m, top);
-        const float alpha = m2 == -INFINITY ? 1.0f : exp2_(m - m2);
-        m = m2;
+        const float alpha = top > m + 8.0f ? exp2_(m - top) : 1.0f;
+        m = top > m + 8.0f ? top : m;
         l *= alpha;
 #pragma unroll
         for (int c = 0; c < NCT; ++c) o[c] *= alpha;
@@ -1257,11 +1255,11 @@ __global__ __launch_bounds__(512, 2) void attend_many(AttendArgs<N> a) {
   };
   const auto raise = [&](float top) __attribute__((always_inline)) {                      // largest raw score of the tile to come
     top = max32(top) * scale;
-    // The sums keep their reference until a score passes it by 8: weights stay below 2^8, and few tiles scale O.
+    // A row's sums keep their reference until one of its scores passes it by 8: weights stay below 2^8, few tiles scale
+    // O, and what a wavefront's other rows see has no part in it.
     if (__any(top > m + 8.0f)) {
-      const float m2 = fmaxf(m, top);
-      const float alpha = m2 == -INFINITY ? 1.0f : exp2_(m - m2);
-      m = m2;
+      const float alpha = top > m + 8.0f ? exp2_(m - top) : 1.0f;
+      m = top > m + 8.0f ? top : m;
       l *= alpha;
 #pragma unroll
       for (int c = 0; c < NCT; ++c) o[c] *= alpha;

@@ -323,3 +323,78 @@ def test_rows_about_the_limits_of_the_few_row_kernels(dtype, nq):
         for c in cases:
             c.check(True)
     attn.close()
+
+
+def chunk_beside(g, h_q, h_kv, d, dtype, n=2600):
+    """A chunk of so much work that its call takes the kernels of many rows for all of its sequences (those of few rows
+    too, as they have fewer keys)."""
+    td = TORCH[dtype]
+    q = torch.randn(h_q, n, d, generator=g, device="cuda").to(td)
+    k, v = (torch.randn(h_kv, n, d, generator=g, device="cuda").to(td) for _ in range(2))
+    out = torch.empty_like(q)
+    return om.make_query(q, out, k, v), (q, k, v, out)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("h_q,h_kv,d", [(6, 2, 64), (14, 2, 128)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_small_sequences_in_the_kernels_of_chunks(dtype, h_q, h_kv, d, causal):
+    attn = handle(h_q, h_kv, d, dtype)
+    g = torch.Generator(device="cuda").manual_seed(d)
+    chunk, keep = chunk_beside(g, h_q, h_kv, d, dtype)
+    for scale in (None, -0.3):
+        cases = [Case(attn, g, h_q, h_kv, d, dtype, *s, scale=scale) for s in SIZES + [(0, 5, 5), (4, 0, 0), (100, 1200, 7), (33, 1000, 1300)]]
+        attn.omnimem_attend([chunk] + [c.query() for c in cases], causal)
+        torch.cuda.synchronize()
+        for c in cases:
+            c.check(causal)
+    attn.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), float("-inf")])
+def test_rows_that_are_not_seen_in_the_kernels_of_chunks(dtype, value):
+    """As above for few rows: queries before the last keys' infinities and NaN are as without them."""
+    attn = handle(6, 2, 64, dtype)
+    g = torch.Generator(device="cuda").manual_seed(8)
+    chunk, keep = chunk_beside(g, 6, 2, 64, dtype)
+    for nq, nm, nt in ((60, 100, 130), (200, 0, 333), (300, 70, 300), (3, 300, 200)):
+        seed = lambda: torch.Generator(device="cuda").manual_seed(nq)
+        c, clean = (Case(attn, seed(), 6, 2, 64, dtype, nq, nm, nt) for _ in range(2))
+        at = nt - nq // 2 - 1
+        c.v[0, at, 5:9] = value
+        c.k[1, at, 0] = value
+        attn.omnimem_attend([chunk, c.query()])
+        attn.omnimem_attend([chunk, clean.query()])
+        torch.cuda.synchronize()
+        before = nq - (nt - at)
+        reach = float((clean.q.float().abs().sum(-1).amax() * torch.cat([clean.k[:, :nt].float().flatten(),
+                      torch.tensor(clean.held[0], device="cuda").float().flatten()]).abs().amax()) * c.scale)
+        near = 2 * (2 * (64 + 6) * U * reach + 2 * (nm + nt + 8) * U) + (3 * 2.0 ** -8 if dtype == "bf16" else 0.0)
+        size = torch.cat([clean.v[:, :nt].float().flatten(), torch.tensor(clean.held[1], device="cuda").float().flatten()]).abs().amax()
+        assert ((c.out[:, :before].float() - clean.out[:, :before].float()).abs() <= near * size).all()
+        assert torch.equal(c.lse[:, :before], clean.lse[:, :before])
+        assert (~torch.isfinite(c.out[:3, before: nq, 5:9])).all()
+        assert ((c.out[:3, before: nq, 9:].float() - clean.out[:3, before: nq, 9:].float()).abs() <= near * size).all()
+    c = Case(attn, g, 6, 2, 64, dtype, 100, 0, 100)            # products that are all -inf
+    c.q.fill_(1.0)
+    c.k[:, :100] = 0.0
+    c.k[:, :100, 0] = float("-inf")
+    attn.omnimem_attend([chunk, c.query()])
+    torch.cuda.synchronize()
+    assert (c.out[:, :100] == 0).all() and torch.isneginf(c.lse[:, :100]).all()
+    attn.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_chunks_over_memories(dtype, d):
+    """Two chunks of odd lengths over memories that end inside a block and a tile, keys split over workgroups."""
+    attn = handle(4, 4, d, dtype)
+    g = torch.Generator(device="cuda").manual_seed(d)
+    cases = [Case(attn, g, 4, 4, d, dtype, *s) for s in [(2101, 2001, 2177), (333, 1999, 333)]]
+    attn.omnimem_attend([c.query() for c in cases])
+    torch.cuda.synchronize()
+    for c in cases:
+        c.check(True)
+    attn.close()
