@@ -398,3 +398,25 @@ def test_chunks_over_memories(dtype, d):
     for c in cases:
         c.check(True)
     attn.close()
+
+
+@pytest.mark.parametrize("dtype,nq", [("bf16", 1), ("bf16", 130), ("f32", 1), ("f32", 120)])
+def test_a_memory_past_32_bits_of_bytes(dtype, nq):
+    """2^26 + 5 rows of zeros, but for ones in the values of the last 37: every weight is 1, so out is 37 of the rows'
+    number and lse its logarithm.  Sums of ones are exact but for the join's: a rounding for each of up to 2048 shares."""
+    rows, d = (1 << 26) + 5, 64
+    attn = handle(1, 1, d, dtype)
+    data = torch.zeros(om.memory_shape(1, d, rows), dtype=torch.uint8, device="cuda")
+    assert data.numel() > 1 << 32
+    data[0, -2:, 16 * d: 32 * d] = 0x22                         # V codes of 1 ...
+    last = data[0, -1, 16 * d: 32 * d].view(d, 16)
+    last[:, 2], last[:, 3:] = 0x02, 0                           # ... in the last block's first five rows
+    data[0, -2:, 33 * d:] = 127                                 # their scale, 2^0
+    q = torch.randn(1, nq, d, device="cuda").to(TORCH[dtype])
+    out, lse = torch.zeros_like(q), torch.zeros(1, nq, device="cuda")
+    attn.omnimem_attend([om.make_query(q, out, memory=data, memory_rows=rows, lse=lse)])
+    torch.cuda.synchronize()
+    join = 2048 * U + 8 * U
+    assert (np.abs(host(out) * rows / 37 - 1) <= join + (2.0 ** -8 if dtype == "bf16" else 0)).all()
+    assert (np.abs(host(lse) - np.log(rows)) <= join + 2 * U * np.log(rows)).all()
+    attn.close()
