@@ -124,7 +124,8 @@ struct QuerySeq {
 // the same keys, and share them), in tiles of R rows; row tiles are numbered
 // over sequences, KV heads and rows.  A row tile's keys come in key tiles,
 // the memory's and then the tail's.  A unit (one workgroup) takes a row tile
-// and all its keys, or one of `splits` equal shares of them; then each writes
+// and all its keys, or one of `splits` equal shares of them (few rows: of whole
+// turns of its wavefronts, the last with what is left); then each writes
 // a partial result (sums against its own maximum) and the join puts them
 // together, in the order of the keys.  The first `whole` row tiles are not
 // split (with whole > 0 all others are by the same number).
