@@ -10,6 +10,7 @@
 
 #include "../../include/omnimem.h"
 #include "attn.h"
+#include "chunk_steps.h"
 
 namespace omnimem {
 namespace {
@@ -1267,28 +1268,14 @@ __global__ __launch_bounds__(512, 2) void attend_many(AttendArgs<N> a) {
   };
 
   if (x.k0 < x.k1) {
-    // Stage of tile t: (t - k0) & 3.  Step t takes K of tile t + 1 and V of tile t, and fetches K of tile t + 3 and V
-    // of tile t + 2; a barrier every second step lies between a fetch and the first step that takes it, and between
-    // the last step that takes a stage and the next fetch into it.
-    const int k0 = x.k0, k1 = x.k1;
-#pragma unroll
-    for (int i = 0; i < 3; ++i) {
-      if (k0 + i < k1) {
-        fetch_k(k0 + i, i);
-        if (i < 2) fetch_v(k0 + i, i);
-        store_k(k0 + i, i);
-        if (i < 2) store_v(k0 + i, i);
-      }
-    }
-    dma_wait();
-    __syncthreads();
     floatx16 s0[2], s1[2];
-    {  // scores of the first tile
+    const auto first = [&](int stage) __attribute__((always_inline)) {       // scores of the first tile
+      const uint16_t* kd = kbuf + stage * TILE;
       s0[0] = s0[1] = floatx16{};
 #pragma unroll
       for (int i = 0; i < 2 * NKS; ++i)
-        s0[i / NKS] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_frag<D>(kbuf, lane, i), q[i % NKS], s0[i / NKS], 0, 0, 0);
-      const int mine = limit_of(k0) - half * 4;
+        s0[i / NKS] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_frag<D>(kd, lane, i), q[i % NKS], s0[i / NKS], 0, 0, 0);
+      const int mine = limit_of(x.k0) - half * 4;
       float top = -INFINITY;
 #pragma unroll
       for (int b = 0; b < 2; ++b)
@@ -1298,36 +1285,24 @@ __global__ __launch_bounds__(512, 2) void attend_many(AttendArgs<N> a) {
           top = fmaxf(top, s0[b][r]);
         }
       raise(top);
-    }
-    const auto step = [&](auto mem, int t, floatx16 (&sc)[2], floatx16 (&next)[2]) __attribute__((always_inline)) {
-      const int i = t - k0;
-      if (t + 3 < k1) fetch_k(t + 3, (i + 3) & 3);
-      if (t + 2 < k1) fetch_v(t + 2, (i + 2) & 3);
+    };
+    const auto step = [&](auto mem, auto swapped, int t, int kst, int vst) __attribute__((always_inline)) {
+      floatx16(&sc)[2] = decltype(swapped)::value ? s1 : s0;
+      floatx16(&next)[2] = decltype(swapped)::value ? s0 : s1;
       const int limit = limit_of(t + 1);
-      const float top = many_step<D, decltype(mem)::value>(kbuf + ((i + 1) & 3) * TILE, vbuf + (i & 3) * TILE, lane, q, sc, next, o, l, m,
-                                                           scale, limit, __any(limit < KT));
-      if (t + 1 < k1) raise(top);
-      if (t + 3 < k1) store_k(t + 3, (i + 3) & 3);
-      if (t + 2 < k1) store_v(t + 2, (i + 2) & 3);
-      if (i & 1) {
-        dma_wait();
-        __syncthreads();
-      }
+      const float top = many_step<D, decltype(mem)::value>(kbuf + kst * TILE, vbuf + vst * TILE, lane, q, sc, next, o, l, m, scale,
+                                                           limit, __any(limit < KT));
+      if (t + 1 < x.k1) raise(top);
     };
-    const auto steps = [&](auto mem, int t, int end) __attribute__((always_inline)) {     // (two at a time: scores stay where they are)
-      for (; t + 1 < end; t += 2) {
-        step(mem, t, s0, s1);
-        step(mem, t + 1, s1, s0);
-      }
-      if (t < end) {
-        step(mem, t, s0, s1);
-        s0[0] = s1[0];
-        s0[1] = s1[1];
-      }
+    const auto keep = [&]() __attribute__((always_inline)) {
+      s0[0] = s1[0];
+      s0[1] = s1[1];
     };
-    const int mid = min(max(mem_tiles, k0), k1);
-    steps(std::true_type{}, k0, mid);
-    steps(std::false_type{}, mid, k1);
+    const auto barrier = []() __attribute__((always_inline)) {
+      dma_wait();
+      __syncthreads();
+    };
+    chunk_steps(x.k0, x.k1, min(max(mem_tiles, x.k0), x.k1), fetch_k, fetch_v, store_k, store_v, first, step, keep, barrier);
   }
   l += __shfl_xor(l, 32);
   write_rows<uint16_t, D, R>(a, s, x, row, wave * 32 + col, half, o, m, l);
