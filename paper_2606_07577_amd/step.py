@@ -479,6 +479,8 @@ class Reader:
         shape = (n_layers, streams, h_kv, self.cap, d)
         self.k, self.v = (torch.zeros(shape, device=device, dtype=self.tdtype) for _ in range(2))
         self.device = self.k.device
+        # (calls come on streams that do not wait for this one, and into captures, which may not wait for it)
+        torch.cuda.current_stream(self.device).synchronize()
         self.tail = [0] * streams                # tail rows of each stream
         self._new = None                         # and those that the current tokens add
         layouts = {om._Layout(h_q, h_kv, d, self.tdtype, self.device.index, rope.n_axes)}

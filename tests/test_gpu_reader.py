@@ -302,3 +302,30 @@ def test_a_reader_takes_the_streams_stacked(dtype):
     lists.close()
     stacked.close()
     attn.close()
+
+
+def test_a_readers_first_layer_on_another_stream(monkeypatch):
+    """What the constructor fills is filled before a call on any stream, whatever its own stream has to do before."""
+    class Slow(om.Attention):
+        def __init__(self, *args):
+            super().__init__(*args)
+            torch.cuda._sleep(20_000_000)          # (what follows on the constructor's stream comes late)
+
+    h_q, h_kv, d, n = 4, 2, 64, 6
+    g = torch.Generator(device="cuda").manual_seed(12)
+    rnd = lambda h: torch.randn(h, n, d, generator=g, device="cuda").bfloat16()
+    memory = HeldMemory([torch.zeros(om.memory_shape(h_kv, d, 0), dtype=torch.uint8, device="cuda")], [0], [0])
+    rope = om.make_rope(d, [0.5 ** j for j in range(32)])
+    pos, q, k, v = torch.arange(n, dtype=torch.int32, device="cuda")[None], rnd(h_q), rnd(h_kv), rnd(h_kv)
+    plain = Reader([memory], h_q, h_kv, d, rope, 8)
+    [want] = plain.layer(0, [q], [k], [v], [pos])
+    torch.cuda.synchronize()
+    monkeypatch.setattr(om, "Attention", Slow)
+    side = torch.cuda.Stream()
+    late = Reader([memory], h_q, h_kv, d, rope, 8)
+    [got] = late.layer(0, [q], [k], [v], [pos], side)
+    torch.cuda.synchronize()
+    assert torch.equal(got, want) and torch.equal(late.k, plain.k) and torch.equal(late.v, plain.v)
+    assert late.v[0, 0, :, :n].abs().sum() > 0
+    plain.close()
+    late.close()
