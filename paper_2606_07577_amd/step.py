@@ -160,7 +160,8 @@ class StreamRunner:
     set: it copies the budgets back after the allocation stage and waits for
     that copy only, so the compaction of one step overlaps the host's
     preparation of the next.  The descriptors are ctypes arrays built once;
-    a step only updates the fields that change.
+    a step only updates the fields that change.  Calls may come on different
+    streams: each waits for the work on the caches that came before it.
 
     In place, kept audio rows that land behind their own row are staged in
     the context's reserve of `stage_rows` rows per (layer, KV head); there
@@ -215,27 +216,47 @@ class StreamRunner:
         self._chunks = (om.Chunk * n_layers)()
         self._budget_ready = torch.cuda.Event()
         self._pending, self._pending_stream = False, None   # a pushed step whose budgets are unread
+        self._last = torch.cuda.current_stream(dev)   # the stream of the last work on the caches
         self.timing = timing       # per step: events before the append, before score, after select_compact
         self.events = []
 
+    # order on the device ---------------------------------------------------
+    def _behind(self, stream):
+        """The stream (default: the current one) for work on the caches, made
+        to wait for what came before on another one: steps, hold() and
+        restore(), and what the current stream did with the caches' views."""
+        stream = stream if stream is not None else torch.cuda.current_stream()
+        if self._last != stream:
+            stream.wait_stream(self._last)
+        self._last = stream
+        return stream
+
+    def _settle(self):
+        """The caches' sizes are known, their rows ordered for the current
+        stream (not into a capture, which may not wait for work outside it)."""
+        self.finish()
+        if not torch.cuda.is_current_stream_capturing():
+            self._behind(None)
+
     # buffers ------------------------------------------------------------
     def cache_k(self, l):
-        """Device view of layer l's kept keys [H_kv, n_cache, d]."""
-        self.finish()
+        """Device view of layer l's kept keys [H_kv, n_cache, d], for the
+        current stream."""
+        self._settle()
         return self.kbuf[self.cur][l][:, : self.n_cache[l]]
 
     def cache_v(self, l):
-        self.finish()
+        self._settle()
         return self.vbuf[self.cur][l][:, : self.n_cache[l]]
 
     def cache_modality(self, l):
-        self.finish()
+        self._settle()
         return self.mbuf[self.cur][l][: self.n_cache[l]]
 
     def set_cache(self, l, k, v, m_v, m_a):
         """Replace layer l's retained cache: k, v [H_kv, m_v + m_a, d] (host or
         device), visual rows first."""
-        self.finish()
+        self._settle()
         m = int(m_v) + int(m_a)
         if m > self.cache_cap:
             raise ValueError(f"cache of {m} rows exceeds the capacity {self.cache_cap}")
@@ -252,7 +273,7 @@ class StreamRunner:
         are read from (see Reader), a quarter of the cache's bytes to keep
         until the stream goes on (see restore)."""
         budgets = self.finish()
-        with torch.cuda.stream(self._behind_step(stream)):
+        with torch.cuda.stream(self._attention_stream(stream)):
             if budgets is None:
                 budgets = self._held_budgets()
             data = [torch.empty(om.memory_shape(self.h_kv, self.d, n), dtype=torch.uint8, device=self.device)
@@ -265,21 +286,18 @@ class StreamRunner:
         self.finish()
         if len(held.rows) != self.L or max(held.rows) > self.cache_cap:
             raise ValueError("the memory has another number of layers, or more rows than the caches hold")
-        with torch.cuda.stream(self._behind_step(stream)):
+        with torch.cuda.stream(self._attention_stream(stream)):
             self.attn.omnimem_unpack(self._held(held.data, held.rows))
             for mod, n, visual in zip(self.mbuf[self.cur], held.rows, held.visual):
                 mod[:visual] = 0
                 mod[visual:n] = 1
         self.n_cache = list(held.rows)
 
-    def _behind_step(self, stream):
-        """The stream (default: the current one) for work on the caches, made to wait for the last step's."""
-        stream = stream if stream is not None else torch.cuda.current_stream()
-        if self._pending_stream is not None and self._pending_stream != stream:
-            stream.wait_stream(self._pending_stream)
+    def _attention_stream(self, stream):
+        """The stream for hold() and restore(), with their handle made."""
         if self.attn is None:
             self.attn = om.Attention(self.h_q, self.h_kv, self.d, om.BF16 if self.tdtype == torch.bfloat16 else om.F32)
-        return stream
+        return self._behind(stream)
 
     def _held(self, data, rows):
         return [om.make_held(self.kbuf[self.cur][l][:, :n], self.vbuf[self.cur][l][:, :n], data[l]) for l, n in enumerate(rows)]
@@ -338,7 +356,7 @@ class StreamRunner:
         None at once: the step's budgets are read by the next push (after it
         has described its chunk, so the host's work overlaps the GPU's) or
         by finish()."""
-        stream = stream if stream is not None else torch.cuda.current_stream()
+        stream = self._behind(stream)
         chunk = self._on_device(chunk)
         cur = self.cur if self.in_place or not self._pending else 1 - self.cur
         self._describe(chunk, [ch["q"] for ch in chunk], cur)
@@ -435,7 +453,7 @@ class StreamRunner:
     def freeze_budgets(self, stream=None):
         """Layer budgets from the steps calibrated so far; later steps split them."""
         self.finish()
-        self.ctx.omnimem_calibration_budgets(self.total_budget, self.layer_budgets, stream)
+        self.ctx.omnimem_calibration_budgets(self.total_budget, self.layer_budgets, self._behind(stream))
         self.calibrating = False
         self.fixed = True
 

@@ -329,3 +329,73 @@ def test_a_readers_first_layer_on_another_stream(monkeypatch):
     assert late.v[0, 0, :, :n].abs().sum() > 0
     plain.close()
     late.close()
+
+
+def test_steps_behind_held_and_restored_caches_on_another_stream():
+    """No synchronization between hold() or restore() on one stream, late as they are, and the step on another: budgets,
+    caches and memories are those of one stream."""
+    layers, h_q, h_kv, d, n = 2, 4, 2, 64, 160
+    g = torch.Generator(device="cuda").manual_seed(13)
+    chunks = [stream_chunk(g, layers, h_q, h_kv, d, n) for _ in range(6)]
+    side, third = torch.cuda.Stream(), torch.cuda.Stream()
+
+    def late():
+        with torch.cuda.stream(third):
+            torch.cuda._sleep(20_000_000)
+
+    runs = []
+    for step, other in ((None, None), (side, third)):
+        run = StreamRunner(layers, h_q, h_kv, d, n, 200)
+        run.push(chunks[0], step)
+        run.hold(other)                            # (makes the handle, which waits for the device)
+        torch.cuda.synchronize()
+        run.push(chunks[1], step, wait=False)
+        if other is not None:
+            late()
+        held = run.hold(other)
+        budgets = [run.push(chunks[2], step)]      # compacts the rows that are held
+        run.push(chunks[3], step, wait=False)
+        if other is not None:
+            late()
+        run.restore(held, other)
+        budgets.append(run.push(chunks[4], step))  # scores the rows that come back
+        run.push(chunks[5], step, wait=False)
+        if other is not None:
+            late()
+        again = run.hold(other)
+        for l in range(layers):
+            run.set_cache(l, chunks[0][l]["k"][:, :30], chunks[0][l]["v"][:, :30], 20, 10)
+        budgets.append(run.push(chunks[0], step))
+        views = [t.clone() for l in range(layers) for t in (run.cache_k(l), run.cache_v(l), run.cache_modality(l))]
+        torch.cuda.synchronize()
+        runs.append((budgets, held.data + again.data + views))
+        run.close()
+    for a, b in zip(*[r[0] for r in runs]):
+        assert np.array_equal(a, b)
+    for a, b in zip(*[r[1] for r in runs]):
+        assert torch.equal(a, b)
+
+
+def test_a_runners_first_step_on_another_stream(monkeypatch):
+    """The caches' fill on the constructor's stream, late as it is, lies before the rows of a step on another."""
+    class Slow(om.Context):
+        def __init__(self, *args, **options):
+            super().__init__(*args, **options)
+            torch.cuda._sleep(20_000_000)          # (what follows on the constructor's stream comes late)
+
+    layers, h_q, h_kv, d, n = 2, 4, 2, 64, 160
+    g = torch.Generator(device="cuda").manual_seed(14)
+    chunk = stream_chunk(g, layers, h_q, h_kv, d, n)
+    plain = StreamRunner(layers, h_q, h_kv, d, n, 200)
+    want = plain.push(chunk)
+    torch.cuda.synchronize()
+    monkeypatch.setattr(om, "Context", Slow)
+    late = StreamRunner(layers, h_q, h_kv, d, n, 200)
+    got = late.push(chunk, torch.cuda.Stream())
+    torch.cuda.synchronize()
+    assert np.array_equal(got, want)
+    for l in range(layers):
+        assert torch.equal(late.cache_k(l), plain.cache_k(l)) and torch.equal(late.cache_v(l), plain.cache_v(l))
+        assert torch.equal(late.cache_modality(l), plain.cache_modality(l))
+    plain.close()
+    late.close()
