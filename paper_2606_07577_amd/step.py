@@ -567,7 +567,6 @@ class Reader:
             raise ValueError("every layer takes the same numbers of tokens (next() begins the next ones)")
         if any(t + n > self.cap for t, n in zip(self.tail, new)):
             raise ValueError(f"more than {self.cap} tail rows")
-        self._new = new
         total, elt = sum(new), self.tdtype.itemsize
         with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
             rotated, out = (torch.empty((total, self.h_q, self.d), device=self.device, dtype=self.tdtype) for _ in range(2))
@@ -584,6 +583,7 @@ class Reader:
         query["n_tail"] = np.add(self.tail, new)
         self.attn.omnimem_rotate(self.rope, self._rows, stream)
         self.attn.omnimem_attend(self._queries[l], True, stream)
+        self._new = new                          # (a call that was refused has added nothing)
         if isinstance(q, torch.Tensor):
             return out.view(len(new), -1, self.h_q, self.d).transpose(1, 2) if total else out.new_empty((len(new), self.h_q, 0, self.d))
         return [out[i: j].transpose(0, 1) for i, j in zip(first[:-1], first[1:])]

@@ -399,3 +399,30 @@ def test_a_runners_first_step_on_another_stream(monkeypatch):
         assert torch.equal(late.cache_modality(l), plain.cache_modality(l))
     plain.close()
     late.close()
+
+
+def test_a_refused_layer_leaves_the_reader_as_it_was():
+    """A call that the library refuses sets no number of tokens: next() adds none, and other numbers are taken."""
+    h_q, h_kv, d = 2, 1, 64
+    g = torch.Generator(device="cuda").manual_seed(15)
+    rnd = lambda h, n: torch.randn(h, n, d, generator=g, device="cuda").bfloat16()
+    pos = lambda n: torch.arange(n, dtype=torch.int32, device="cuda")[None]
+    memory = HeldMemory([torch.zeros(om.memory_shape(h_kv, d, 0), dtype=torch.uint8, device="cuda")] * 2, [0, 0], [0, 0])
+    reader = Reader([memory], h_q, h_kv, d, om.make_rope(d, [0.5 ** j for j in range(32)]), 16)
+    off = torch.zeros(h_q * 5 * d + 1, device="cuda", dtype=torch.bfloat16)[1:].view(h_q, 5, d)      # (2 bytes past 16)
+    with pytest.raises(om.OmnimemError):
+        reader.layer(0, [off], [rnd(h_kv, 5)], [rnd(h_kv, 5)], [pos(5)])
+    reader.next()
+    assert reader.tail == [0]
+    with pytest.raises(om.OmnimemError):
+        reader.layer(0, [off], [rnd(h_kv, 5)], [rnd(h_kv, 5)], [pos(5)])
+    for l in range(2):
+        reader.layer(l, [rnd(h_q, 3)], [rnd(h_kv, 3)], [rnd(h_kv, 3)], [pos(3)])
+    with pytest.raises(om.OmnimemError):           # (a layer before it was taken: its numbers stay)
+        reader.layer(1, [off[:, :3]], [rnd(h_kv, 3)], [rnd(h_kv, 3)], [pos(3)])
+    with pytest.raises(ValueError, match="same numbers"):
+        reader.layer(1, [rnd(h_q, 4)], [rnd(h_kv, 4)], [rnd(h_kv, 4)], [pos(4)])
+    reader.next()
+    assert reader.tail == [3]
+    torch.cuda.synchronize()
+    reader.close()
