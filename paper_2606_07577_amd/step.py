@@ -93,11 +93,12 @@ class DeviceStep:
             with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream()):
                 self.attn_out = [torch.zeros((c, self.h_q, self.d), device=self.device, dtype=self.tdtype).transpose(0, 1)
                                  for c in chunk]
-                lse = [torch.zeros((self.h_q, c), device=self.device, dtype=torch.float32) for c in chunk]
+                self._attn_lse = [torch.zeros((self.h_q, c), device=self.device, dtype=torch.float32) for c in chunk]
             self._queries = om.array_of([om.make_query(self.q[l], self.attn_out[l], self.k[l], self.v[l],
-                                                       sm_scale=self.sm_scale[l], lse=lse[l])
+                                                       sm_scale=self.sm_scale[l], lse=self._attn_lse[l])
                                          for l in range(self.n_layers)])
-            self.set_lse_inputs(lse)
+        if any(a is not b for a, b in zip(self.lse_in, self._attn_lse)):
+            self.set_lse_inputs(self._attn_lse)
         self.attn.omnimem_attend(self._queries, self.ctx.cfg.causal, stream)
 
     # offline budgets (calibration) ----------------------------------------

@@ -426,3 +426,24 @@ def test_a_refused_layer_leaves_the_reader_as_it_was():
     assert reader.tail == [3]
     torch.cuda.synchronize()
     reader.close()
+
+
+def test_a_chunks_attention_after_other_lse_inputs():
+    """attend() again behind set_lse_inputs(): its log-sum-exp goes to arrays of its own (which the caller's inputs do not
+    free), and the scores take it again."""
+    layer = synth.make_layer([7, 1], h_q=4, h_kv=2, d=64, n_cache_v=90, n_cache_a=30, n_frames=2, frame_v=20, frame_a=5,
+                             dup_frac=0.3, head_scale=(0.5, 2.0), dtype="bf16")
+    step = DeviceStep([layer], 80)
+    step.attend()
+    step.score()
+    torch.cuda.synchronize()
+    want, lse, c = step.host("a", 0), step.lse_in[0].clone(), step.n[0] - step.n_cache[0]
+    step.set_lse_inputs([None])
+    others = [torch.full((4, c), 3.0, device="cuda") for _ in range(20)]   # (freed arrays would be among these)
+    step.set_lse_inputs([others[0]])
+    step.attend()
+    step.score()
+    torch.cuda.synchronize()
+    assert all((t == 3.0).all() for t in others)
+    assert torch.equal(step.lse_in[0], lse) and np.array_equal(step.host("a", 0), want)
+    step.close()
