@@ -55,6 +55,7 @@ class DeviceStep:
         self.lse_in = [None] * self.n_layers
         self.attn = None                    # made by attend()
         self.descs = self._descs()
+        torch.cuda.current_stream(self.device).synchronize()   # (stages may come on streams that do not wait for this one)
 
     def _descs(self):
         return [om.make_layer(self.q[l], self.k[l], self.v[l], self.mod[l], self.n_cache[l],

@@ -447,3 +447,26 @@ def test_a_chunks_attention_after_other_lse_inputs():
     assert all((t == 3.0).all() for t in others)
     assert torch.equal(step.lse_in[0], lse) and np.array_equal(step.host("a", 0), want)
     step.close()
+
+
+def test_a_steps_first_stage_on_another_stream(monkeypatch):
+    """What the constructor fills, late as it is, is filled before a stage on another stream writes there."""
+    layer = synth.make_layer([8, 1], h_q=4, h_kv=2, d=64, n_cache_v=90, n_cache_a=30, n_frames=2, frame_v=20, frame_a=5,
+                             dup_frac=0.3, head_scale=(0.5, 2.0), dtype="bf16")
+    plain = DeviceStep([layer], 80)
+    plain.score()
+    torch.cuda.synchronize()
+    zeros_like, side = torch.zeros_like, torch.cuda.Stream()
+
+    def slow(t):
+        torch.cuda._sleep(20_000_000)              # (what follows on the constructor's stream comes late)
+        return zeros_like(t)
+
+    monkeypatch.setattr(torch, "zeros_like", slow)
+    late = DeviceStep([layer], 80)
+    late.score(side)
+    torch.cuda.synchronize()
+    assert np.array_equal(late.host("a", 0), plain.host("a", 0)) and plain.host("a", 0).sum() > 0
+    assert np.array_equal(late.host("lse", 0), plain.host("lse", 0))
+    plain.close()
+    late.close()
