@@ -281,14 +281,22 @@ class StreamRunner:
             data = [torch.empty(om.memory_shape(self.h_kv, self.d, n), dtype=torch.uint8, device=self.device)
                     for n in self.n_cache]
             self.attn.omnimem_pack(self._held(data, self.n_cache))
-        return HeldMemory(data, list(self.n_cache), [int(b) for b in budgets[:, 0]])
+            ready = torch.cuda.Event()
+            ready.record()
+        return HeldMemory(data, list(self.n_cache), [int(b) for b in budgets[:, 0]], ready)
 
     def restore(self, held, stream=None):
         """Take a held memory's rows, as they are held, for the retained caches."""
         self.finish()
         if len(held.rows) != self.L or max(held.rows) > self.cache_cap:
             raise ValueError("the memory has another number of layers, or more rows than the caches hold")
-        with torch.cuda.stream(self._attention_stream(stream)):
+        stream = self._attention_stream(stream)
+        with torch.cuda.stream(stream):
+            if not torch.cuda.is_current_stream_capturing():   # (a capture may not wait for work outside it)
+                if held.ready is not None:
+                    stream.wait_event(held.ready)
+                for data in held.data:
+                    data.record_stream(stream)                 # (the memory may be dropped before the stream is here)
             self.attn.omnimem_unpack(self._held(held.data, held.rows))
             for mod, n, visual in zip(self.mbuf[self.cur], held.rows, held.visual):
                 mod[:visual] = 0
@@ -468,10 +476,12 @@ class StreamRunner:
 
 class HeldMemory:
     """A stream's kept rows in 4 bits: data[l] uint8 [H_kv, blocks, 34 d],
-    rows[l] kept rows, visual[l] of them visual (in front)."""
+    rows[l] kept rows, visual[l] of them visual (in front).  ready: the event
+    behind what writes the data, or None if nothing has to be waited for;
+    restore() and Reader wait for it."""
 
-    def __init__(self, data, rows, visual):
-        self.data, self.rows, self.visual = data, rows, visual
+    def __init__(self, data, rows, visual, ready=None):
+        self.data, self.rows, self.visual, self.ready = data, rows, visual, ready
 
 
 class Reader:
@@ -501,6 +511,9 @@ class Reader:
         self.device = self.k.device
         # (calls come on streams that do not wait for this one, and into captures, which may not wait for it)
         torch.cuda.current_stream(self.device).synchronize()
+        for m in self.memories:
+            if m.ready is not None:
+                m.ready.synchronize()
         self.tail = [0] * streams                # tail rows of each stream
         self._new = None                         # and those that the current tokens add
         layouts = {om._Layout(h_q, h_kv, d, self.tdtype, self.device.index, rope.n_axes)}

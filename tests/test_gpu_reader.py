@@ -470,3 +470,45 @@ def test_a_steps_first_stage_on_another_stream(monkeypatch):
     assert np.array_equal(late.host("lse", 0), plain.host("lse", 0))
     plain.close()
     late.close()
+
+
+def test_a_memory_that_is_still_being_held():
+    """Another stream's caches are brought back from a memory that is packed late, and dropped before they are; and an
+    answer is read from such a memory."""
+    layers, h_q, h_kv, d, n = 2, 4, 2, 64, 160
+    g = torch.Generator(device="cuda").manual_seed(16)
+    run, other = (StreamRunner(layers, h_q, h_kv, d, n, 200) for _ in range(2))
+    run.hold()
+    other.hold()                                   # (make the handles, which wait for the device)
+    side, third = torch.cuda.Stream(), torch.cuda.Stream()
+
+    def late():
+        run.push(stream_chunk(g, layers, h_q, h_kv, d, n), wait=False)
+        with torch.cuda.stream(third):
+            torch.cuda._sleep(20_000_000)
+        return run.hold(third)
+
+    held = late()
+    other.restore(held, side)
+    del held
+    with torch.cuda.stream(third):                 # (would take the memory's place)
+        noise = [torch.full((1 << i,), 0xA5, dtype=torch.uint8, device="cuda") for i in range(8, 20) for _ in range(4)]
+    want = run.hold()
+    torch.cuda.synchronize()
+    assert other.n_cache == want.rows
+    for l in range(layers):
+        kv = orc.unpack(want.data[l].cpu().numpy(), want.rows[l])
+        assert np.array_equal(host(other.cache_k(l)), kv[0]) and np.array_equal(host(other.cache_v(l)), kv[1])
+    rope = om.make_rope(d, [0.5 ** j for j in range(32)])
+    q, k, v = (torch.randn(h, 3, d, generator=g, device="cuda").bfloat16() for h in (h_q, h_kv, h_kv))
+    pos = torch.arange(3, dtype=torch.int32, device="cuda")[None]
+    torch.cuda.synchronize()
+    outs, held = [], late()
+    for memory in (held, None):
+        reader = Reader([memory or run.hold()], h_q, h_kv, d, rope, 8)
+        outs.append(reader.layer(0, [q], [k], [v], [pos], side)[0])
+        torch.cuda.synchronize()
+        reader.close()
+    assert torch.equal(*outs)
+    run.close()
+    other.close()
