@@ -367,7 +367,8 @@ class StreamRunner:
         has described its chunk, so the host's work overlaps the GPU's) or
         by finish()."""
         stream = self._behind(stream)
-        chunk = self._on_device(chunk)
+        with torch.cuda.stream(stream):
+            chunk = self._on_device(chunk)
         cur = self.cur if self.in_place or not self._pending else 1 - self.cur
         self._describe(chunk, [ch["q"] for ch in chunk], cur)
         self.finish()              # the previous step's budgets give this step's kept rows

@@ -512,3 +512,23 @@ def test_a_memory_that_is_still_being_held():
     assert torch.equal(*outs)
     run.close()
     other.close()
+
+
+def test_a_chunk_that_is_copied_for_a_step_on_another_stream():
+    """Rows that push() makes contiguous are made so on the step's stream, whatever the current one has to do before."""
+    layers, h_q, h_kv, d, n = 2, 4, 2, 64, 160
+    g = torch.Generator(device="cuda").manual_seed(17)
+    chunk = stream_chunk(g, layers, h_q, h_kv, d, n)
+    spread = [dict(ch, **{x: torch.stack([ch[x]] * 2, -1)[..., 0] for x in ("q", "k", "v")}) for ch in chunk]
+    plain, late = (StreamRunner(layers, h_q, h_kv, d, n, 200) for _ in range(2))
+    want = plain.push(chunk)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    torch.cuda._sleep(20_000_000)
+    got = late.push(spread, side)
+    torch.cuda.synchronize()
+    assert np.array_equal(got, want)
+    for l in range(layers):
+        assert torch.equal(late.cache_k(l), plain.cache_k(l)) and torch.equal(late.cache_v(l), plain.cache_v(l))
+    plain.close()
+    late.close()
