@@ -462,10 +462,11 @@ omnimem_status omnimem_rotate(omnimem_attn* attn, const omnimem_rope* rope, cons
  * rows and 34 d bytes.  32 values share a scale 2^e: of K, 32 consecutive
  * channels of a row; of V, a channel's 32 rows (the axis that each is summed
  * along).  With m the group's largest magnitude, e is the smallest exponent
- * of at least -120 with m <= 7 * 2^e, and a value x is held as the multiple of
- * 2^e in {0, 0.5, 1, 1.5, 2, 3, 4, 6} nearest to |x| (ties to the even code),
- * with x's sign: off by at most 2^e.  A group with an infinity or NaN comes
- * back as NaN.  A block's bytes:
+ * of at least -120 with m <= 7 * 2^e, but at most 125, and a value x is held as
+ * the multiple of 2^e in {0, 0.5, 1, 1.5, 2, 3, 4, 6} nearest to |x| (ties to
+ * the even code), with x's sign: off by at most 2^e, or 2^126 where |x| is past
+ * 7 * 2^125 (held as 6 * 2^125: every finite value comes back finite).  A group
+ * with an infinity or NaN comes back as NaN.  A block's bytes:
  *   [0, 16 d)     K codes, row t at (d / 2) t: channels 2i, 2i + 1 in the low
  *                 and high half of byte i; code = sign << 3 | index above;
  *   [16 d, 32 d)  V codes, channel c at 16 c: rows 2i, 2i + 1 in byte i;

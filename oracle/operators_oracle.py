@@ -25,7 +25,7 @@ def hold_group(x):
     if not np.isfinite(x).all():
         return np.zeros(len(x), np.int64), 255
     e = -120
-    while m > 7 * 2.0 ** e:
+    while m > 7 * 2.0 ** e and e < 125:
         e += 1
     codes = []
     for v in x:

@@ -27,7 +27,7 @@ struct MemBlock {
   __host__ __device__ static inline int v_scale(int c) { return VS + (c & 15) * (D / 16) + (c >> 4); }
 };
 constexpr uint32_t kScaleNan = 255;    // the scale byte of a group with an infinity or NaN
-constexpr uint32_t kScaleMin = 7;      // 2^-120
+constexpr uint32_t kScaleMin = 7, kScaleMax = 252;   // 2^-120 and 2^125
 __device__ inline float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
 
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));

@@ -8,11 +8,12 @@ namespace {
 
 // The scale byte of a group whose largest magnitude has the bits m: the
 // smallest exponent with m <= 1.75 * 2^(e + 2), from the exponent field of m
-// with anything past 1.75 carried into it.
+// with anything past 1.75 carried into it; 2^125 at most, whose largest code
+// is 6 * 2^125 (a code of 4 * 2^126 would come back as an infinity).
 __device__ inline uint32_t scale_byte(uint32_t m) {
   if (m >= 0x7F800000u) return kScaleNan;
   const int e = (int)((m + 0x1FFFFFu) >> 23) - 2;
-  return (uint32_t)max(e, (int)kScaleMin);
+  return (uint32_t)min(max(e, (int)kScaleMin), (int)kScaleMax);
 }
 __device__ inline uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7FFFFFFFu; }
 

@@ -114,3 +114,31 @@ def test_offsets_past_32_bits():
     torch.cuda.synchronize()
     assert torch.equal(far[0], near_k) and torch.equal(far[1], near_v)
     attn.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_the_largest_finite_values_come_back_finite(dtype, d):
+    """Groups up to the type's largest value: bytes and values of the definition, off by at most 2^126 (4 * 2^126, the code
+    nearest to the largest value at the next scale, is no fp32 or bf16 number)."""
+    td, n = TORCH[dtype], 64
+    top = torch.finfo(td).max
+    attn = om.Attention(1, 1, d, om.BF16 if dtype == "bf16" else om.F32)
+    g = torch.Generator(device="cuda").manual_seed(d)
+    k, v = ((torch.rand(1, n, d, generator=g, device="cuda", dtype=torch.float64) * 2 - 1).mul_(top).to(td) for _ in range(2))
+    k[0, 0, :8] = torch.tensor([top, -top, 7 * 2.0 ** 125, 7.0625 * 2.0 ** 125, 6 * 2.0 ** 125, 2.0 ** 127, 3.5 * 2.0 ** 125, 1.0])
+    v[0, :8, 0] = k[0, 0, :8]
+    k[0, 1] = 7 * 2.0 ** 125                       # the largest group of the scale 2^125 that is not cut off
+    data = torch.zeros(om.memory_shape(1, d, n), dtype=torch.uint8, device="cuda")
+    attn.omnimem_pack([om.make_held(k, v, data)])
+    back = [torch.zeros_like(k) for _ in range(2)]
+    attn.omnimem_unpack([om.make_held(*back, data)])
+    torch.cuda.synchronize()
+    want = orc.pack(k.double().cpu().numpy(), v.double().cpu().numpy())
+    assert np.array_equal(data.cpu().numpy(), want)
+    for t, x, y in zip(back, orc.unpack(want, n), (k, v)):
+        got, was = t.double().cpu().numpy(), y.double().cpu().numpy()
+        assert np.isfinite(got).all() and np.array_equal(got, x)
+        assert (np.abs(got - was) <= 2.0 ** 126).all()
+        assert (np.abs(got) <= 6 * 2.0 ** 125).all() and (np.sign(got[was != 1]) * np.sign(was[was != 1]) >= 0).all()
+    attn.close()
