@@ -143,14 +143,15 @@ __device__ inline float log_of(float m, float l) { return l == 0.0f ? -INFINITY 
 
 // ---------------------------------------------------------------------------
 // Rows that a query does not see have weight 0, but the matrix cores multiply
-// it with what the row holds, and 0 times an infinity or NaN is NaN.  A unit
-// whose sums are not finite forms the rows again that have such a row among
-// its keys, each by one wavefront over the keys that the row sees, and writes
-// them over what it wrote.
+// it with what the row holds, and 0 times an infinity or NaN is NaN.  So do the
+// rows behind the last one in its tile, which are copies of it.  A unit whose
+// sums are not finite forms the rows again that have either among its keys, each
+// by one wavefront over the keys that the row sees, and writes them over what
+// it wrote.
 // ---------------------------------------------------------------------------
-template <typename T, int D, int KT>
-__device__ inline bool sees_all(const QuerySeq& s, const Unit& x, const Row& row) {
-  return row.seen >= min((int64_t)s.nt, (int64_t)(x.k1 - x.mem_tiles) * KT);
+template <int KT>
+__device__ inline bool sees_all(const Unit& x, const Row& row) {     // whole tiles
+  return row.seen >= (int64_t)(x.k1 - x.mem_tiles) * KT;
 }
 template <int D, typename T>
 __device__ inline void channels(const T* p, int lane, float (&y)[D / 64]) {
@@ -166,7 +167,7 @@ __device__ __forceinline__ void form_again(const AttendArgs<N>& a, const QuerySe
   constexpr int E = (int)sizeof(T), C = D / 64;
   const int lane = threadIdx.x & 63;
   const Row row = row_of(a, s, x, x.rt * R + r);
-  if (!row.live || sees_all<T, D, KT>(s, x, row)) return;
+  if (!row.live || sees_all<KT>(x, row)) return;
   const float ref = m == -INFINITY ? 0.0f : m;
   float q[C], o[C] = {};
   channels<D>(static_cast<const T*>(s.q) + row.h * elems(s.q_hs, E) + row.i * elems(s.q_rs, E), lane, q);
@@ -222,7 +223,7 @@ __device__ __forceinline__ void form_own(const AttendArgs<N>& a, const QuerySeq&
   for (int c = 0; c < D / 32; ++c)
 #pragma unroll
     for (int e = 0; e < 16; ++e) zero = __builtin_fmaf(o[c][e], 0.0f, zero);
-  uint64_t odd = __ballot(zero != 0.0f && row.live && !sees_all<T, D, KT>(s, x, row));
+  uint64_t odd = __ballot(zero != 0.0f && row.live && !sees_all<KT>(x, row));
   for (odd = (odd | odd >> 32) & 0xFFFFFFFFu; odd; odd &= odd - 1) {
     const int r = __builtin_ctzll(odd);
     form_again<T, D, R, KT>(a, s, x, r0 + r, __shfl(m, r), __shfl(l, r));

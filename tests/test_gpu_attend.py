@@ -420,3 +420,43 @@ def test_a_memory_past_32_bits_of_bytes(dtype, nq):
     assert (np.abs(host(out) * rows / 37 - 1) <= join + (2.0 ** -8 if dtype == "bf16" else 0)).all()
     assert (np.abs(host(lse) - np.log(rows)) <= join + 2 * U * np.log(rows)).all()
     attn.close()
+
+
+def infinite_last(attn, g, dtype, nq, nm, nt):
+    c = Case(attn, g, 6, 2, 64, dtype, nq, nm, nt)
+    c.v[0, nt - 1, 5], c.v[0, nt - 1, 6] = float("inf"), float("-inf")
+    return c
+
+
+def check_infinite_last(c, causal):
+    """Channels 5 and 6 of heads 0 .. 2 are infinities of one sign for queries that see the last row; all else as it is
+    without them."""
+    nq, nm, nt = c.sizes
+    seeing = slice(nq - 1, nq) if causal else slice(0, nq)
+    got = c.out[:3, seeing, 5:7].float()
+    assert bool((got[..., 0] == float("inf")).all()) and bool((got[..., 1] == float("-inf")).all())
+    c.v[0, nt - 1, 5:7] = 0.0                      # (the others against the definition)
+    c.out[:3, seeing, 5:7] = 0.0
+    k, v = (np.concatenate([m, host(t[:, :nt])], 1) for m, t in zip(c.held, (c.k, c.v)))
+    out, lse, size, reach = orc.attend(host(c.q), k, v, nm, c.scale, causal)
+    half, n = (2.0 ** -8 if c.q.dtype == torch.bfloat16 else 0.0), nm + nt
+    tol = size * (2 * (64 + 6) * U * reach[..., None] + 2 * (n + 8) * U + half) + (half or U) * np.abs(out)
+    off = np.abs(host(c.out[:, :nq]) - out)
+    off[:3, seeing, 5:7] = 0.0
+    assert (off <= tol + n * 2.0 ** -126 * np.abs(v).max()).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("nq,nm,nt", [(1, 0, 5), (5, 0, 33), (40, 31, 77), (130, 0, 131), (300, 100, 411), (3, 2100, 2001), (200, 0, 1333)])
+def test_an_infinity_in_the_last_tail_row(dtype, causal, nq, nm, nt):
+    """A tile that ends behind it adds nothing to it: what sees it gets an infinity and not NaN, alone and beside a chunk."""
+    attn = handle(6, 2, 64, dtype)
+    g = torch.Generator(device="cuda").manual_seed(nt)
+    chunk, keep = chunk_beside(g, 6, 2, 64, dtype)
+    for before in ([], [chunk]):
+        c = infinite_last(attn, g, dtype, nq, nm, nt)
+        attn.omnimem_attend(before + [c.query()], causal)
+        torch.cuda.synchronize()
+        check_infinite_last(c, causal)
+    attn.close()
