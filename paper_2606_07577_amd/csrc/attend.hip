@@ -139,6 +139,9 @@ __device__ inline float max16(float x) {
   const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
+// A row's sums over the sum of its weights; 0 if it has none, whatever the
+// values are that weights of 0 were multiplied with.
+__device__ inline floatx4 over(floatx4 y, float l) { return l == 0.0f ? floatx4{} : y * (1.0f / l); }
 __device__ inline float log_of(float m, float l) { return l == 0.0f ? -INFINITY : (m + log2f(l)) * kLn2; }
 
 // ---------------------------------------------------------------------------
@@ -204,13 +207,13 @@ __device__ __forceinline__ void form_again(const AttendArgs<N>& a, const QuerySe
     channels<D>(static_cast<const T*>(s.v) + hs + j * rs, lane, v);
     add(k, v);
   }
-  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+  const float inv = 1.0f / l;
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");   // (after what the workgroup wrote there)
 #pragma unroll
   for (int i = 0; i < C; ++i) {
     const int c = lane + i * 64;
     if (x.slot >= 0) __hip_atomic_store(a.part_o + ((int64_t)x.slot * R + r) * D + c, o[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    else put1(static_cast<T*>(s.out) + row.h * elems(s.out_hs, E) + row.i * elems(s.out_rs, E) + c, o[i] * inv);
+    else put1(static_cast<T*>(s.out) + row.h * elems(s.out_hs, E) + row.i * elems(s.out_rs, E) + c, l == 0.0f ? 0.0f : o[i] * inv);
   }
 }
 // The same for a wavefront's own 32 rows (a lane each, twice).
@@ -248,7 +251,7 @@ __device__ __forceinline__ void finish(const AttendArgs<N>& a, const QuerySeq& s
   const int tid = threadIdx.x, live = min(R, x.rows - x.rt * R);
   const auto put_row = [&](int r, int c, floatx4 y, float l) __attribute__((always_inline)) {
     const Row row = row_of(a, s, x, x.rt * R + r);
-    put4(static_cast<T*>(s.out) + row.h * elems(s.out_hs, E) + row.i * elems(s.out_rs, E) + c, y * (l == 0.0f ? 0.0f : 1.0f / l));
+    put4(static_cast<T*>(s.out) + row.h * elems(s.out_hs, E) + row.i * elems(s.out_rs, E) + c, over(y, l));
   };
   const auto put_lse = [&](int r, float m, float l) __attribute__((always_inline)) {
     const Row row = row_of(a, s, x, x.rt * R + r);
@@ -364,14 +367,13 @@ __device__ inline void write_rows(const AttendArgs<N>& a, const QuerySeq& s, con
       for (int e = 0; e < 4; ++e)
         put4(a.part_o + at * D + c * 32 + e * 8 + half * 4, floatx4{o[c][4 * e], o[c][4 * e + 1], o[c][4 * e + 2], o[c][4 * e + 3]});
   } else if (row.live) {
-    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
     T* out = static_cast<T*>(s.out) + row.h * elems(s.out_hs, E) + row.i * elems(s.out_rs, E);
     if (half == 0 && s.lse) s.lse[row.h * (int64_t)s.lse_hs + row.i] = log_of(m, l);
 #pragma unroll
     for (int c = 0; c < D / 32; ++c)
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        put4(out + c * 32 + e * 8 + half * 4, floatx4{o[c][4 * e], o[c][4 * e + 1], o[c][4 * e + 2], o[c][4 * e + 3]} * inv);
+        put4(out + c * 32 + e * 8 + half * 4, over(floatx4{o[c][4 * e], o[c][4 * e + 1], o[c][4 * e + 2], o[c][4 * e + 3]}, l));
   }
 }
 
@@ -1398,8 +1400,7 @@ __global__ __launch_bounds__(THREADS) void join_splits(AttendArgs<N> a) {
   }
   if (!live) return;
   const int i = row / a.group, h = x.g * a.group + row % a.group;
-  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-  put4(static_cast<T*>(s.out) + h * elems(s.out_hs, E) + i * elems(s.out_rs, E) + c, o * inv);
+  put4(static_cast<T*>(s.out) + h * elems(s.out_hs, E) + i * elems(s.out_rs, E) + c, over(o, l));
   if (c == 0 && s.lse) s.lse[h * (int64_t)s.lse_hs + i] = log_of(m, l);
 }
 

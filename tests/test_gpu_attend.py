@@ -460,3 +460,22 @@ def test_an_infinity_in_the_last_tail_row(dtype, causal, nq, nm, nt):
         torch.cuda.synchronize()
         check_infinite_last(c, causal)
     attn.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("nq,nt", [(1, 64), (1, 3000), (40, 77), (130, 128), (200, 2500)])
+def test_no_weight_at_all_is_0_whatever_the_values(dtype, nq, nt):
+    """Products that are all -inf beside values that are infinite or NaN: out = 0 and lse = -inf all the same."""
+    attn = handle(6, 2, 64, dtype)
+    g = torch.Generator(device="cuda").manual_seed(nt)
+    chunk, keep = chunk_beside(g, 6, 2, 64, dtype)
+    for before in ([], [chunk]):
+        c = Case(attn, g, 6, 2, 64, dtype, nq, 0, nt)
+        c.q.fill_(1.0)
+        c.k[:, :nt] = 0.0
+        c.k[:, :nt, 0] = float("-inf")
+        c.v[0, :nt:3, 5], c.v[1, :nt:5, 9] = float("inf"), float("nan")
+        attn.omnimem_attend(before + [c.query()], False)
+        torch.cuda.synchronize()
+        assert (c.out[:, :nq] == 0).all() and torch.isneginf(c.lse[:, :nq]).all()
+    attn.close()
