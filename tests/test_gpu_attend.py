@@ -479,3 +479,68 @@ def test_no_weight_at_all_is_0_whatever_the_values(dtype, nq, nt):
         torch.cuda.synchronize()
         assert (c.out[:, :nq] == 0).all() and torch.isneginf(c.lse[:, :nq]).all()
     attn.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("nq,nm,nt", [(3, 0, 33), (40, 31, 77), (130, 0, 131), (300, 100, 411), (3, 2100, 2001)])
+def test_nan_that_is_seen(dtype, causal, nq, nm, nt):
+    """Queries that are NaN, and NaN in a key and in a value that every query sees: NaN where the definition has it, alone
+    and beside a chunk."""
+    attn = handle(6, 2, 64, dtype)
+    g = torch.Generator(device="cuda").manual_seed(nt)
+    chunk, keep = chunk_beside(g, 6, 2, 64, dtype)
+    nan = float("nan")
+    for before in ([], [chunk]):
+        for what in ("query", "key", "value"):
+            c = Case(attn, g, 6, 2, 64, dtype, nq, nm, nt)
+            if what == "query":
+                c.q[1, nq // 2], c.q[4, nq - 1, 7] = nan, nan
+            elif what == "key":
+                c.k[1, 0, 3] = nan
+            else:
+                c.v[1, 0, 3] = nan
+            attn.omnimem_attend(before + [c.query()], causal)
+            torch.cuda.synchronize()
+            # (as Case.check, with the largest value that is not NaN)
+            k, v = (np.concatenate([m, host(t[:, :nt])], 1) for m, t in zip(c.held, (c.k, c.v)))
+            out, lse, size, reach = orc.attend(host(c.q), k, v, nm, c.scale, causal)
+            half, n, got = (2.0 ** -8 if dtype == "bf16" else 0.0), nm + nt, host(c.out[:, :nq])
+            nans = np.isnan(out)
+            assert nans.any() and not nans.all() and np.array_equal(np.isnan(got), nans)
+            tol = size * (2 * (64 + 6) * U * reach[..., None] + 2 * (n + 8) * U + half) + (half or U) * np.abs(out)
+            assert (np.abs(got - out)[~nans] <= tol[~nans] + n * 2.0 ** -126 * np.nanmax(np.abs(v))).all()
+            assert np.array_equal(np.isnan(host(c.lse[:, :nq])), np.isnan(lse))
+    attn.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("nq", [4, 1000])
+def test_nan_that_is_seen_costs_no_second_pass(dtype, nq):
+    """NaN that belongs into the results takes the time of the pass, not that of forming the rows again one by one (30 to
+    140 times as long at these sizes)."""
+    attn = handle(8, 2, 128, dtype)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    rnd = lambda h, n: torch.randn(h, n, 128, generator=g, device="cuda").to(TORCH[dtype])
+    q, k, v = rnd(8, nq), rnd(2, 2001), rnd(2, 2001)
+    out = torch.empty_like(q)
+
+    def least(q, v, causal):
+        queries = om.array_of([om.make_query(q, out, k, v)])
+        times = []
+        for _ in range(5):
+            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            a.record()
+            attn.omnimem_attend(queries, causal)
+            b.record()
+            torch.cuda.synchronize()
+            times.append(a.elapsed_time(b))
+        return min(times)
+
+    bad_q, bad_v = torch.full_like(q, float("nan")), v.clone()
+    bad_v[:, 0] = float("nan")
+    for causal in (True, False):
+        plain = least(q, v, causal)
+        for args in ((bad_q, v), (q, bad_v)):
+            assert least(*args, causal) < 4 * plain + 0.05
+    attn.close()
