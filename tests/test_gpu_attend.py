@@ -544,3 +544,41 @@ def test_nan_that_is_seen_costs_no_second_pass(dtype, nq):
         for args in ((bad_q, v), (q, bad_v)):
             assert least(*args, causal) < 4 * plain + 0.05
     attn.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_a_call_of_several_launches(dtype, d):
+    """70 sequences where a launch describes 32, long ones whose keys are split and joined in each of the launches (they use
+    the same partials and counters), and empty ones about the borders."""
+    attn = handle(4, 2, d, dtype)
+    g = torch.Generator(device="cuda").manual_seed(d)
+    sizes = [(1 + (5 * i) % 7, (337 * i) % 2900, 1 + (11 * i) % 90) for i in range(70)]
+    for i in (0, 30, 31, 32, 33, 64, 69):
+        sizes[i] = (0, 40, 5) if i % 2 else (2, 0, 0)
+    sizes[12], sizes[45] = (1, 9000, 3), (9, 0, 6000)
+    cases = [Case(attn, g, 4, 2, d, dtype, *s, lse=i % 3 == 0) for i, s in enumerate(sizes)]
+    queries = om.array_of([c.query() for c in cases])
+    for _ in range(2):
+        for c in cases:
+            c.out.fill_(7.0)
+        attn.omnimem_attend(queries)
+        torch.cuda.synchronize()
+        for c in cases:
+            c.check(True)
+    attn.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_chunks_and_tokens_in_a_call_of_several_launches(dtype):
+    """A chunk among the first 32 sequences and one behind them, tokens with more keys beside each."""
+    attn = handle(4, 4, 64, dtype)
+    g = torch.Generator(device="cuda").manual_seed(6)
+    sizes = [(1, 20 + 3 * i, 1 + i % 5) for i in range(40)]
+    sizes[3], sizes[4], sizes[36], sizes[37] = (2600, 0, 2600), (1, 3000, 5), (1, 2000, 900), (1500, 300, 1500)
+    cases = [Case(attn, g, 4, 4, 64, dtype, *s) for s in sizes]
+    attn.omnimem_attend([c.query() for c in cases])
+    torch.cuda.synchronize()
+    for c in cases:
+        c.check(True)
+    attn.close()

@@ -142,3 +142,32 @@ def test_the_largest_finite_values_come_back_finite(dtype, d):
         assert (np.abs(got - was) <= 2.0 ** 126).all()
         assert (np.abs(got) <= 6 * 2.0 ** 125).all() and (np.sign(got[was != 1]) * np.sign(was[was != 1]) >= 0).all()
     attn.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_call_of_several_launches(dtype):
+    """150 sequences where a launch describes 64, empty ones about the borders: each as in a call of its own."""
+    h, d, b, td = 2, 64, 150, TORCH[dtype]
+    g = torch.Generator(device="cuda").manual_seed(9)
+    attn = om.Attention(h, h, d, om.BF16 if dtype == "bf16" else om.F32)
+    lengths = [1 + (13 * i) % 70 for i in range(b)]
+    for i in (0, 62, 63, 64, 65, 128, 149):
+        lengths[i] = 0
+    k, v = (torch.randn(b, h, 70, d, generator=g, device="cuda").to(td) for _ in range(2))
+    data, one = (torch.zeros(b, h, 3, 34 * d, dtype=torch.uint8, device="cuda") for _ in range(2))
+    attn.omnimem_pack([om.make_held(k[i, :, :n], v[i, :, :n], data[i]) for i, n in enumerate(lengths)])
+    for i, n in enumerate(lengths):
+        attn.omnimem_pack([om.make_held(k[i, :, :n], v[i, :, :n], one[i])])
+    back, alone = ([torch.full_like(t, 7.0) for t in (k, v)] for _ in range(2))
+    attn.omnimem_unpack([om.make_held(back[0][i, :, :n], back[1][i, :, :n], data[i]) for i, n in enumerate(lengths)])
+    for i, n in enumerate(lengths):
+        attn.omnimem_unpack([om.make_held(alone[0][i, :, :n], alone[1][i, :, :n], data[i])])
+    torch.cuda.synchronize()
+    assert torch.equal(data, one)
+    for i, n in enumerate(lengths):
+        want = orc.pack(k[i, :, :n].double().cpu().numpy(), v[i, :, :n].double().cpu().numpy())
+        assert np.array_equal(data[i, :, : want.shape[1]].cpu().numpy(), want)
+        for x, y, z in zip(back, alone, orc.unpack(want, n)):
+            assert torch.equal(x[i], y[i]) and (x[i, :, n:] == 7).all()
+            assert np.array_equal(x[i, :, :n].double().cpu().numpy(), z)
+    attn.close()
