@@ -290,6 +290,7 @@ class StreamRunner:
         self.finish()
         if len(held.rows) != self.L or max(held.rows) > self.cache_cap:
             raise ValueError("the memory has another number of layers, or more rows than the caches hold")
+        rows = self._held(held.data, held.rows)                # (refuses tensors that do not fit)
         stream = self._attention_stream(stream)
         with torch.cuda.stream(stream):
             if not torch.cuda.is_current_stream_capturing():   # (a capture may not wait for work outside it)
@@ -297,7 +298,7 @@ class StreamRunner:
                     stream.wait_event(held.ready)
                 for data in held.data:
                     data.record_stream(stream)                 # (the memory may be dropped before the stream is here)
-            self.attn.omnimem_unpack(self._held(held.data, held.rows))
+            self.attn.omnimem_unpack(rows)
             for mod, n, visual in zip(self.mbuf[self.cur], held.rows, held.visual):
                 mod[:visual] = 0
                 mod[visual:n] = 1
@@ -483,6 +484,11 @@ class HeldMemory:
 
     def __init__(self, data, rows, visual, ready=None):
         self.data, self.rows, self.visual, self.ready = data, rows, visual, ready
+
+    def __getstate__(self):                        # copies, and what is saved, hold what is written
+        if self.ready is not None:
+            self.ready.synchronize()
+        return dict(self.__dict__, ready=None)
 
 
 class Reader:

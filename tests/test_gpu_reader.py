@@ -1,6 +1,9 @@
 """The operators around the step as they are used together: a chunk's attention and the scores that take its
 log-sum-exp, a stream's caches held in 4 bits and brought back, answers read from held memories, and a token's calls
 captured into a graph."""
+import copy
+import pickle
+
 import numpy as np
 import pytest
 import torch
@@ -532,3 +535,23 @@ def test_a_chunk_that_is_copied_for_a_step_on_another_stream():
         assert torch.equal(late.cache_k(l), plain.cache_k(l)) and torch.equal(late.cache_v(l), plain.cache_v(l))
     plain.close()
     late.close()
+
+
+def test_a_memory_is_copied_and_one_in_host_memory_refused():
+    """A copy of a memory (or a saved one) waits for its packing and needs no event; rows in host memory are refused as
+    other tensors that do not fit, and the caches stay."""
+    layers, h_q, h_kv, d, n = 2, 4, 2, 64, 160
+    g = torch.Generator(device="cuda").manual_seed(18)
+    run = StreamRunner(layers, h_q, h_kv, d, n, 200)
+    run.push(stream_chunk(g, layers, h_q, h_kv, d, n))
+    held = run.hold()
+    for other in (copy.deepcopy(held), pickle.loads(pickle.dumps(held))):
+        assert other.ready is None and other.rows == held.rows and other.visual == held.visual
+        assert all(torch.equal(a, b) for a, b in zip(other.data, held.data))
+        run.restore(other)
+        assert run.n_cache == held.rows
+    before = [run.cache_k(l).clone() for l in range(layers)]
+    with pytest.raises(ValueError, match="one device"):
+        run.restore(HeldMemory([x.cpu() for x in held.data], held.rows, held.visual))
+    assert run.n_cache == held.rows and all(torch.equal(run.cache_k(l), before[l]) for l in range(layers))
+    run.close()
