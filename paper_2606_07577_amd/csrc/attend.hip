@@ -1554,7 +1554,7 @@ hipError_t launch(const AttendArgs<N>& a, int64_t joins, int splits, Kernel kern
   if (e != hipSuccess || joins == 0) return e;
   if (splits <= 8) join<T, D, P::R, 1, 256>(a, joins, st);
   else if (splits <= 32 || P::R >= 128) join<T, D, P::R, 4, 256>(a, joins, st);
-  else join<T, D, P::R, 1024 / (D / 4), 1024>(a, joins, st);
+  else if constexpr (P::R < 128) join<T, D, P::R, 1024 / (D / 4), 1024>(a, joins, st);
   return hipGetLastError();
 }
 template <typename T, typename P, int D, typename One, typename All>
