@@ -775,10 +775,14 @@ __global__ __launch_bounds__(256, 2) void attend_f32_many(AttendArgs<N> a) {
 // (i, g) = (lane % 16, lane / 16) reads a quarter of K row i of eight 16-row
 // sets, and channel i's 32 rows of V block g, 16 bytes each; the sets are chosen
 // (rows 4 T .. 4 T + 3 of each of the four blocks) so that set T's scores in
-// lane (query, g) are those of V's rows 4 T .. of block g.  HBM bounds it on
+// lane (query, g) are those of V's rows 4 T .. of block g.  Memory bounds it on
 // many long caches (32 tokens of 28 heads over up to 16384 rows, 164 MB, 39 us:
-// 4.3 TB/s), latency and the join on one (40256 rows, 22 MB: 14 us, 5 of them the
-// join) and on short ones (219 rows: 6 us).
+// 4.3 TB/s), its latency and the join on one (40256 rows, 22 MB: 13.5 us, 4.7 of
+// them the join; 640 wavefronts wait 46% of their cycles and issue vector
+// instructions in 32%) and on short ones (219 rows: 6 us).  Questions (7
+// sequences, 180 rows of a head at most, 15.8 us) have one wavefront to a SIMD,
+// which issues vector instructions, most of them to convert codes, in 38% of
+// its cycles and waits in 41%.
 // ---------------------------------------------------------------------------
 template <int D, int NR>
 struct Few {
@@ -824,6 +828,7 @@ __device__ inline void weigh(floatx4 (&sc)[NR][N], Stats<NR>& st, float (&alpha)
     st.l[n] = st.l[n] * alpha[n] + sum;
   }
 }
+// (rounded to bf16 for the second product, see Weights)
 __device__ inline frag pack_weights(floatx4 x, floatx4 y) {
   return __builtin_bit_cast(frag, make_uint4(round2(x[0], x[1]), round2(x[2], x[3]), round2(y[0], y[1]), round2(y[2], y[3])));
 }
