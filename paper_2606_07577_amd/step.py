@@ -226,19 +226,21 @@ class StreamRunner:
     def _behind(self, stream):
         """The stream (default: the current one) for work on the caches, made
         to wait for what came before on another one: steps, hold() and
-        restore(), and what the current stream did with the caches' views."""
+        restore(), and what the current stream did with the caches' views.  A
+        stream that is captured may not wait for work outside its graph."""
         stream = stream if stream is not None else torch.cuda.current_stream()
         if self._last != stream:
+            with torch.cuda.stream(stream):
+                if torch.cuda.is_current_stream_capturing():
+                    return stream
             stream.wait_stream(self._last)
-        self._last = stream
+            self._last = stream
         return stream
 
     def _settle(self):
-        """The caches' sizes are known, their rows ordered for the current
-        stream (not into a capture, which may not wait for work outside it)."""
+        """The caches' sizes are known, their rows ordered for the current stream."""
         self.finish()
-        if not torch.cuda.is_current_stream_capturing():
-            self._behind(None)
+        self._behind(None)
 
     # buffers ------------------------------------------------------------
     def cache_k(self, l):
@@ -293,7 +295,7 @@ class StreamRunner:
         rows = self._held(held.data, held.rows)                # (refuses tensors that do not fit)
         stream = self._attention_stream(stream)
         with torch.cuda.stream(stream):
-            if not torch.cuda.is_current_stream_capturing():   # (a capture may not wait for work outside it)
+            if not torch.cuda.is_current_stream_capturing():   # (see _behind)
                 if held.ready is not None:
                     stream.wait_event(held.ready)
                 for data in held.data:
@@ -481,6 +483,8 @@ class HeldMemory:
     rows[l] kept rows, visual[l] of them visual (in front).  ready: the event
     behind what writes the data, or None if nothing has to be waited for;
     restore() and Reader wait for it."""
+
+    ready = None                                   # (of memories saved without one)
 
     def __init__(self, data, rows, visual, ready=None):
         self.data, self.rows, self.visual, self.ready = data, rows, visual, ready

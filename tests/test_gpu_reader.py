@@ -555,3 +555,29 @@ def test_a_memory_is_copied_and_one_in_host_memory_refused():
         run.restore(HeldMemory([x.cpu() for x in held.data], held.rows, held.visual))
     assert run.n_cache == held.rows and all(torch.equal(run.cache_k(l), before[l]) for l in range(layers))
     run.close()
+
+
+def test_a_memory_brought_back_in_a_graph():
+    """restore() captured behind steps on another stream, and replayed with eager work between."""
+    layers, h_q, h_kv, d, n = 2, 4, 2, 64, 160
+    g = torch.Generator(device="cuda").manual_seed(19)
+    run = StreamRunner(layers, h_q, h_kv, d, n, 200)
+    run.push(stream_chunk(g, layers, h_q, h_kv, d, n))
+    held = run.hold()
+    run.restore(held)
+    want = [t.clone() for l in range(layers) for t in (run.cache_k(l), run.cache_v(l), run.cache_modality(l))]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run.restore(held)
+        views = [t for l in range(layers) for t in (run.cache_k(l), run.cache_v(l), run.cache_modality(l))]
+    for i in range(3):
+        for t in views:
+            t.fill_(1)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(views, want))
+    run.push(stream_chunk(g, layers, h_q, h_kv, d, n))
+    assert sum(run.n_cache) == 200
+    run.close()
