@@ -501,7 +501,9 @@ class Reader:
 
     A model calls layer() for each of its layers with the projections of the
     streams' next tokens (a prompt's, or one each), in order, and next() after
-    the last layer.  `capacity`: tail rows of a stream.
+    the last layer.  `capacity`: tail rows of a stream.  Calls on different HIP
+    streams are the caller's to order (they share the tails and a handle); what
+    the constructor fills, and the memories, are there before it returns.
 
     The calls' descriptors are made once; layer() sets what changes.  Where
     every stream has the same number of tokens it takes the streams' tensors

@@ -581,3 +581,49 @@ def test_a_memory_brought_back_in_a_graph():
     run.push(stream_chunk(g, layers, h_q, h_kv, d, n))
     assert sum(run.n_cache) == 200
     run.close()
+
+
+def test_a_readers_and_a_steps_calls_in_graphs():
+    """A token's layer, and a chunk's attention with the scores behind it, captured once and replayed on new inputs."""
+    h_q, h_kv, d, layers = 4, 2, 64, 2
+    g = torch.Generator(device="cuda").manual_seed(20)
+    rnd = lambda *s: torch.randn(*s, generator=g, device="cuda").bfloat16()
+    attn = om.Attention(h_q, h_kv, d)
+    data = [torch.zeros(om.memory_shape(h_kv, d, 700), dtype=torch.uint8, device="cuda") for _ in range(layers)]
+    attn.omnimem_pack([om.make_held(rnd(h_kv, 700, d), rnd(h_kv, 700, d), x) for x in data])
+    memory = HeldMemory(data, [700] * layers, [350] * layers)
+    rope = om.make_rope(d, [0.5 ** j for j in range(32)])
+    captured, eager = (Reader([memory], h_q, h_kv, d, rope, 8) for _ in range(2))
+    q, k, v = rnd(layers, h_q, 1, d), rnd(layers, h_kv, 1, d), rnd(layers, h_kv, 1, d)
+    pos = torch.zeros(1, 1, dtype=torch.int32, device="cuda")
+    token = lambda r: [r.layer(l, [q[l]], [k[l]], [v[l]], [pos])[0] for l in range(layers)]
+    layer = synth.make_layer([9, 1], h_q=h_q, h_kv=h_kv, d=d, n_cache_v=300, n_cache_a=30, n_frames=2, frame_v=60, frame_a=5,
+                             dup_frac=0.3, head_scale=(0.5, 2.0), dtype="bf16")
+    steps = [DeviceStep([layer], 80) for _ in range(2)]
+    for s in steps:
+        s.attend()
+        s.score()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = token(captured)
+        steps[0].attend()
+        steps[0].score()
+    for i in range(4):
+        for t in (q, k, v):
+            t.copy_(rnd(*t.shape))
+        pos.fill_(700 + 11 * i)
+        fresh = rnd(*steps[0].q[0].shape)
+        for s in steps:
+            s.q[0].copy_(fresh)
+            s.a.fill_(7.0)
+        torch.cuda.synchronize()
+        graph.replay()
+        want = token(eager)
+        steps[1].attend()
+        steps[1].score()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, want)) and torch.equal(captured.k, eager.k)
+        assert torch.equal(steps[0].attn_out[0], steps[1].attn_out[0]) and torch.equal(steps[0].a, steps[1].a)
+    for x in (captured, eager, attn, *steps):
+        x.close()
