@@ -531,6 +531,100 @@ typedef struct {
 omnimem_status omnimem_attend(omnimem_attn* attn, const omnimem_query* seqs, int32_t n, int32_t causal,
                               hipStream_t stream);
 
+/* ---------------------------------------------------------------------------
+ * Caches in pages: answers that grow, each by its own, share one store of
+ * pages instead of a run of rows of one capacity each.
+ *
+ *   omnimem_rotate_pages   omnimem_rotate into pages;
+ *   omnimem_attend_pages   omnimem_attend over tail rows in pages, with a sliding
+ *                          window and first rows that stay visible, or of a
+ *                          tree of drafted tokens;
+ *   omnimem_keep_pages     the accepted drafts' rows become the cache's next.
+ *
+ * A sequence's row r lies on page table[r / page_rows], row r % page_rows of it,
+ * with table [ceil(rows / page_rows)] in DEVICE memory, read when the call runs:
+ * one table serves every layer, and a captured graph may be replayed with other
+ * pages in it.  An entry that is negative or not below n_pages is no page: rows
+ * on it are not written and not seen.  Two sequences may read the same pages;
+ * rows that a call writes must lie on pages that no other sequence of the call
+ * has.  Handle and conventions are those above. */
+typedef struct {
+  void* k;                  /* [n_pages][H_kv][page_rows][d]                   */
+  void* v;
+  int64_t page_stride, head_stride, row_stride;  /* elements, shared by k and v, nested in any order; rows less than 16 MiB apart */
+  int32_t n_pages;
+  int32_t page_rows;        /* 16, 32, 64, 128 or 256                          */
+} omnimem_pages;
+
+/* One sequence's projected rows and the first of its cache that they become. */
+typedef struct {
+  const void* q;            /* [H_q][n_rows][d]                                */
+  int64_t q_head_stride, q_row_stride;
+  const void* k;            /* [H_kv][n_rows][d]                               */
+  const void* v;
+  int64_t kv_head_stride, kv_row_stride;   /* elements, shared by k and v      */
+  const int32_t* pos;       /* [n_axes][n_rows] positions                      */
+  int64_t pos_stride;       /* elements between axes                           */
+  int64_t n_rows;
+  void* q_out;              /* [H_q][n_rows][d]                                */
+  int64_t q_out_head_stride, q_out_row_stride;
+  const int32_t* table;     /* the cache's pages, those of the new rows among them */
+  int64_t first_row;        /* rows first_row .. first_row + n_rows - 1 are written */
+} omnimem_paged_projection;
+
+/* What omnimem_rotate does, its keys and values going to pages.  q_out is q
+ * (same pointer and strides) or overlaps no input; neither overlaps the pages.
+ * Errors: INVALID_ARG, UNSUPPORTED (rotary_dim not a multiple of 16, page_rows). */
+omnimem_status omnimem_rotate_pages(omnimem_attn* attn, const omnimem_rope* rope, const omnimem_pages* pages,
+                                    const omnimem_paged_projection* seqs, int32_t n, hipStream_t stream);
+
+/* One sequence's queries and the rows that they attend to: those of an
+ * optional memory, then the cache's first n_tail rows (the queries' own last). */
+typedef struct {
+  const void* q;            /* [H_q][n_queries][d]                             */
+  int64_t q_head_stride, q_row_stride;
+  int64_t n_queries;
+  const void* memory;       /* or NULL                                         */
+  int64_t memory_head_stride; /* bytes, a multiple of 16                       */
+  int64_t memory_rows;      /* 0 without a memory                              */
+  const int32_t* table;     /* or NULL without tail rows                       */
+  int64_t n_tail;
+  const uint64_t* tree;     /* optional DEVICE [n_queries]: the last n_queries (at most 64) tail rows are drafts */
+  float sm_scale;           /* 0 -> 1/sqrt(d)                                   */
+  void* out;                /* [H_q][n_queries][d]                             */
+  int64_t out_head_stride, out_row_stride;
+  float* lse;               /* optional [H_q][n_queries] fp32                  */
+  int64_t lse_head_stride;  /* elements                                        */
+} omnimem_paged_query;
+
+/* omnimem_attend over pages.  Query i sees every memory row.  Without `tree` it
+ * stands at row p = n_tail - n_queries + i of the tail and sees the rows j <= p
+ * that have j > p - window or j < sinks; window 0: all rows j <= p.  With `tree`
+ * it sees of the drafts those b whose bit 1 << b is set in tree[i] (its own among
+ * them or not; bits from n_queries on are not looked at), stands at row p =
+ * n_tail - n_queries + (drafts that it sees) - 1, as many rows on as its branch is
+ * long, and sees of the rows before the drafts those with j > p - window or
+ * j < sinks.  Pages that no query of a row tile sees are not read: entries of
+ * pages behind every window may be anything.  All else as omnimem_attend. */
+omnimem_status omnimem_attend_pages(omnimem_attn* attn, const omnimem_pages* pages, const omnimem_paged_query* seqs,
+                                    int32_t n, int64_t window, int64_t sinks, hipStream_t stream);
+
+/* One sequence's accepted drafts. */
+typedef struct {
+  const int32_t* table;
+  int64_t first_row;        /* the cache's row of the first draft              */
+  const uint8_t* path;      /* HOST [n_kept], ascending, below 64              */
+  int32_t n_kept;           /* 0 .. 64                                         */
+} omnimem_path;
+
+/* Row first_row + path[i] becomes row first_row + i, for i = 0 .. n_kept - 1, of
+ * every KV head of each of `n_layers` stores (alike but for k and v), in one
+ * launch.  Rows behind the kept ones are left as they are, but for those that
+ * are written.  Of a row without a page, and to one, nothing is moved.
+ * Errors: INVALID_ARG, UNSUPPORTED (page_rows). */
+omnimem_status omnimem_keep_pages(omnimem_attn* attn, const omnimem_pages* layers, int32_t n_layers,
+                                  const omnimem_path* seqs, int32_t n, hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

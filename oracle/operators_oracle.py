@@ -102,3 +102,49 @@ def attend(q, k, v, held, scale, causal):
             size[h, i] = p @ np.abs(vv[:rows])
             reach[h, i] = (np.abs(kk[:rows]) @ np.abs(q[h, i])).max() * abs(scale)
     return out, lse, size, reach
+
+
+def paged(pool, table, n, page_rows):
+    """The first n rows [h, n, d] of a cache on pages pool [pages, h, page_rows, d], and whether each has a page."""
+    r = np.arange(n)
+    page = np.asarray(table)[r // page_rows] if n else np.zeros(0, np.int64)
+    there = (page >= 0) & (page < len(pool))
+    return pool[np.where(there, page, 0), :, r % page_rows].transpose(1, 0, 2), there
+
+
+def paged_seen(n, tail, window, sinks, masks=None):
+    """see [n, tail]: whether query i sees tail row j (window 0: all that come before); masks: of drafts, n integers."""
+    see = np.zeros((n, tail), bool)
+    for i in range(n):
+        first = tail if masks is None else tail - n
+        drafts = [] if masks is None else [b for b in range(n) if masks[i] >> b & 1]
+        p = tail - n + (i if masks is None else len(drafts) - 1)
+        for j in range(min(p + 1, first)):
+            see[i, j] = window == 0 or j > p - window or j < sinks
+        for b in drafts:
+            see[i, first + b] = True
+    return see
+
+
+def attend_seen(q, k, v, see, scale):
+    """attend for the rows see [n, rows] of k, v [h_kv, rows, d]."""
+    h_q, n, d = q.shape
+    group = h_q // k.shape[0]
+    out, lse = np.zeros((h_q, n, d)), np.full((h_q, n), -np.inf)
+    size, reach = np.zeros((h_q, n, d)), np.zeros((h_q, n))
+    for h in range(h_q):
+        for i in range(n):
+            kk, vv = k[h // group][see[i]], v[h // group][see[i]]
+            if len(kk) == 0:
+                continue
+            s = kk @ q[h, i] * scale
+            m = s.max()
+            if m == -np.inf:
+                continue
+            p = np.exp(s - m)
+            lse[h, i] = m + np.log(p.sum())
+            p /= p.sum()
+            out[h, i] = p @ vv
+            size[h, i] = p @ np.abs(vv)
+            reach[h, i] = (np.abs(kk) @ np.abs(q[h, i])).max() * abs(scale)
+    return out, lse, size, reach

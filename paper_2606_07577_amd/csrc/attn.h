@@ -92,6 +92,9 @@ struct RotateSeq {
 };
 template <int N>
 struct RotateArgs {
+  static constexpr int kSeqs = N;
+  static constexpr bool kPaged = false;
+  using One = RotateArgs<1>;
   RotateSeq seq[N];
   double turns[64];            // inv_freq / 2 pi
   uint8_t axis[64];
@@ -131,6 +134,9 @@ struct QuerySeq {
 // split (with whole > 0 all others are by the same number).
 template <int N>
 struct AttendArgs {
+  static constexpr int kSeqs = N;
+  static constexpr bool kPaged = false;
+  using One = AttendArgs<1>;
   QuerySeq seq[N];
   int32_t unit0[N];            // a sequence's first unit after the whole row tiles (whole = 0), or row tile
   int n_seqs, h_kv, group, causal, whole, units;
@@ -142,11 +148,79 @@ struct AttendArgs {
 static_assert(sizeof(RotateArgs<kRotatesPerLaunch>) <= 3968 && sizeof(HeldArgs) <= 3968 && sizeof(AttendArgs<kQueriesPerLaunch>) <= 3968,
               "a kernel's arguments, with what the runtime adds, stay below 4 KiB");
 
+// A cache in pages, in bytes.  Row r of a sequence is row r % (1 << shift) of
+// page table[r >> shift]; an entry that is not below n_pages is no page.
+struct PagePool {
+  char* k; char* v;
+  int64_t page, head;          // from a page (a head) to the next
+  uint32_t row;                // below 2^24
+  uint32_t n_pages;
+  int shift;                   // 4 to 8: 16 rows from a multiple of 16 lie on one page
+};
+// Byte of a head's row of the cache from that head's first row on page 0, below
+// 0 if it has no page (a store spans less than 64 TiB).
+__device__ inline int64_t paged_row(const PagePool& pool, const int32_t* table, int row) {
+  const uint32_t entry = gload<uint32_t>(table + (row >> pool.shift));
+  return entry < pool.n_pages ? entry * pool.page + (row & ((1 << pool.shift) - 1)) * (int64_t)pool.row : INT64_MIN;
+}
+struct PagedRotateSeq {
+  const void* q; const void* k; const void* v;
+  const int32_t* pos;
+  void* q_out;
+  const int32_t* table;
+  int64_t pos_s;
+  uint32_t q_hs, q_rs, kv_hs, kv_rs, qo_hs, qo_rs;   // units of 16 bytes
+  int32_t first, n;
+};
+template <int N>
+struct PagedRotateArgs {
+  static constexpr int kSeqs = N;
+  static constexpr bool kPaged = true;
+  using One = PagedRotateArgs<1>;
+  PagedRotateSeq seq[N];
+  PagePool pool;
+  double turns[64];
+  uint8_t axis[64];
+  const void* q_w; const void* k_w;
+  float eps;
+  int rot, neighbours, h_q, h_kv;
+};
+constexpr int kPagedRotatesPerLaunch = 32;
+
+// Accepted drafts: `skip` rows are in their place, the others move.
+constexpr int kKeptPerLaunch = 36, kStoresPerLaunch = 32, kMaxDrafts = 64;
+struct KeptSeq {
+  const int32_t* table;
+  int32_t first;
+  uint8_t skip, n;
+  uint8_t path[kMaxDrafts];
+};
+struct KeepArgs {
+  KeptSeq seq[kKeptPerLaunch];
+  char* k[kStoresPerLaunch];
+  char* v[kStoresPerLaunch];
+  PagePool pool;               // (k, v: not used)
+};
+static_assert(sizeof(PagedRotateArgs<kPagedRotatesPerLaunch>) <= 3968 && sizeof(KeepArgs) <= 3968, "as above");
+
+// Attention's arguments for tail rows in pages: a sequence's `k` is its table and its `v`
+// its drafts' masks, or null.
+template <int N>
+struct PagedArgs : AttendArgs<N> {
+  static constexpr bool kPaged = true;
+  using One = PagedArgs<1>;
+  PagePool pool;
+  int32_t window, sinks;       // at most 2^30
+};
+static_assert(sizeof(PagedArgs<kQueriesPerLaunch>) <= 3968, "as above");
+
 struct AttnDims {
   int h_q, h_kv, group, d, dtype;
 };
 // (a: room for the most; the launch takes what n sequences need)
 hipError_t launch_rotate(const AttnDims& dm, const RotateArgs<kRotatesPerLaunch>& a, int n, hipStream_t st);
+hipError_t launch_rotate_pages(const AttnDims& dm, const PagedRotateArgs<kPagedRotatesPerLaunch>& a, int n, hipStream_t st);
+hipError_t launch_keep(const AttnDims& dm, const KeepArgs& a, int n, int stores, hipStream_t st);
 hipError_t launch_hold(const AttnDims& dm, const HeldArgs& a, int n, bool pack, hipStream_t st);
 // Workspace of a handle: partials, then a counter for each (all 0 at first).
 constexpr int64_t kPartBytes = (int64_t)128 << 20, kMaxPartials = 32768;
@@ -154,5 +228,7 @@ constexpr int64_t kPartBytes = (int64_t)128 << 20, kMaxPartials = 32768;
 hipError_t prepare_attend(const AttnDims& dm);
 // Fills the plan fields of `a` for n sequences and launches their attention.
 hipError_t launch_attend(const AttnDims& dm, AttendArgs<kQueriesPerLaunch>& a, int n, int compute_units, void* workspace, hipStream_t st);
+hipError_t prepare_attend_pages(const AttnDims& dm);
+hipError_t launch_attend_pages(const AttnDims& dm, PagedArgs<kQueriesPerLaunch>& a, int n, int compute_units, void* workspace, hipStream_t st);
 
 }  // namespace omnimem

@@ -32,6 +32,7 @@ EXPORTED = [
     "omnimem_append", "omnimem_allocate_noalloc", "omnimem_set_topk_path",
     "omnimem_attn_create", "omnimem_attn_destroy", "omnimem_attn_last_error", "omnimem_rotate", "omnimem_pack",
     "omnimem_unpack", "omnimem_memory_bytes", "omnimem_attend",
+    "omnimem_rotate_pages", "omnimem_attend_pages", "omnimem_keep_pages",
 ]
 
 
@@ -116,6 +117,38 @@ class Query(ctypes.Structure):
     ]
 
 
+class Pages(ctypes.Structure):
+    _fields_ = [
+        ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("page_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
+        ("row_stride", ctypes.c_int64), ("n_pages", ctypes.c_int32), ("page_rows", ctypes.c_int32),
+    ]
+
+
+class PagedProjection(ctypes.Structure):
+    _fields_ = [
+        ("q", ctypes.c_void_p), ("q_head_stride", ctypes.c_int64), ("q_row_stride", ctypes.c_int64),
+        ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("kv_head_stride", ctypes.c_int64),
+        ("kv_row_stride", ctypes.c_int64), ("pos", ctypes.c_void_p), ("pos_stride", ctypes.c_int64),
+        ("n_rows", ctypes.c_int64), ("q_out", ctypes.c_void_p), ("q_out_head_stride", ctypes.c_int64),
+        ("q_out_row_stride", ctypes.c_int64), ("table", ctypes.c_void_p), ("first_row", ctypes.c_int64),
+    ]
+
+
+class PagedQuery(ctypes.Structure):
+    _fields_ = [
+        ("q", ctypes.c_void_p), ("q_head_stride", ctypes.c_int64), ("q_row_stride", ctypes.c_int64),
+        ("n_queries", ctypes.c_int64), ("memory", ctypes.c_void_p), ("memory_head_stride", ctypes.c_int64),
+        ("memory_rows", ctypes.c_int64), ("table", ctypes.c_void_p), ("n_tail", ctypes.c_int64), ("tree", ctypes.c_void_p),
+        ("sm_scale", ctypes.c_float), ("out", ctypes.c_void_p), ("out_head_stride", ctypes.c_int64),
+        ("out_row_stride", ctypes.c_int64), ("lse", ctypes.c_void_p), ("lse_head_stride", ctypes.c_int64),
+    ]
+
+
+class Path(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("first_row", ctypes.c_int64), ("path", ctypes.POINTER(ctypes.c_uint8)),
+                ("n_kept", ctypes.c_int32)]
+
+
 class KernelTime(ctypes.Structure):
     _fields_ = [("name", ctypes.c_char * 32), ("launches", ctypes.c_int32), ("total_ms", ctypes.c_double)]
 
@@ -185,6 +218,13 @@ def load_library(path=LIB_PATH):
     lib.omnimem_memory_bytes.restype = ctypes.c_int64
     lib.omnimem_attend.argtypes = [vp, ctypes.POINTER(Query), ctypes.c_int32, ctypes.c_int32, vp]
     lib.omnimem_attend.restype = i32
+    lib.omnimem_rotate_pages.argtypes = [vp, ctypes.POINTER(Rope), ctypes.POINTER(Pages), ctypes.POINTER(PagedProjection),
+                                         ctypes.c_int32, vp]
+    lib.omnimem_rotate_pages.restype = i32
+    lib.omnimem_attend_pages.argtypes = [vp, ctypes.POINTER(Pages), ctypes.POINTER(PagedQuery), ctypes.c_int32, i64, i64, vp]
+    lib.omnimem_attend_pages.restype = i32
+    lib.omnimem_keep_pages.argtypes = [vp, ctypes.POINTER(Pages), ctypes.c_int32, ctypes.POINTER(Path), ctypes.c_int32, vp]
+    lib.omnimem_keep_pages.restype = i32
     _lib = lib
     return lib
 
@@ -384,6 +424,8 @@ def make_chunk(k, v, modality):
 
 
 MEMORY_ROWS = 32   # rows of a memory block
+PAGE_ROWS = (16, 32, 64, 128, 256)   # rows that a page may have
+MAX_DRAFTS = 64    # drafted tokens of a tree
 
 
 class _Layout(typing.NamedTuple):
@@ -400,6 +442,8 @@ def array_of(descriptors):
     """A ctypes array of descriptors of one type: built once, passed to any number of calls."""
     arr = (type(descriptors[0]) * len(descriptors))(*descriptors)
     arr._layouts = {d._layout for d in descriptors if hasattr(d, "_layout")}
+    arr._rows = max((d._table_rows for d in descriptors if hasattr(d, "_table_rows")), default=0)
+    arr._kept = [d._path for d in descriptors if hasattr(d, "_path")]    # (host arrays, kept alive with the descriptors)
     return arr
 
 
@@ -544,6 +588,119 @@ def make_query(q, out, k=None, v=None, memory=None, memory_rows=0, sm_scale=0.0,
     return x
 
 
+def make_pages(k, v):
+    """Descriptor of a store of pages k, v [n_pages, H_kv, page_rows, d] (any strides, the channels contiguous)."""
+    for t in (k, v):
+        if t.dim() != 4 or t.stride(3) != 1 or t.dtype not in (torch.bfloat16, torch.float32):
+            raise ValueError("pages must be [n_pages, H_kv, page_rows, d], bf16 or fp32, their channels contiguous")
+    if k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype:
+        raise ValueError("k and v must share shape, strides and type")
+    _one_device(k, v)
+    p = Pages()
+    p.k, p.v, p.n_pages, p.page_rows = _ptr(k), _ptr(v), k.shape[0], k.shape[2]
+    p.page_stride, p.head_stride, p.row_stride = k.stride()[:3]
+    p._layout = _Layout(None, k.shape[1], k.shape[3], k.dtype, k.device.index)
+    return p
+
+
+def _table(table, rows):
+    """A sequence's table of pages, int32 [>= ceil(rows / page_rows)]: the rows of the smallest page that it is long enough with."""
+    if table.dtype != torch.int32 or table.dim() != 1 or (table.stride(0) != 1 and table.shape[0] > 1):
+        raise ValueError("a table is int32 [pages], contiguous")
+    need = [p for p in PAGE_ROWS if table.shape[0] * p >= rows]
+    if not need:
+        raise ValueError(f"a table of {table.shape[0]} pages does not hold {rows} rows")
+    return need[0]
+
+
+def make_paged_projection(q, k, v, pos, q_out, table, first_row):
+    """Descriptor of a sequence's projected rows q [H_q, n, d], k, v [H_kv, n, d] at positions pos int32 [axes, n]: the
+    rotated queries go to q_out [H_q, n, d], keys and values to the cache's rows from first_row on, on the pages of table
+    (int32, one entry for each page of the cache)."""
+    n = k.shape[1]
+    for what, group in (("q", (q,)), ("k and v", (k, v)), ("q_out", (q_out,))):
+        _rows(what, *group)
+    if q_out.shape != q.shape or q.shape[1:] != k.shape[1:]:
+        raise ValueError("q_out must have q's shape, k and v its rows and width")
+    if len({t.dtype for t in (q, k, q_out)}) != 1:
+        raise TypeError("rows must have one type")
+    if pos.dtype != torch.int32 or pos.dim() != 2 or pos.shape[1] != n or (pos.stride(1) != 1 and n > 1):
+        raise ValueError("pos must be int32 [axes, n], its positions contiguous")
+    _one_device(q, k, v, pos, q_out, table)
+    p = PagedProjection()
+    p._table_rows = _table(table, int(first_row) + n)
+    p.q, p.q_head_stride, p.q_row_stride = _ptr(q), q.stride(0), q.stride(1)
+    p.k, p.v, p.kv_head_stride, p.kv_row_stride = _ptr(k), _ptr(v), k.stride(0), k.stride(1)
+    p.pos, p.pos_stride, p.n_rows = _ptr(pos), pos.stride(0), n
+    p.q_out, p.q_out_head_stride, p.q_out_row_stride = _ptr(q_out), q_out.stride(0), q_out.stride(1)
+    p.table, p.first_row = _ptr(table), int(first_row)
+    p._layout = _Layout(q.shape[0], k.shape[0], q.shape[2], q.dtype, q.device.index, pos.shape[0])
+    return p
+
+
+def make_paged_query(q, out, table=None, n_tail=0, memory=None, memory_rows=0, tree=None, sm_scale=0.0, lse=None):
+    """Descriptor of a sequence's queries q [H_q, n, d], their results out [H_q, n, d] (lse fp32 [H_q, n]) and the rows
+    they attend to: memory_rows rows of an optional memory, then the cache's first n_tail rows, on the pages of table
+    (int32).  tree: int64 [n], the masks of the last n tail rows' tree (see tree_masks)."""
+    _rows("q", q)
+    _rows("out", out)
+    if out.shape != q.shape or out.dtype != q.dtype:
+        raise ValueError("out must have q's shape and type")
+    n = q.shape[1]
+    if memory is not None:
+        _memory(memory, int(memory_rows))
+        if memory.shape[2] != 34 * q.shape[2]:
+            raise ValueError("the memory's width differs from the queries'")
+    elif memory_rows:
+        raise ValueError("memory_rows without a memory")
+    if lse is not None and (lse.dtype != torch.float32 or lse.shape != q.shape[:2] or lse.stride(1) != 1):
+        raise ValueError("lse must be fp32 [H_q, n], its queries contiguous")
+    if tree is not None and (tree.dtype != torch.int64 or tree.shape != (n,) or (tree.stride(0) != 1 and n > 1)):
+        raise ValueError("tree must be contiguous int64 [n]")
+    if n_tail and table is None:
+        raise ValueError("tail rows without a table")
+    _one_device(q, out, table, memory, tree, lse)
+    x = PagedQuery()
+    x.q, x.q_head_stride, x.q_row_stride, x.n_queries = _ptr(q), q.stride(0), q.stride(1), n
+    x.out, x.out_head_stride, x.out_row_stride = _ptr(out), out.stride(0), out.stride(1)
+    x.sm_scale, x.n_tail, x.tree = float(sm_scale), int(n_tail), _ptr(tree)
+    if table is not None:
+        x._table_rows = _table(table, int(n_tail))
+        x.table = _ptr(table)
+    if memory is not None:
+        x.memory, x.memory_head_stride, x.memory_rows = _ptr(memory), memory.stride(0), int(memory_rows)
+    if lse is not None:
+        x.lse, x.lse_head_stride = _ptr(lse), lse.stride(0)
+    x._layout = _Layout(q.shape[0], memory.shape[0] if memory is not None else None, q.shape[2], q.dtype, q.device.index)
+    return x
+
+
+def tree_masks(parents):
+    """The masks of a tree of drafts from each one's parent (before it; -1: it follows the cache): draft i sees itself and
+    those that it follows.  A list of integers as int64 holds their 64 bits."""
+    masks = []
+    if len(parents) > MAX_DRAFTS:
+        raise ValueError(f"at most {MAX_DRAFTS} drafts")
+    for i, parent in enumerate(parents):
+        if not -1 <= parent < i:
+            raise ValueError(f"draft {i} has parent {parent}: -1 or a draft before it is needed")
+        masks.append((masks[parent] if parent >= 0 else 0) | 1 << i)
+    return [m - (m >> 63 << 64) for m in masks]
+
+
+def make_path(table, first_row, path):
+    """Descriptor of a sequence's accepted drafts: the cache's rows first_row + path[i] become rows first_row + i."""
+    path = [int(i) for i in path]
+    if any(not 0 <= i < MAX_DRAFTS for i in path) or any(a >= b for a, b in zip(path, path[1:])):
+        raise ValueError(f"a path ascends, below {MAX_DRAFTS}")
+    p = Path()
+    p._table_rows = _table(table, int(first_row) + (path[-1] + 1 if path else 0))
+    p._path = (ctypes.c_uint8 * max(1, len(path)))(*path)
+    p.table, p.first_row, p.path, p.n_kept = _ptr(table), int(first_row), p._path, len(path)
+    p._layout = _Layout(device=table.device.index)
+    return p
+
+
 class Attention:
     """An omnimem_attn: the operators around the compression step for one head layout, on the current device.  Calls
     take lists of descriptors or arrays from array_of, one entry per sequence, of tensors on that device."""
@@ -596,6 +753,40 @@ class Attention:
 
     def omnimem_attend(self, queries, causal=True, stream=None):
         self._call(self._lib.omnimem_attend, queries, Query, int(bool(causal)), stream=stream)
+
+    def omnimem_rotate_pages(self, rope, pages, projections, stream=None):
+        self._check_layouts(getattr(rope, "_layouts", frozenset()))
+        for layout in getattr(projections, "_layouts", None) or {p._layout for p in projections if hasattr(p, "_layout")}:
+            if layout.axes < rope.n_axes:
+                raise ValueError(f"the rope has {rope.n_axes} axes, a projection positions for {layout.axes}")
+        projections = self._paged(pages, projections, PagedProjection)
+        self._call(self._lib.omnimem_rotate_pages, projections, PagedProjection, before=(ctypes.byref(rope), ctypes.byref(pages)),
+                   stream=stream)
+
+    def omnimem_attend_pages(self, pages, queries, window=0, sinks=0, stream=None):
+        queries = self._paged(pages, queries, PagedQuery)
+        self._call(self._lib.omnimem_attend_pages, queries, PagedQuery, int(window), int(sinks), before=(ctypes.byref(pages),),
+                   stream=stream)
+
+    def omnimem_keep_pages(self, layers, paths, stream=None):
+        """layers: a list of Pages or an array from array_of, alike but for their rows' places."""
+        if not (isinstance(layers, ctypes.Array) and layers._type_ is Pages):
+            layers = array_of(layers) if len(layers) else None
+        if layers is None:
+            return
+        self._check_layouts(getattr(layers, "_layouts", frozenset()))
+        paths = self._paged(layers[0], paths, Path, check=False)
+        self._call(self._lib.omnimem_keep_pages, paths, Path, before=(layers, len(layers)), stream=stream)
+
+    def _paged(self, pages, descriptors, kind, check=True):
+        """The descriptors as an array, their tables long enough for these pages."""
+        if check and hasattr(pages, "_layout"):
+            self._check_layouts({pages._layout})
+        if not (isinstance(descriptors, ctypes.Array) and descriptors._type_ is kind):
+            descriptors = array_of(descriptors) if len(descriptors) else None
+        if getattr(descriptors, "_rows", 0) > pages.page_rows:
+            raise ValueError(f"a table is too short for pages of {pages.page_rows} rows")
+        return descriptors if descriptors is not None else []
 
     def close(self):
         if self.handle:
