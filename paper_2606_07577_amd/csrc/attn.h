@@ -92,9 +92,6 @@ struct RotateSeq {
 };
 template <int N>
 struct RotateArgs {
-  static constexpr int kSeqs = N;
-  static constexpr bool kPaged = false;
-  using One = RotateArgs<1>;
   RotateSeq seq[N];
   double turns[64];            // inv_freq / 2 pi
   uint8_t axis[64];
@@ -158,9 +155,13 @@ struct PagePool {
   int shift;                   // 4 to 8: 16 rows from a multiple of 16 lie on one page
 };
 // Byte of a head's row of the cache from that head's first row on page 0, below
-// 0 if it has no page (a store spans less than 64 TiB).
+// 0 if it has no page (a store spans less than 64 TiB).  SAME: of one row in
+// every lane, whose entry is a scalar load.
+template <bool SAME>
 __device__ inline int64_t paged_row(const PagePool& pool, const int32_t* table, int row) {
-  const uint32_t entry = gload<uint32_t>(table + (row >> pool.shift));
+  uint32_t entry;
+  if constexpr (SAME) entry = ((const __attribute__((address_space(4))) uint32_t*)(uintptr_t)table)[uniform(row) >> pool.shift];
+  else entry = gload<uint32_t>(table + (row >> pool.shift));
   return entry < pool.n_pages ? entry * pool.page + (row & ((1 << pool.shift) - 1)) * (int64_t)pool.row : INT64_MIN;
 }
 struct PagedRotateSeq {
@@ -174,16 +175,14 @@ struct PagedRotateSeq {
 };
 template <int N>
 struct PagedRotateArgs {
-  static constexpr int kSeqs = N;
-  static constexpr bool kPaged = true;
-  using One = PagedRotateArgs<1>;
   PagedRotateSeq seq[N];
   PagePool pool;
   double turns[64];
   uint8_t axis[64];
   const void* q_w; const void* k_w;
   float eps;
-  int rot, neighbours, h_q, h_kv;
+  int rot, neighbours, h_q, h_kv, n_axes;
+  int waves;                   // to a token
 };
 constexpr int kPagedRotatesPerLaunch = 32;
 

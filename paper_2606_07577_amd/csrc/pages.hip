@@ -24,8 +24,8 @@ __global__ __launch_bounds__(256) void keep_rows(KeepArgs a, int chunks, int ite
 #pragma unroll
     for (int i = 0; i < kRowsAhead; ++i) {
       const int j = min(i0 + i, s.n - 1);
-      from[i] = paged_row(a.pool, s.table, s.first + s.path[j]);
-      to[i] = paged_row(a.pool, s.table, s.first + j);
+      from[i] = paged_row<true>(a.pool, s.table, s.first + s.path[j]);
+      to[i] = paged_row<true>(a.pool, s.table, s.first + j);
     }
 #pragma unroll
     for (int i = 0; i < kRowsAhead; ++i) x[i] = from[i] >= 0 ? gload16(base + from[i]) : make_uint4(0, 0, 0, 0);

@@ -64,6 +64,7 @@ omnimem_status omnimem_rotate_pages(omnimem_attn* attn, const omnimem_rope* rope
   Store store;
   if ((st = take_rope(attn, rope, a)) != OMNIMEM_OK || (st = take_pages(attn, pages, store)) != OMNIMEM_OK) return st;
   a.pool = store.pool;
+  a.n_axes = rope->n_axes;
   for (int i = 0; i < n; ++i) {
     const omnimem_paged_projection& s = seqs[i];
     if (s.n_rows < 0 || s.n_rows > kMaxRows || s.first_row < 0 || s.first_row > kMaxRows - s.n_rows)

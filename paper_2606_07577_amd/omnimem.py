@@ -442,8 +442,9 @@ def array_of(descriptors):
     """A ctypes array of descriptors of one type: built once, passed to any number of calls."""
     arr = (type(descriptors[0]) * len(descriptors))(*descriptors)
     arr._layouts = {d._layout for d in descriptors if hasattr(d, "_layout")}
-    arr._rows = max((d._table_rows for d in descriptors if hasattr(d, "_table_rows")), default=0)
-    arr._kept = [d._path for d in descriptors if hasattr(d, "_path")]    # (host arrays, kept alive with the descriptors)
+    # what calls on pages compare, and host arrays that are kept alive with the descriptors
+    arr._fit = frozenset().union(*[d._fit for d in descriptors if hasattr(d, "_fit")])
+    arr._kept = [d._path for d in descriptors if hasattr(d, "_path")]
     return arr
 
 
@@ -508,6 +509,7 @@ def make_rope(head_dim, inv_freq, axis=None, n_axes=None, rotary_dim=None, neigh
     r.q_weight, r.k_weight, r.eps = _ptr(q_weight), _ptr(k_weight), float(eps)
     r._weights = weights    # (kept alive with the descriptor)
     r._layouts = {_Layout(head_dim=head_dim)} | {_Layout(dtype=w.dtype, device=w.device.index) for w in weights}
+    r._fit = frozenset([("layout", x) for x in r._layouts] + [("axes", r.n_axes)])
     return r
 
 
@@ -600,6 +602,7 @@ def make_pages(k, v):
     p.k, p.v, p.n_pages, p.page_rows = _ptr(k), _ptr(v), k.shape[0], k.shape[2]
     p.page_stride, p.head_stride, p.row_stride = k.stride()[:3]
     p._layout = _Layout(None, k.shape[1], k.shape[3], k.dtype, k.device.index)
+    p._fit = frozenset([("layout", p._layout), ("page_rows", k.shape[2])])
     return p
 
 
@@ -628,13 +631,14 @@ def make_paged_projection(q, k, v, pos, q_out, table, first_row):
         raise ValueError("pos must be int32 [axes, n], its positions contiguous")
     _one_device(q, k, v, pos, q_out, table)
     p = PagedProjection()
-    p._table_rows = _table(table, int(first_row) + n)
+    rows = _table(table, int(first_row) + n)
     p.q, p.q_head_stride, p.q_row_stride = _ptr(q), q.stride(0), q.stride(1)
     p.k, p.v, p.kv_head_stride, p.kv_row_stride = _ptr(k), _ptr(v), k.stride(0), k.stride(1)
     p.pos, p.pos_stride, p.n_rows = _ptr(pos), pos.stride(0), n
     p.q_out, p.q_out_head_stride, p.q_out_row_stride = _ptr(q_out), q_out.stride(0), q_out.stride(1)
     p.table, p.first_row = _ptr(table), int(first_row)
     p._layout = _Layout(q.shape[0], k.shape[0], q.shape[2], q.dtype, q.device.index, pos.shape[0])
+    p._fit = frozenset([("layout", p._layout), ("rows", rows)])
     return p
 
 
@@ -664,14 +668,16 @@ def make_paged_query(q, out, table=None, n_tail=0, memory=None, memory_rows=0, t
     x.q, x.q_head_stride, x.q_row_stride, x.n_queries = _ptr(q), q.stride(0), q.stride(1), n
     x.out, x.out_head_stride, x.out_row_stride = _ptr(out), out.stride(0), out.stride(1)
     x.sm_scale, x.n_tail, x.tree = float(sm_scale), int(n_tail), _ptr(tree)
+    rows = 0
     if table is not None:
-        x._table_rows = _table(table, int(n_tail))
+        rows = _table(table, int(n_tail))
         x.table = _ptr(table)
     if memory is not None:
         x.memory, x.memory_head_stride, x.memory_rows = _ptr(memory), memory.stride(0), int(memory_rows)
     if lse is not None:
         x.lse, x.lse_head_stride = _ptr(lse), lse.stride(0)
     x._layout = _Layout(q.shape[0], memory.shape[0] if memory is not None else None, q.shape[2], q.dtype, q.device.index)
+    x._fit = frozenset([("layout", x._layout), ("rows", rows)])
     return x
 
 
@@ -694,10 +700,11 @@ def make_path(table, first_row, path):
     if any(not 0 <= i < MAX_DRAFTS for i in path) or any(a >= b for a, b in zip(path, path[1:])):
         raise ValueError(f"a path ascends, below {MAX_DRAFTS}")
     p = Path()
-    p._table_rows = _table(table, int(first_row) + (path[-1] + 1 if path else 0))
+    rows = _table(table, int(first_row) + (path[-1] + 1 if path else 0))
     p._path = (ctypes.c_uint8 * max(1, len(path)))(*path)
     p.table, p.first_row, p.path, p.n_kept = _ptr(table), int(first_row), p._path, len(path)
     p._layout = _Layout(device=table.device.index)
+    p._fit = frozenset([("layout", p._layout), ("rows", rows)])
     return p
 
 
@@ -718,6 +725,7 @@ class Attention:
         self.device = torch.cuda.current_device()
         self._layout = _Layout(n_q_heads, n_kv_heads, head_dim, torch.bfloat16 if dtype == BF16 else torch.float32, self.device)
         self._fits = set()      # layouts that were compared
+        self._paged_fits = set()
 
     def _check_layouts(self, layouts):
         for layout in layouts - self._fits:
@@ -755,38 +763,54 @@ class Attention:
         self._call(self._lib.omnimem_attend, queries, Query, int(bool(causal)), stream=stream)
 
     def omnimem_rotate_pages(self, rope, pages, projections, stream=None):
-        self._check_layouts(getattr(rope, "_layouts", frozenset()))
-        for layout in getattr(projections, "_layouts", None) or {p._layout for p in projections if hasattr(p, "_layout")}:
-            if layout.axes < rope.n_axes:
-                raise ValueError(f"the rope has {rope.n_axes} axes, a projection positions for {layout.axes}")
-        projections = self._paged(pages, projections, PagedProjection)
-        self._call(self._lib.omnimem_rotate_pages, projections, PagedProjection, before=(ctypes.byref(rope), ctypes.byref(pages)),
-                   stream=stream)
+        self._paged(self._lib.omnimem_rotate_pages, (rope, pages), projections, PagedProjection, stream=stream)
 
     def omnimem_attend_pages(self, pages, queries, window=0, sinks=0, stream=None):
-        queries = self._paged(pages, queries, PagedQuery)
-        self._call(self._lib.omnimem_attend_pages, queries, PagedQuery, int(window), int(sinks), before=(ctypes.byref(pages),),
-                   stream=stream)
+        self._paged(self._lib.omnimem_attend_pages, (pages,), queries, PagedQuery, int(window), int(sinks), stream=stream)
 
     def omnimem_keep_pages(self, layers, paths, stream=None):
         """layers: a list of Pages or an array from array_of, alike but for their rows' places."""
         if not (isinstance(layers, ctypes.Array) and layers._type_ is Pages):
             layers = array_of(layers) if len(layers) else None
-        if layers is None:
-            return
-        self._check_layouts(getattr(layers, "_layouts", frozenset()))
-        paths = self._paged(layers[0], paths, Path, check=False)
-        self._call(self._lib.omnimem_keep_pages, paths, Path, before=(layers, len(layers)), stream=stream)
+        if layers is not None:
+            self._paged(self._lib.omnimem_keep_pages, (layers,), paths, Path, stream=stream)
 
-    def _paged(self, pages, descriptors, kind, check=True):
-        """The descriptors as an array, their tables long enough for these pages."""
-        if check and hasattr(pages, "_layout"):
-            self._check_layouts({pages._layout})
+    def _paged(self, function, before, descriptors, kind, *more, stream=None):
+        """A call on pages: what its descriptors say of the handle, the rope and the tables is compared once for each
+        combination (a set of what was compared, not of the calls' arrays)."""
         if not (isinstance(descriptors, ctypes.Array) and descriptors._type_ is kind):
             descriptors = array_of(descriptors) if len(descriptors) else None
-        if getattr(descriptors, "_rows", 0) > pages.page_rows:
-            raise ValueError(f"a table is too short for pages of {pages.page_rows} rows")
-        return descriptors if descriptors is not None else []
+        fits = (getattr(descriptors, "_fit", None), *[getattr(x, "_fit", None) for x in before])
+        if fits not in self._paged_fits:
+            self._check_paged(fits)
+        args = [x if isinstance(x, ctypes.Array) else ctypes.byref(x) for x in before]
+        if kind is Path:
+            args.append(len(before[0]))
+        s = stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(self.device)
+        st = function(self.handle, *args, descriptors, len(descriptors) if descriptors is not None else 0, *more, s)
+        if st != OK:
+            raise OmnimemError(st, self._lib.omnimem_attn_last_error(self.handle).decode())
+
+    def _check_paged(self, fits):
+        layouts, known = set(), [f for f in fits if f is not None]
+        axes, short, page_rows = 0, 0, 0
+        for fit in known:
+            for what, value in fit:
+                if what == "layout":
+                    layouts.add(value)
+                elif what == "axes":
+                    axes = value
+                elif what == "rows":
+                    short = max(short, value)
+                else:
+                    page_rows = value
+        self._check_layouts(layouts)
+        for layout in layouts:
+            if layout.axes is not None and layout.axes < axes:
+                raise ValueError(f"the rope has {axes} axes, a projection positions for {layout.axes}")
+        if page_rows and short > page_rows:
+            raise ValueError(f"a table is too short for pages of {page_rows} rows")
+        self._paged_fits.add(fits)
 
     def close(self):
         if self.handle:
