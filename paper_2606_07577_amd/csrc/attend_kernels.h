@@ -1812,6 +1812,37 @@ int64_t plan_rounds(A& a, int64_t slots, int width, double ends, double partial)
   return splits == 1 ? 0 : rest;
 }
 
+// Sequences of different lengths, of which plan_rounds' equal splits would let
+// the longest end last: shares of the same number of key tiles, all row tiles in
+// their order, the number of them that takes least.  `width` units at a time
+// take as long as the longest share, more of them their average and half a share
+// to end.
+template <int R, int KT, class A>
+int64_t plan_lengths(A& a, int64_t slots, int width, double ends, double partial) {
+  int64_t most = 1;
+  for (int i = 0; i < a.n_seqs; ++i) most = std::max(most, (int64_t)tiles_of<KT>(a.seq[i].nm) + tiles_of<KT>(tail_rows<R>(a, a.seq[i])));
+  int64_t best = most;
+  double least = 1e30;
+  for (int64_t share = most;;) {
+    const Shares x = set_shares<R, KT>(a, share);
+    if (x.parts > slots || x.units > INT32_MAX) break;
+    const double whole = x.largest + ends, all = (x.tiles + ends * x.units) / width;
+    const double cost = (x.units <= width ? whole : all + whole / 2) + (x.parts > 0 ? ends + partial * x.parts : 0);
+    if (cost < least) {
+      least = cost;
+      best = share;
+    }
+    if (share == 1) break;
+    share = std::max<int64_t>(1, share - (share + 7) / 8);
+  }
+  a.whole = 0;
+  a.units = (int)set_shares<R, KT>(a, best).units;
+  int64_t joins = 0;
+  for (int i = 0; i < a.n_seqs; ++i)
+    if (a.seq[i].splits > 1) joins += (int64_t)a.h_kv * a.seq[i].row_tiles;
+  return joins;
+}
+
 // The arguments with room for one sequence.
 inline void first_of(const AttendArgs<kQueriesPerLaunch>& a, AttendArgs<1>& x) {
   x.seq[0] = a.seq[0];
@@ -1879,13 +1910,29 @@ hipError_t launch_shares(A& a, void* ws, int cus, One one, All all, hipStream_t 
   return launch<T, P, D>(a, ws, a.joined ? 0 : joins, splits, one, all, st);
 }
 
+// Whether some row tiles have a quarter more key tiles than they have on average.
+template <int R, int KT, class A>
+bool uneven(A& a) {
+  int64_t keys, most = 0;
+  const int64_t n = count_tiles<R, KT>(a, &keys);
+  for (int i = 0; i < a.n_seqs; ++i) most = std::max(most, (int64_t)tiles_of<KT>(a.seq[i].nm) + tiles_of<KT>(tail_rows<R>(a, a.seq[i])));
+  return 4 * most * n > 5 * keys;
+}
+
 // Many rows: units, and a join of the split row tiles.
 template <typename T, typename P, int D, class A, typename One, typename All>
 hipError_t launch_rounds(A& a, void* ws, int cus, double ends, double partial, One one, All all, hipStream_t st) {
-  const int64_t joins = plan_rounds<P::R, P::KT>(a, partials<P::R, D>(), cus, ends, partial);
+  int64_t joins = plan_rounds<P::R, P::KT>(a, partials<P::R, D>(), cus, ends, partial);
   if (joins < 0) return hipErrorInvalidConfiguration;
+  int splits = a.seq[0].splits;
+  if constexpr (A::kPaged) {
+    if (uneven<P::R, P::KT>(a)) {
+      joins = plan_lengths<P::R, P::KT>(a, partials<P::R, D>(), cus, ends, partial);
+      for (int i = 0; i < a.n_seqs; ++i) splits = std::max(splits, a.seq[i].splits);
+    }
+  }
   a.joined = 0;
-  return launch<T, P, D>(a, ws, joins, a.seq[0].splits, one, all, st);
+  return launch<T, P, D>(a, ws, joins, splits, one, all, st);
 }
 
 template <int D, int NR, class A>
@@ -1936,7 +1983,10 @@ hipError_t attend(const AttnDims& dm, A& a, int cus, void* ws, hipStream_t st) {
     // 8 sequences of 32768 memory rows of width 64: 64 rows 232 and 329, 84 287 and 330, 112 450 and 330, 168 548 and 644;
     // of 8192 tail rows of width 128: 116 and 170, 181 and 171, 212 and 172, 328 and 314; one of 1500 tail rows of width
     // 64: 320 rows 17 and 23 (2 tiles), 500 19 and 22 (3), 1332 34 and 36 (8); of width 128: 25 and 28, 30 and 31, 65 and 57.
-    if (rows <= 96 || (rows > 128 && rows <= 192 && memory >= tail) || memory + tail <= 3 * cus)
+    // In pages at most 9 tiles for width 64: 1332 rows of 4 heads, a window of 250 16 and 24 (2), two sequences 27 and 33 (4),
+    // four 42 and 46 (8), a window of 1000 31 and 34 (5), two 75 and 61 (10), without a window 37 and 39 (8), two 70 and 61
+    // (16); width 128, 1600 rows of 2 heads, a window of 250 29 and 32 (2.3), 55 and 45 (4.7), of 1000 41 and 35 (3.1).
+    if (rows <= 96 || (rows > 128 && rows <= 192 && memory >= tail) || memory + tail <= (A::kPaged && D == 64 ? 9 : 3) * cus)
       return launch_shares<float, F32<D>, D>(a, ws, cus, attend_f32<D, typename A::One>, attend_f32<D, A>, st);
     A few = take_few<F32Many<D>::R, F32Many<D>::KT>(a, kAlwaysFew, cus);
     if (few.n_seqs > 0) {
@@ -1951,8 +2001,12 @@ hipError_t attend(const AttnDims& dm, A& a, int cus, void* ws, hipStream_t st) {
   // to a compute unit.  us, it and the many-row kernel, 4 heads of width 128: 56 rows, 8 sequences of 32768 memory rows
   // 61 and 120, of 8192 tail rows 37 and 50; 84 rows 83 and 122, 59 and 53 (48 tiles); 112 rows 105 and 125, 60 and 53
   // (64); 168 rows 137 and 130 (193), 74 and 55 (96); 448 rows over 8192 memory rows 24 and 34 (14), 8 sequences of 1024
-  // tail rows 31 and 33 (28); 700 rows over 8192 33 and 35 (22), over 32768 73 and 65 (88).
-  if (rows <= kAlwaysFew || (rows <= 128 && memory >= tail) || memory + 2 * tail <= 40 * cus) return attend_few_rows<D, 2>(a, cus, ws, st);
+  // tail rows 31 and 33 (28); 700 rows over 8192 33 and 35 (22), over 32768 73 and 65 (88).  In pages, whose lengths are
+  // shared out evenly (plan_lengths), to 28: trees over 500 to 8192 rows, 448 rows of a head 32.0 and 32.0 (28; one
+  // sequence), 42 and 38 (37; 2), 27.5 and 29.6 (14; 4 over up to 2048), 88 and 59 (98; 8), 224 rows 28 and 30 (18), 38 and
+  // 35 (29); a window of 512, 7168 rows 47 and 35 (35), 1792 rows 18 and 28 (9).
+  if (rows <= kAlwaysFew || (rows <= 128 && memory >= tail) || memory + 2 * tail <= (A::kPaged ? 28 : 40) * cus)
+    return attend_few_rows<D, 2>(a, cus, ws, st);
   A few = take_few<Many<D>::R, Many<D>::KT>(a, kAlwaysFew, cus);
   if (few.n_seqs > 0) {
     const hipError_t e = attend<D>(dm, few, cus, ws, st);
