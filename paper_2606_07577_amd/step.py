@@ -624,3 +624,173 @@ class Reader:
 
     def close(self):
         self.attn.close()
+
+
+class PagedReader(Reader):
+    """A Reader whose tails lie in pages of one store, so that answers of any
+    lengths share it, with a sliding window for layers that have one, and
+    tokens drafted as a tree.
+
+    A stream takes pages as its tail grows, `max_rows` at most, and gives back
+    those that no layer's window sees any more.  window: tail rows that a
+    query sees (0: all), one number or one for each layer; sinks: first tail
+    rows that stay visible.  Memories are seen whole.
+
+    layer() and next() are the Reader's.  With `tree` in the layer() calls the
+    tokens are drafts, and accept() takes the place of next().  Pages are
+    taken by the first layer() call of some tokens, or ahead by reserve();
+    calls that are captured find them reserved.
+    """
+
+    def __init__(self, memories, h_q, h_kv, d, rope, n_pages, max_rows, page_rows=64, dtype="bf16", device="cuda", sm_scale=0.0,
+                 window=0, sinks=0):
+        self.tdtype = torch.bfloat16 if dtype == "bf16" else torch.float32
+        self.h_q, self.h_kv, self.d, self.cap, self.page_rows = h_q, h_kv, d, int(max_rows), int(page_rows)
+        self.memories, self.rope, self.sm_scale = list(memories), rope, float(sm_scale)
+        if not self.memories or len({len(m.data) for m in self.memories}) != 1:
+            raise ValueError("one memory at least, all of one number of layers")
+        if self.page_rows not in om.PAGE_ROWS or n_pages < 1 or max_rows < 1:
+            raise ValueError(f"pages have one of {om.PAGE_ROWS} rows; one page and one row at least")
+        n_layers, streams = len(self.memories[0].data), len(self.memories)
+        self.window = [int(window)] * n_layers if isinstance(window, int) else [int(w) for w in window]
+        self.sinks = int(sinks)
+        if len(self.window) != n_layers or min(self.window) < 0 or self.sinks < 0:
+            raise ValueError(f"window: one number >= 0, or one for each of {n_layers} layers; sinks >= 0")
+        self.attn = om.Attention(h_q, h_kv, d, om.BF16 if dtype == "bf16" else om.F32)
+        shape = (n_layers, int(n_pages), h_kv, self.page_rows, d)
+        self.k, self.v = (torch.zeros(shape, device=device, dtype=self.tdtype) for _ in range(2))
+        self.device = self.k.device
+        entries = -(-self.cap // self.page_rows)
+        self.tables = torch.full((streams, entries), -1, dtype=torch.int32, device=device)
+        # (calls come on streams that do not wait for this one, and into captures, which may not wait for it)
+        torch.cuda.current_stream(self.device).synchronize()
+        for m in self.memories:
+            if m.ready is not None:
+                m.ready.synchronize()
+        self._table = np.full((streams, entries), -1, dtype=np.int32)      # the tables' next contents
+        self._free = list(range(int(n_pages) - 1, -1, -1))
+        self._taken, self._given = [0] * streams, [0] * streams            # table entries that had a page; that were given back
+        self.tail = [0] * streams
+        self._new, self._drafts = None, False
+        layout = om._Layout(h_q, h_kv, d, self.tdtype, self.device.index, rope.n_axes)
+        fit = frozenset([("layout", layout), ("rows", self.page_rows)])
+        self._stores = om.array_of([om.make_pages(self.k[l], self.v[l]) for l in range(n_layers)])
+        self._pages = [om.make_pages(self.k[l], self.v[l]) for l in range(n_layers)]
+        at = np.arange(streams, dtype=np.uint64) * np.uint64(4 * entries) + np.uint64(self.tables.data_ptr())
+        self._rows = (om.PagedProjection * streams)()
+        self._rows._fit = fit
+        row = self._row = om.columns_of(self._rows)
+        row["q_out_head_stride"], row["q_out_row_stride"], row["table"] = d, h_q * d, at
+        self._queries, self._query = [], []
+        for l in range(n_layers):
+            queries = (om.PagedQuery * streams)()
+            queries._fit = fit
+            x = om.columns_of(queries)
+            x["q_head_stride"] = x["out_head_stride"] = d
+            x["q_row_stride"] = x["out_row_stride"] = h_q * d
+            x["table"], x["sm_scale"] = at, self.sm_scale
+            for b, m in enumerate(self.memories):
+                if m.rows[l]:
+                    om._memory(m.data[l], m.rows[l], self.k[l, 0])
+                    if m.data[l].device != self.device:
+                        raise ValueError("the memories must lie on the reader's device")
+                    queries[b].memory, queries[b].memory_head_stride = m.data[l].data_ptr(), m.data[l].stride(0)
+                    queries[b].memory_rows = m.rows[l]
+            self._queries.append(queries)
+            self._query.append(x)
+
+    def reserve(self, rows, stream=None):
+        """Pages for the next `rows` tokens of each stream (a number, or one
+        for each).  Raises, and takes none, where the store or a table has not
+        as many."""
+        rows = [int(rows)] * len(self.tail) if isinstance(rows, int) else [int(r) for r in rows]
+        if len(rows) != len(self.tail) or min(rows) < 0:
+            raise ValueError(f"rows: one number, or one for each of {len(self.tail)} streams")
+        if any(t + n > self.cap for t, n in zip(self.tail, rows)):
+            raise ValueError(f"more than {self.cap} tail rows")
+        need = [max(0, -(-(t + n) // self.page_rows) - have) for t, n, have in zip(self.tail, rows, self._taken)]
+        if sum(need) > len(self._free):
+            raise RuntimeError(f"{sum(need)} pages are needed, {len(self._free)} are free")
+        if not sum(need):          # (an entry whose page was given back is behind every window)
+            return
+        with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
+            if torch.cuda.is_current_stream_capturing():
+                raise RuntimeError("pages cannot be taken in a capture: reserve() them before it")
+            for b, n in enumerate(need):
+                for _ in range(n):
+                    self._table[b, self._taken[b]] = self._free.pop()
+                    self._taken[b] += 1
+            # (a pinned copy of its own: the next one may be made before this one has gone)
+            self.tables.copy_(torch.from_numpy(self._table.copy()).pin_memory(), non_blocking=True)
+
+    def layer(self, l, q, k, v, pos, tree=None, stream=None):
+        """Reader.layer over the pages.  tree: int64 [n_b] for each stream
+        (a list, or stacked), the masks of its drafts (omnimem.tree_masks):
+        token i of a stream sees of these tokens those of its mask."""
+        qp, qh, qr, new = self._columns("q", q, self.h_q, self.d)
+        kp, kh, kr, nk = self._columns("k", k, self.h_kv, self.d)
+        vp, vh, vr, nv = self._columns("v", v, self.h_kv, self.d)
+        pp, ps, _, np_ = self._columns("pos", pos, self.rope.n_axes, None)
+        if not new == nk == nv == np_:
+            raise ValueError("q, k, v and pos have different numbers of tokens")
+        if np.any(np.not_equal(kh, vh)) or np.any(np.not_equal(kr, vr)):
+            raise ValueError("k and v must share their strides")
+        if self._new is not None and (new != self._new or (tree is not None) != self._drafts):
+            raise ValueError("every layer takes the same tokens (next() or accept() begins the next ones)")
+        masks = 0
+        if tree is not None:
+            if len(tree) != len(new) or any(t.dtype != torch.int64 or t.device != self.device or t.shape != (n,) or
+                                            (n > 1 and t.stride(0) != 1) for t, n in zip(tree, new)):
+                raise ValueError("tree: contiguous int64 [n] of the reader's device for each stream")
+            if max(new) > om.MAX_DRAFTS:
+                raise ValueError(f"at most {om.MAX_DRAFTS} drafts")
+            masks = [t.data_ptr() for t in tree]
+        self.reserve(new, stream)
+        total, elt = sum(new), self.tdtype.itemsize
+        with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
+            rotated, out = (torch.empty((total, self.h_q, self.d), device=self.device, dtype=self.tdtype) for _ in range(2))
+        first = np.cumsum([0] + new)
+        at = first[:-1].astype(np.uint64) * np.uint64(self.h_q * self.d * elt)
+        row, query = self._row, self._query[l]
+        row["q"], row["q_head_stride"], row["q_row_stride"] = qp, qh, qr
+        row["k"], row["v"], row["kv_head_stride"], row["kv_row_stride"] = kp, vp, kh, kr
+        row["pos"], row["pos_stride"], row["n_rows"], row["first_row"] = pp, ps, new, self.tail
+        row["q_out"] = query["q"] = at + np.uint64(rotated.data_ptr())
+        query["out"], query["n_queries"] = at + np.uint64(out.data_ptr()), new
+        query["n_tail"], query["tree"] = np.add(self.tail, new), masks
+        self.attn.omnimem_rotate_pages(self.rope, self._pages[l], self._rows, stream)
+        self.attn.omnimem_attend_pages(self._pages[l], self._queries[l], self.window[l], self.sinks, stream)
+        self._new, self._drafts = new, tree is not None      # (a call that was refused has added nothing)
+        if isinstance(q, torch.Tensor):
+            return out.view(len(new), -1, self.h_q, self.d).transpose(1, 2) if total else out.new_empty((len(new), self.h_q, 0, self.d))
+        return [out[i: j].transpose(0, 1) for i, j in zip(first[:-1], first[1:])]
+
+    def next(self):
+        if self._drafts:
+            raise ValueError("the last tokens were drafts: accept() says which of them stay")
+        super().next()
+        self._give_back()
+
+    def accept(self, paths, stream=None):
+        """The drafts of the last layer() calls that stay, for each stream
+        those of a path through its tree (ascending; none: []): their rows
+        become the tail's next, the others are dropped."""
+        if not self._drafts:
+            raise ValueError("the last tokens were no drafts")
+        paths = [[int(i) for i in p] for p in paths]
+        if len(paths) != len(self._new) or any(p and not 0 <= p[0] <= p[-1] < n for p, n in zip(paths, self._new)):
+            raise ValueError("paths: drafts of each stream")
+        self.attn.omnimem_keep_pages(self._stores, [om.make_path(self.tables[b], self.tail[b], p) for b, p in enumerate(paths)], stream)
+        self._new, self._drafts = [len(p) for p in paths], False
+        self.next()
+
+    def _give_back(self):
+        """Pages behind every layer's window, but for the sinks', are free."""
+        if min(self.window) == 0:
+            return
+        for b, tail in enumerate(self.tail):       # (a query stands at row tail - 1 at least)
+            first, end = -(-self.sinks // self.page_rows), (tail - max(self.window)) // self.page_rows
+            for i in range(max(first, self._given[b]), min(end, self._taken[b])):
+                self._free.append(int(self._table[b, i]))
+                self._table[b, i] = -1
+            self._given[b] = max(self._given[b], min(end, self._taken[b]))

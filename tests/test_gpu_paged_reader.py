@@ -1,0 +1,247 @@
+"""Answers read from memories with their tails in pages: prompts, single tokens, drafted trees and what is accepted of
+them, windows, pages that are given back and taken again, calls captured and on other streams.  Each layer's result is
+compared with the definition on the memory's values and on the tail's rows as the library rotated them (the rotation's own
+bounds are tested with it), within the bounds of the attention's tests."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import operators_oracle as orc
+from paper_2606_07577_amd import omnimem as om
+from paper_2606_07577_amd.step import HeldMemory, PagedReader, Reader
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+H_Q, H_KV, D = 6, 2, 64
+
+
+def host(t):
+    return t.double().cpu().numpy()
+
+
+class Model:
+    """The streams' next projections, and what the tails have to hold."""
+
+    def __init__(self, dtype, rows, layers, window, sinks, seed=8, **more):
+        self.td = torch.bfloat16 if dtype == "bf16" else torch.float32
+        self.g = torch.Generator(device="cuda").manual_seed(seed)
+        self.layers, self.window, self.sinks = layers, window if isinstance(window, list) else [window] * layers, sinks
+        attn = om.Attention(H_Q, H_KV, D, om.BF16 if dtype == "bf16" else om.F32)
+        self.memories = []
+        for n in rows:
+            data = [torch.zeros(om.memory_shape(H_KV, D, n), dtype=torch.uint8, device="cuda") for _ in range(layers)]
+            if n:
+                attn.omnimem_pack([om.make_held(self.rnd(H_KV, n, D), self.rnd(H_KV, n, D), x) for x in data])
+            self.memories.append(HeldMemory(data, [n] * layers, [n // 2] * layers))
+        torch.cuda.synchronize()
+        attn.close()
+        freq = [1000.0 ** (-j / 16) for j in range(16)]
+        weight = self.weight = self.rnd(2, D)
+        self.rope = om.make_rope(D, freq, [j % 3 for j in range(16)], q_weight=weight[0], k_weight=weight[1])
+        self.reader = PagedReader(self.memories, H_Q, H_KV, D, self.rope, dtype=dtype, window=window, sinks=sinks, **more)
+        self.tails = [[np.zeros((2, H_KV, 0, D)) for _ in rows] for _ in range(layers)]   # rotated keys and values
+        self.held = [[orc.unpack(x.cpu().numpy(), m.rows[0]) if m.rows[0] else (np.zeros((H_KV, 0, D)),) * 2 for x in m.data]
+                     for m in self.memories]
+
+    def rnd(self, *shape):
+        return torch.randn(*shape, generator=self.g, device="cuda").to(self.td)
+
+    def tokens(self, lengths):
+        q, k, v = ([self.rnd(h, n, D) for n in lengths] for h in (H_Q, H_KV, H_KV))
+        return q, k, v, [torch.randint(0, 5000, (3, n), generator=self.g, device="cuda").to(torch.int32) for n in lengths]
+
+    def rotated(self, x, pos, key):
+        """The library's own rotation, by omnimem_rotate."""
+        attn, out = om.Attention(H_Q, H_KV, D, om.BF16 if self.td == torch.bfloat16 else om.F32), torch.zeros_like(x)
+        n = x.shape[1]
+        if n:
+            q = x if not key else self.rnd(H_Q, n, D)
+            k = x if key else self.rnd(H_KV, n, D)
+            qo, ko, vo = torch.zeros_like(q), torch.zeros_like(k), torch.zeros_like(k)
+            attn.omnimem_rotate(self.rope, [om.make_projection(q, k, k, pos, qo, ko, vo)])
+            out = ko if key else qo
+        torch.cuda.synchronize()
+        attn.close()
+        return host(out)
+
+    def step(self, lengths, trees=None, stacked=False, stream=None):
+        """One turn through the layers, each checked."""
+        masks = None if trees is None else [torch.tensor(om.tree_masks(t), dtype=torch.int64, device="cuda") for t in trees]
+        seen = None if trees is None else [[m % (1 << 64) for m in om.tree_masks(t)] for t in trees]
+        self.new = []
+        torch.cuda.synchronize()
+        for l in range(self.layers):
+            q, k, v, pos = self.tokens(lengths)
+            args = [torch.stack(x) if stacked else x for x in (q, k, v, pos)]
+            torch.cuda.synchronize()
+            out = self.reader.layer(l, *args, tree=masks, stream=stream)
+            torch.cuda.synchronize()
+            self.new.append([])
+            for b, n in enumerate(lengths):
+                rows = np.stack([self.rotated(k[b], pos[b], True), host(v[b])])
+                self.new[l].append(rows)
+                self.check(l, b, out[b], self.rotated(q[b], pos[b], False), np.concatenate([self.tails[l][b], rows], 2),
+                           seen[b] if seen else None)
+
+    def check(self, l, b, out, q, tail, masks):
+        n, nm = q.shape[1], self.memories[b].rows[l]
+        see = np.concatenate([np.ones((n, nm), bool), orc.paged_seen(n, tail.shape[2], self.window[l], self.sinks, masks)], 1)
+        k, v = (np.concatenate(x, 1) for x in zip(self.held[b][l], tail))
+        want, _, size, reach = orc.attend_seen(q, k, v, see, D ** -0.5)
+        half = 2.0 ** -8 if self.td == torch.bfloat16 else 0.0
+        # (queries and keys are off by the rounding of two libraries' rotations at most: the same one here)
+        near = 2 * (D + 6) * U * reach[..., None] + 2 * (see.shape[1] + 8) * U + half + self.slack(reach)
+        tol = size * near + (half or U) * np.abs(want) + see.shape[1] * 2.0 ** -126 * 10
+        assert (np.abs(host(out) - want) <= tol).all(), (l, b, n)
+
+    def slack(self, reach):
+        """Rotations into pages and into rows sum a norm's squares in another order: each is off from the definition by 24 u
+        of its pair, their keys and queries by 2 * 24 u each, and in bf16 by a step more (2^-8 to 2^-7 of a value) where they
+        round apart: 2 * (48 u + 2^-7) of the sum of |q||k|."""
+        return 2 * 2 * (48 * U + (2.0 ** -7 if self.td == torch.bfloat16 else 0.0)) * reach[..., None]
+
+    def grow(self, paths=None):
+        for l in range(self.layers):
+            for b, rows in enumerate(self.new[l]):
+                keep = list(range(rows.shape[2])) if paths is None else paths[b]
+                self.tails[l][b] = np.concatenate([self.tails[l][b], rows[:, :, keep]], 2)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("window,sinks", [(0, 0), ([0, 12], 3), (20, 2)])
+def test_answers_with_drafts(dtype, window, sinks):
+    m = Model(dtype, (77, 0, 300), 2, window, sinks, n_pages=30, max_rows=120, page_rows=16)
+    m.step([5, 17, 1])
+    m.reader.next()
+    m.grow()
+    for turn in range(3):
+        m.step([1, 1, 1], stacked=turn == 1)
+        m.reader.next()
+        m.grow()
+        trees = [[-1, 0, 0, 2, -1, 3], [-1] * 3, []] if turn != 1 else [[-1, 0, 1], [-1, 0, 0, 0, 1, 2, 3, 3], [-1]]
+        m.step([len(t) for t in trees], trees)
+        paths = [[0, 2, 3, 5], [1], []] if turn != 1 else [[], [0, 3, 7], [0]]
+        with pytest.raises(ValueError):
+            m.reader.next()
+        m.reader.accept(paths)
+        m.grow(paths)
+        assert m.reader.tail == [x.shape[2] for x in m.tails[0]]
+    m.step([4, 30, 2])
+    m.reader.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_pages_are_given_back_and_taken_again(dtype):
+    """Two long answers through a window in a store that does not hold them whole."""
+    # (a stream has its first page, and 31 rows of a window with 7 new ones on 4 pages at most)
+    m = Model(dtype, (40, 0), 1, 30, 4, n_pages=10, max_rows=2000, page_rows=16)
+    m.step([20, 33])
+    m.reader.next()
+    m.grow()
+    for turn in range(24):
+        m.step([7, 5])
+        m.reader.next()
+        m.grow()
+    assert sum(m.reader.tail) == 53 + 24 * 12 > 10 * 16
+    assert len(m.reader._free) + (m.reader._table >= 0).sum() == 10
+    used = m.reader._table[m.reader._table >= 0].tolist() + m.reader._free
+    assert sorted(used) == list(range(10))
+    m.reader.close()
+
+
+def test_more_than_the_store_holds_is_refused():
+    m = Model("bf16", (40, 0), 1, 0, 0, n_pages=3, max_rows=40, page_rows=16)
+    q, k, v, pos = m.tokens([20, 20])
+    for bad in ([20, 30], [41, 0]):
+        with pytest.raises((ValueError, RuntimeError)):
+            m.reader.layer(0, *m.tokens(bad))
+    assert len(m.reader._free) == 3 and m.reader._new is None and m.reader._taken == [0, 0]
+    m.step([20, 10])
+    m.reader.next()
+    m.grow()
+    with pytest.raises(RuntimeError):
+        m.reader.reserve([1, 7])
+    m.reader.reserve([12, 6])
+    m.step([12, 6])
+    with pytest.raises(ValueError):
+        m.reader.accept([[0], [0]])
+    tree = [torch.zeros(n, dtype=torch.int64, device="cuda") for n in (1, 1)]
+    with pytest.raises(ValueError):                            # (the tokens before were no drafts)
+        m.reader.layer(0, *m.tokens([12, 6]), tree=tree)
+    m.reader.next()
+    for bad in ([tree[0]], [tree[0].int(), tree[1]], [tree[0], torch.zeros(2, dtype=torch.int64, device="cuda")], [t.cpu() for t in tree]):
+        with pytest.raises(ValueError):
+            m.reader.layer(0, *m.tokens([1, 1]), tree=bad)
+    with pytest.raises(ValueError):
+        PagedReader(m.memories, H_Q, H_KV, D, m.rope, n_pages=3, max_rows=40, page_rows=24)
+    with pytest.raises(ValueError):
+        PagedReader(m.memories, H_Q, H_KV, D, m.rope, n_pages=3, max_rows=40, window=[1, 2])
+    m.reader.close()
+
+
+@pytest.mark.parametrize("stacked", [False, True])
+def test_a_tokens_calls_captured(stacked):
+    """A token's layers in a graph, replayed with other projections; its pages are reserved before."""
+    m = Model("bf16", (40, 0), 2, 25, 2, n_pages=12, max_rows=100, page_rows=16)
+    m.step([15, 31])
+    m.reader.next()
+    m.grow()
+    q, k, v, pos = (torch.stack(x) for x in m.tokens([1, 1]))
+    pos = pos.contiguous()
+    args = (q, k, v, pos) if stacked else tuple(list(x) for x in (q, k, v, pos))
+    stream, graph, outs = torch.cuda.Stream(), torch.cuda.CUDAGraph(), []
+    torch.cuda.synchronize()
+    with torch.cuda.stream(stream):
+        with pytest.raises(RuntimeError):                      # (15 and 31 rows: the next tokens need no page; 3 rows do)
+            with torch.cuda.graph(torch.cuda.CUDAGraph(), stream=stream):
+                m.reader.reserve(3)
+        torch.cuda.synchronize()
+        m.reader.reserve(1)
+        with torch.cuda.graph(graph, stream=stream):
+            for l in range(2):
+                outs.append(m.reader.layer(l, *args))
+    for turn in range(3):
+        new = [torch.stack(x) for x in m.tokens([1, 1])]
+        for old, x in zip((q, k, v, pos), new):
+            old.copy_(x)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for l in range(2):
+            for b in range(2):
+                tail = np.concatenate([m.tails[l][b], np.stack([m.rotated(k[b], pos[b], True), host(v[b])])], 2)
+                m.check(l, b, outs[l][b], m.rotated(q[b], pos[b], False), tail, None)
+    m.reader.close()
+
+
+def test_turns_on_different_streams():
+    m = Model("bf16", (40, 0), 2, 0, 0, n_pages=12, max_rows=100, page_rows=16)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for turn in range(4):
+        m.step([3, 9], stream=streams[turn % 2])               # (each turn waited for: their order is the caller's)
+        m.reader.next()
+        m.grow()
+    m.step([3, 2], [[-1, 0, 0], [-1, -1]], stream=streams[0])
+    m.reader.accept([[0, 2], [1]], stream=streams[0])
+    m.grow([[0, 2], [1]])
+    torch.cuda.synchronize()
+    m.step([1, 1], stream=streams[1])
+    m.reader.close()
+
+
+def test_whole_tails_read_as_the_readers():
+    """Without window or drafts: the Reader's results (the same rotation in bf16 without norms, the same sums)."""
+    m = Model("bf16", (100, 0), 1, 0, 0, n_pages=20, max_rows=100, page_rows=32)
+    rope = om.make_rope(D, [1000.0 ** (-j / 16) for j in range(16)], [j % 3 for j in range(16)])
+    plain, paged = Reader(m.memories, H_Q, H_KV, D, rope, 100), PagedReader(m.memories, H_Q, H_KV, D, rope, 20, 100)
+    for lengths in ([9, 30], [1, 1], [1, 1]):
+        args = m.tokens(lengths)
+        a, b = plain.layer(0, *args), paged.layer(0, *args)
+        torch.cuda.synchronize()
+        for x, y in zip(a, b):
+            assert torch.equal(x, y)
+        plain.next()
+        paged.next()
+    plain.close()
+    paged.close()
+    m.reader.close()
