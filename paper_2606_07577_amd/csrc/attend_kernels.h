@@ -363,6 +363,7 @@ __device__ __forceinline__ void finish(const A& a, const QuerySeq& s, const Unit
     const Row row = row_of(a, s, x, x.rt * R + r);
     if (s.lse) s.lse[row.h * (int64_t)s.lse_hs + row.i] = log_of(m, l);
   };
+  bool odd = false;
   if (tid < R) joint->flag[tid] = 0;
   __syncthreads();
   for (int e = tid; e < live * TPR; e += THREADS) {
@@ -381,15 +382,20 @@ __device__ __forceinline__ void finish(const A& a, const QuerySeq& s, const Unit
     } else {
       put_row(r, c, y, joint->ml[r].y);
     }
-    if (x.k1 > x.mem_tiles && (y[0] + y[1] + y[2] + y[3]) * 0.0f != 0.0f) joint->flag[r] = 1;
+    if (x.k1 > x.mem_tiles && (y[0] + y[1] + y[2] + y[3]) * 0.0f != 0.0f) {
+      joint->flag[r] = 1;
+      odd = true;
+    }
   }
   if (tid < live) {
     const float2 ml = joint->ml[tid];
     if (x.slot >= 0) share8(&a.part_ml[(int64_t)x.slot * R + tid].x, ml.x, ml.y);
     else put_lse(tid, ml.x, ml.y);
   }
-  __syncthreads();
-  for (int r = wave_id(); r < live; r += WAVES)
+  bool again = true;                                       // (one look at all flags where no row has one)
+  if constexpr (A::kPaged) again = __syncthreads_or(odd) != 0;
+  else __syncthreads();
+  for (int r = wave_id(); again && r < live; r += WAVES)
     if (uniform(joint->flag[r])) form_again<T, D, R, KT>(a, s, x, r, joint->ml[r].x, joint->ml[r].y);
   if (x.slot < 0 || !a.joined) return;
 
@@ -955,10 +961,11 @@ __global__ __launch_bounds__(256, 2) void attend_f32_many(A a) {
 // which issues vector instructions, most of them to convert codes, in 38% of
 // its cycles and waits in 41%.
 // ---------------------------------------------------------------------------
-template <int D, int NR>
+template <int D, int NR, int KEYS = 128>                 // KEYS 32: without memories
 struct Few {
-  static constexpr int R = 16 * NR, KT = 128;
+  static constexpr int R = 16 * NR, KT = KEYS;
   static constexpr int WAVES = 4;
+  static constexpr bool MEM = KEYS == 128;
   static constexpr int STEPS = D * NR == 256 ? 2 : 1;      // a memory tile's, by the registers of two wavefronts a SIMD
   static constexpr int OROW = D + 4;
   static constexpr int VBUF = 32 * D * 2;                  // bytes of a wavefront's tail V rows in LDS
@@ -1012,13 +1019,13 @@ __device__ inline uint4 load_part(const char* p) {   // 16 or 8 bytes
   return make_uint4(x.x, x.y, 0, 0);
 }
 
-template <int D, int NR, class A>
+template <int D, int NR, class A, int KEYS = 128>
 __global__ __launch_bounds__(256, 2) void attend_few(A a) {
-  using P = Few<D, NR>;
+  using P = Few<D, NR, KEYS>;
   using B = MemBlock<D>;
   constexpr int R = P::R, KT = P::KT, WAVES = P::WAVES, NS = D / 32, NC = D / 16, STEPS = P::STEPS, T = 8 / STEPS;
   extern __shared__ __align__(16) char lds[];
-  const Unit x = unit_of<R, KT, kFewWaves>(a, blockIdx.x);
+  const Unit x = unit_of<R, KT, WAVES>(a, blockIdx.x);
   const QuerySeq& s = a.seq[x.s];
   const int lane = threadIdx.x & 63, wave = wave_id(), g = lane >> 4, i16 = lane & 15;
   Row row[NR];
@@ -1038,7 +1045,7 @@ __global__ __launch_bounds__(256, 2) void attend_few(A a) {
   const float scale = s.scale_log2;
   int kti = x.k0 + wave;
 
-  if (kti < min(x.k1, x.mem_tiles)) {
+  if (P::MEM && kti < min(x.k1, x.mem_tiles)) {
     // channels g D/4 .. of the queries, as the lanes hold K's
 #pragma unroll
     for (int n = 0; n < NR; ++n)
@@ -1180,7 +1187,7 @@ __global__ __launch_bounds__(256, 2) void attend_few(A a) {
       }
     };
     // (each wavefront's 32-row steps: four to a key tile)
-    const auto next = [&](int key) { return (key & 96) != 96 ? key + 32 : key + 32 + (WAVES - 1) * KT; };
+    const auto next = [&](int key) { return (key & (KT - 32)) != KT - 32 ? key + 32 : key + 32 + (WAVES - 1) * KT; };
     int end = min((x.k1 - x.mem_tiles) * KT, s.nt);
     if constexpr (A::kPaged) end = min((x.k1 - x.mem_tiles) * KT, s.nt - x.tail.skip * KT);
     int key = (kti - x.mem_tiles) * KT;
@@ -1749,14 +1756,28 @@ Shares set_shares(A& a, int64_t share) {
   }
   return x;
 }
-template <int R, int KT, class A>
+// Short key tiles, of 32 rows (bf16 in pages without memories), count a quarter of those of 128,
+// and no split and what a join costs are weighed too: in tiles' time 5 and 5 for
+// each partial on a compute unit (32 rows: 8 and 12).  us, split and not, width
+// 128, 4 KV heads: a token that sees 1028 rows 9.0 and 14.1, 516 7.9 and 9.7, 132 7.7
+// and 6.7; 16 tokens that see 516 11.2 and 12.6, 32 13.8 and 12.9; trees over 500
+// rows, 112 rows of a head 11.2 and 12.7, four of 448 16.0 and 13.2.
+template <int R, int KT, bool kShort, class A>
 bool plan_shares(A& a, int64_t slots, int cus) {
+  constexpr int kEnds = kShort ? 24 : 6;
+  const auto join = [cus](const Shares& x) { return x.parts == 0 ? 0.0 : R == 16 ? 5 + 5.0 * x.parts / cus : 8 + 12.0 * x.parts / cus; };
+
   int64_t keys, most = 1;
   count_tiles<R, KT>(a, &keys);
   a.whole = 0;
   for (int i = 0; i < a.n_seqs; ++i) most = std::max(most, (int64_t)tiles_of<KT>(a.seq[i].nm) + tiles_of<KT>(tail_rows<R>(a, a.seq[i])));
   int64_t best = (most + kFewWaves - 1) / kFewWaves, high = best;   // in kFewWaves tiles: no split
   double least = 1e30;
+  if constexpr (kShort) {
+    const Shares x = set_shares<R, KT>(a, high * kFewWaves);
+    const double n = (double)((x.units + cus - 1) / cus);
+    least = (n - 1) * x.tiles / x.units + x.largest + kEnds * n;
+  }
   for (int k : {1, 2, 3, 4, 6, 8}) {
     int64_t low = 1;
     if (set_shares<R, KT>(a, high * kFewWaves).units > (int64_t)k * cus) continue;
@@ -1765,7 +1786,7 @@ bool plan_shares(A& a, int64_t slots, int cus) {
       if (set_shares<R, KT>(a, mid * kFewWaves).units <= (int64_t)k * cus) high = mid; else low = mid + 1;
     }
     const Shares x = set_shares<R, KT>(a, high * kFewWaves);
-    const double n = (double)((x.units + cus - 1) / cus), cost = (n - 1) * x.tiles / x.units + x.largest + 6 * n;
+    const double n = (double)((x.units + cus - 1) / cus), cost = (n - 1) * x.tiles / x.units + x.largest + kEnds * n + (kShort ? join(x) : 0);
     if (x.parts <= slots && cost < least) {
       least = cost;
       best = high;
@@ -1894,7 +1915,7 @@ hipError_t launch_shares(A& a, void* ws, int cus, One one, All all, hipStream_t 
   constexpr int64_t slots = partials<P::R, D>();
   static_assert(slots <= kMaxPartials, "a counter to a partial");
   static_assert(P::WAVES == kFewWaves, "shares for the workgroup's wavefronts");
-  if (!plan_shares<P::R, P::KT>(a, slots, cus)) return hipErrorInvalidConfiguration;
+  if (!plan_shares<P::R, P::KT, sizeof(T) == 2 && P::KT == 32>(a, slots, cus)) return hipErrorInvalidConfiguration;
   int splits = 1;
   int64_t joins = 0, batches = 0;
   for (int i = 0; i < a.n_seqs; ++i) {
@@ -1937,6 +1958,14 @@ hipError_t launch_rounds(A& a, void* ws, int cus, double ends, double partial, O
 
 template <int D, int NR, class A>
 hipError_t attend_few_rows(A& a, int cus, void* ws, hipStream_t st) {
+  if constexpr (A::kPaged) {
+    bool memory = false;
+    for (int i = 0; i < a.n_seqs; ++i) memory |= a.seq[i].nm > 0;
+    if (!memory) {
+      using P = Few<D, NR, 32>;
+      return launch_shares<uint16_t, P, D>(a, ws, cus, attend_few<D, NR, typename A::One, 32>, attend_few<D, NR, A, 32>, st);
+    }
+  }
   using P = Few<D, NR>;
   return launch_shares<uint16_t, P, D>(a, ws, cus, attend_few<D, NR, typename A::One>, attend_few<D, NR, A>, st);
 }
@@ -1996,6 +2025,20 @@ hipError_t attend(const AttnDims& dm, A& a, int cus, void* ws, hipStream_t st) {
     return launch_rounds<float, F32Many<D>, D>(a, ws, cus, 1.0, 0.003, attend_f32_many<D, typename A::One>, attend_f32_many<D, A>, st);
   }
   if (rows <= 16) return attend_few_rows<D, 1>(a, cus, ws, st);
+  if constexpr (A::kPaged) {
+    // Units of 16 rows where a compute unit has one at most and 4 tail tiles (of 128 rows): half the instructions of those of
+    // 32 one after the other.  us, 32 and 16 rows, 4 heads of width 128: trees of 28 rows of a head over 12 rows 7.9 and 6.2,
+    // over 2000 11.2 and 9.8, of 112 rows over 500 10.8 and 9.6, four over up to 2000 16.0 and 15.5 (4), 448 rows over 500
+    // 12.4 and 10.4 (2), over 2000 16.5 and 18.6 (7); 7 of 104 rows over 4096 memory rows of width 64 15.0 and 13.2, 16 of
+    // them 19.1 and 17.2.
+    int64_t units = 0, tiles = 0;
+    for (int i = 0; i < a.n_seqs; ++i) {
+      const int64_t n = a.h_kv * (((int64_t)a.group * a.seq[i].nq + 15) / 16);
+      units += n;
+      tiles += n * tiles_of<128>(tail_rows<16>(a, a.seq[i]));
+    }
+    if (units <= cus && tiles <= 4 * cus) return attend_few_rows<D, 1>(a, cus, ws, st);
+  }
   // The few-row kernel up to 64 rows of a head, to 128 over memories (whose codes it reads again for each 32 rows at a
   // quarter of tail rows' cost), and where that leaves at most 40 tiles (32 rows and 128 memory rows, or 64 tail rows)
   // to a compute unit.  us, it and the many-row kernel, 4 heads of width 128: 56 rows, 8 sequences of 32768 memory rows
@@ -2026,6 +2069,10 @@ hipError_t prepare() {
   if (e == hipSuccess) e = allow(attend_f32_many<D, A>, F32Many<D>::LDS);
   if (e == hipSuccess) e = allow(attend_few<D, 1, A>, Few<D, 1>::LDS);
   if (e == hipSuccess) e = allow(attend_few<D, 2, A>, Few<D, 2>::LDS);
+  if constexpr (A::kPaged) {
+    if (e == hipSuccess) e = allow(attend_few<D, 1, A, 32>, Few<D, 1, 32>::LDS);
+    if (e == hipSuccess) e = allow(attend_few<D, 2, A, 32>, Few<D, 2, 32>::LDS);
+  }
   if (e == hipSuccess) e = allow(attend_many<D, A>, Many<D>::LDS);
   return e;
 }
