@@ -50,6 +50,11 @@ omnimem_status take_pages(omnimem_attn* attn, const omnimem_pages* pages, Store&
 bool on(const Store& x, const Span& a) { return overlap(x.k, a) || overlap(x.v, a); }
 
 const char* kTable = "table must be given, 4-byte aligned";
+// The table's entries for rows before `rows`, as an array of bytes.
+Span entries(const Store& x, const int32_t* table, int64_t rows) {
+  const int64_t bytes = ((rows - 1) >> x.pool.shift) * 4 + 4;
+  return {reinterpret_cast<uintptr_t>(table), 1, 1, 0, 0, bytes};
+}
 
 }  // namespace
 
@@ -83,8 +88,11 @@ omnimem_status omnimem_rotate_pages(omnimem_attn* attn, const omnimem_rope* rope
     const Span k = span(attn, s.k, H, s.n_rows, s.kv_head_stride, s.kv_row_stride);
     const Span v = span(attn, s.v, H, s.n_rows, s.kv_head_stride, s.kv_row_stride);
     const Span o = span(attn, s.q_out, Hq, s.n_rows, s.q_out_head_stride, s.q_out_row_stride);
-    if (on(store, q) || on(store, k) || on(store, v) || on(store, o)) return bad(attn, i, "q, k, v or q_out overlaps the pages");
-    if ((!same(o, q) && overlap(o, q)) || overlap(o, k) || overlap(o, v)) return bad(attn, i, "q_out overlaps an input that it is not");
+    const Span table = entries(store, s.table, s.first_row + s.n_rows);
+    if (on(store, q) || on(store, k) || on(store, v) || on(store, o) || on(store, table))
+      return bad(attn, i, "q, k, v, q_out or the table overlaps the pages");
+    if ((!same(o, q) && overlap(o, q)) || overlap(o, k) || overlap(o, v) || overlap(o, table))
+      return bad(attn, i, "q_out overlaps an input that it is not");
   }
   OnDevice dev(attn->device);
   hipError_t e = dev.err;
@@ -138,8 +146,10 @@ omnimem_status omnimem_attend_pages(omnimem_attn* attn, const omnimem_pages* pag
     const Span lse = {reinterpret_cast<uintptr_t>(s.lse), Hq, 1, s.lse_head_stride * 4, s.n_queries * 4, s.n_queries * 4};
     const auto written = [&](const Span& x) { return overlap(o, x) || (s.lse && overlap(lse, x)); };
     if (written(q) || (s.lse && overlap(o, lse)) || written(store.k) || written(store.v) ||
+        (s.n_tail > 0 && written(entries(store, s.table, s.n_tail))) ||
+        (s.tree && written({reinterpret_cast<uintptr_t>(s.tree), 1, 1, 0, 0, s.n_queries * 8})) ||
         (s.memory_rows > 0 && written({reinterpret_cast<uintptr_t>(s.memory), H, 1, s.memory_head_stride, bytes, bytes})))
-      return bad(attn, i, "out or lse overlaps the other, q, the pages or the memory");
+      return bad(attn, i, "out or lse overlaps the other, q, the pages, the memory, the table or the tree");
   }
   OnDevice dev(attn->device);
   hipError_t e = dev.err;
@@ -190,6 +200,11 @@ omnimem_status omnimem_keep_pages(omnimem_attn* attn, const omnimem_pages* layer
     if (!s.path) return bad(attn, i, "null path");
     for (int j = 0; j < s.n_kept; ++j)
       if (s.path[j] >= kMaxDrafts || (j > 0 && s.path[j] <= s.path[j - 1])) return bad(attn, i, "path must ascend, below 64");
+    for (int l = 0; l < n_layers; ++l) {
+      store.k.base = reinterpret_cast<uintptr_t>(layers[l].k);
+      store.v.base = reinterpret_cast<uintptr_t>(layers[l].v);
+      if (on(store, entries(store, s.table, s.first_row + s.path[s.n_kept - 1] + 1))) return bad(attn, i, "the table overlaps the pages");
+    }
   }
   OnDevice dev(attn->device);
   hipError_t e = dev.err;

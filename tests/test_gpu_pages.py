@@ -418,6 +418,33 @@ def test_rows_go_to_their_pages(dtype, d, rot, neighbours, norm, page_rows, layo
     attn.close()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("h_q,h_kv,d", [(120, 30, 128), (31, 31, 64), (1, 1, 64)])
+def test_more_heads_than_a_workgroup_has_lanes_for(dtype, h_q, h_kv, d):
+    """As omnimem_rotate in rows of their own, within twice its bound (the norm's squares are summed in another order)."""
+    attn = handle(h_q, h_kv, d, dtype)
+    g = torch.Generator(device="cuda").manual_seed(h_q)
+    n = 9
+    store = Store(g, h_kv, d, dtype, 16, [n + 3])
+    q, k, v = (torch.randn(h, n, d, generator=g, device="cuda").to(TORCH[dtype]) for h in (h_q, h_kv, h_kv))
+    w = (1 + 0.3 * torch.randn(2, d, generator=g, device="cuda")).to(TORCH[dtype])
+    pos = torch.randint(0, 9000, (2, n), generator=g, device="cuda").to(torch.int32)
+    rope = om.make_rope(d, [0.9 ** j for j in range(d // 2)], [j % 2 for j in range(d // 2)], q_weight=w[0], k_weight=w[1])
+    out, outs = torch.zeros_like(q), [torch.zeros_like(x) for x in (q, k, v)]
+    attn.omnimem_rotate_pages(rope, store.pages(), [om.make_paged_projection(q, k, v, pos, out, store.device_tables[0], 3)])
+    attn.omnimem_rotate(rope, [om.make_projection(q, k, v, pos, *outs)])
+    torch.cuda.synchronize()
+    at = torch.arange(3, 3 + n, device="cuda")
+    page = store.device_tables[0].long()[at // 16]
+    keys = store.k[page, :, at % 16].transpose(0, 1)
+    for x, y, raw, weight in ((out, outs[0], q, w[0]), (keys, outs[1], k, w[1])):
+        flat = orc.rotate(host(raw), pos.cpu().numpy(), [0.0] * (d // 2), [0] * (d // 2), 0, False, host(weight), 1e-6)
+        tol = 2 * (torch.finfo(x.dtype).eps / 2 * np.abs(host(y)) * (1 + 2.0 ** -7) + 24 * U * size_of(flat, d, False))
+        assert (np.abs(host(x) - host(y)) <= tol).all()
+    assert torch.equal(store.v[page, :, at % 16].transpose(0, 1), v)
+    attn.close()
+
+
 @pytest.mark.parametrize("rows", [5, 5000])
 def test_rows_without_a_page_are_dropped(rows):
     attn = handle(2, 2, 64, "bf16")

@@ -181,7 +181,8 @@ def test_rotate_pages(lib, attn):
                                 dict(k=None), dict(v=None), dict(k=BASE + (1 << 20) + 8), dict(kv_row_stride=D - unit), dict(kv_row_stride=D + 1),
                                 dict(pos=None), dict(pos=BASE + 2), dict(pos_stride=-1), dict(q_out=None), dict(q_out_row_stride=0),
                                 dict(q_out_head_stride=D), dict(table=None), dict(table=BASE + 6), dict(q_out=BASE + 16), dict(q_out=FAR),
-                                dict(k=FAR), dict(v=2 * FAR + 64), dict(q=FAR + PAGE * attn.elt * 99), dict(q_out=BASE + (1 << 20))])
+                                dict(k=FAR), dict(v=2 * FAR + 64), dict(q=FAR + PAGE * attn.elt * 99), dict(q_out=BASE + (1 << 20)),
+                                dict(table=2 * FAR), dict(table=BASE + (4 << 20) + 16)])
     bad = om.Rope(n_axes=1, eps=-1.0)
     assert rotate(lib, attn, rope=bad) == om.ERR_INVALID_ARG
     assert rotate(lib, attn, rope=om.Rope(n_axes=1, rotary_dim=8, inv_freq=(ctypes.c_double * 4)())) == om.ERR_UNSUPPORTED
@@ -191,7 +192,7 @@ def test_attend_pages(lib, attn):
     unit = 16 // attn.elt
     tree = BASE + (6 << 20)
     taken(lib, attn, attend, [{}, dict(window=1), dict(window=2 ** 62, sinks=2 ** 62), dict(sinks=5), dict(tree=tree), dict(tree=tree, n_tail=N),
-                              dict(memory=None, memory_rows=0), dict(n_tail=0, table=None), dict(lse=None), dict(n_tail=1 << 30),
+                              dict(memory=None, memory_rows=0), dict(n_tail=0, table=None), dict(lse=None), dict(n_tail=1 << 30, table=BASE + (1 << 30)),
                               dict(out_head_stride=D, out_row_stride=4 * D)])
     lib.standin_launches()
     assert attend(lib, attn, n_queries=0, q=None, table=None) == om.OK and lib.standin_launches() == 0
@@ -201,7 +202,8 @@ def test_attend_pages(lib, attn):
                                 dict(memory_head_stride=34 * D * 3), dict(memory=BASE + (1 << 20) + 4), dict(sm_scale=float("inf")),
                                 dict(sm_scale=float("nan")), dict(sm_scale=3e38), dict(out_row_stride=D - unit), dict(out_row_stride=0),
                                 dict(lse=BASE + (4 << 20) + 2), dict(lse_head_stride=N - 1), dict(out=BASE), dict(out=FAR), dict(lse=2 * FAR + 4),
-                                dict(out=BASE + (1 << 20)), dict(lse=BASE + (3 << 20))])
+                                dict(out=BASE + (1 << 20)), dict(lse=BASE + (3 << 20)), dict(table=BASE + (3 << 20)), dict(table=BASE + (4 << 20) + 4),
+                                dict(tree=BASE + (3 << 20) + 8)])
     for change in (dict(window=-1), dict(sinks=-1)):
         assert attend(lib, attn, **change) == om.ERR_INVALID_ARG and b"window" in lib.omnimem_attn_last_error(attn)
         assert lib.standin_launches() == 0
@@ -214,7 +216,7 @@ def test_keep_pages(lib, attn):
     for path in ((), (0,), (0, 1, 2, 3)):                       # nothing moves
         assert keep(lib, attn, path=path) == om.OK and lib.standin_launches() == 0
     refused(lib, attn, keep, [dict(n_kept=-1), dict(n_kept=65), dict(first_row=-1), dict(first_row=1 << 30), dict(table=None),
-                              dict(table=BASE + 1)])
+                              dict(table=BASE + 1), dict(table=FAR + 4)])
     refused(lib, attn, keep, [dict(path=(1, 1)), dict(path=(3, 2)), dict(path=(64,)), dict(path=(1, 255))], text=b"sequence 0")
     seqs = (om.Path * 1)(om.Path(BASE, 5, None, 2))
     assert lib.omnimem_keep_pages(attn, ctypes.byref(om.Pages(**POOL)), 1, seqs, 1, None) == om.ERR_INVALID_ARG
@@ -222,6 +224,7 @@ def test_keep_pages(lib, attn):
     # layers: alike but for k and v, in launches of some
     many = [{**POOL, "k": FAR * (2 * i + 1), "v": FAR * (2 * i + 2)} for i in range(70)]
     lib.standin_moved()
+    assert keep(lib, attn, pools=many, table=many[60]["v"] + 8) == om.ERR_INVALID_ARG and lib.standin_launches() == 0
     assert keep(lib, attn, pools=many) == om.OK and lib.standin_moved() == 70 and 2 <= lib.standin_launches() <= 4
     for change in (dict(n_pages=99), dict(page_stride=2 * PAGE), dict(head_stride=D, row_stride=H * D)):
         assert keep(lib, attn, pools=(POOL, {**POOL, **change})) == om.ERR_INVALID_ARG
