@@ -20,7 +20,11 @@ constexpr int kRun = 16 / (int)sizeof(T);
 // many wavefronts as they fill.  What a lane waits for, its rows, the table's
 // entry, the token's positions, its frequency and that one's axis, depends on
 // the arguments alone and is asked for at once; the cosines are formed while the
-// rows are on their way.
+// rows are on their way.  Latency bounds it: 32 tokens of 36 heads of width 128
+// take 4.0 us a launch on the device, of which an empty one has 3.1 (without the
+// stores 3.7); 2331 of 20 heads of width 64 in fp32 (23.9 MB) 9.4, where loads,
+// 3.2, and stores, 4.4, follow one another in all wavefronts at once (with runs
+// of 32 bytes to a lane 12.1).
 constexpr int kRowWaves = 12;    // at most
 template <typename T, int D, class A>
 __global__ __launch_bounds__(64 * kRowWaves) void rotate_row(A a) {
@@ -76,7 +80,8 @@ __global__ __launch_bounds__(64 * kRowWaves) void rotate_row(A a) {
 }
 
 // Many tokens: a workgroup to as many neighbouring tokens as a wavefront has rows, a head of all of
-// them to a wavefront at a time, as rotate_tokens.
+// them to a wavefront at a time, as rotate_tokens.  Bandwidth bounds it: 16384
+// tokens of 36 heads of width 128 (302 MB read and written) take 63 us, 4.8 TB/s.
 template <typename T, int D, class A>
 __global__ __launch_bounds__(256) void rotate_rows(A a) {
   constexpr int C = kRun<T>, U = D / (2 * C), TOKENS = 64 / U, F = D / 2;
@@ -136,7 +141,7 @@ void launch(const All& a, int n, int64_t rows, int64_t tokens, hipStream_t st) {
   x.pool = a.pool;
   std::memcpy(x.turns, a.turns, sizeof a - offsetof(All, turns));
   constexpr int U = D / (2 * kRun<T>), TOKENS = 64 / U;
-  if (tokens >= 4096) {
+  if (tokens >= 4096) {                                    // (see rotate.hip)
     rotate_rows<T, D, PagedRotateArgs<N>><<<dim3((unsigned)((rows + TOKENS - 1) / TOKENS), n), 256, 0, st>>>(x);
   } else {
     const int waves = std::min((a.h_q + 2 * a.h_kv + TOKENS - 1) / TOKENS, kRowWaves);
