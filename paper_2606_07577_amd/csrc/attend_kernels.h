@@ -40,8 +40,8 @@ __device__ inline uint32_t entry_of(const PagePool& pool, const QuerySeq& s, int
   typedef const __attribute__((address_space(4))) uint32_t scalar_t;
   return ((scalar_t*)(uintptr_t)s.k)[uniform(group_of(s.nt, key)) >> pool.shift];
 }
-__device__ inline Place place_at(const PagePool& pool, const QuerySeq& s, uint32_t entry, int key) {
-  return place_of(pool, s.nt, (uint32_t)uniform((int)entry), uniform(key));
+__device__ inline Place place_at(const PagePool& pool, const QuerySeq& s, uint32_t entry, int key, uint32_t spare) {
+  return place_of(pool, s.nt, (uint32_t)uniform((int)entry), uniform(key), (uint32_t)uniform((int)spare));
 }
 
 // ---------------------------------------------------------------------------
@@ -61,7 +61,8 @@ struct Unit {
   int slot;                  // partial, or -1: the result is final
   int split, splits;         // its share of the row tile
   TailTiles tail;            // in pages
-  bool holes;                // and some of them without a page
+  bool holes;                // and some of them without a page,
+  uint32_t spare;            // for which the page with this entry is read
 };
 // Row tile's tail key tile tt of those that it takes.
 template <class A>
@@ -112,6 +113,7 @@ __device__ inline Unit unit_of(const A& a, int u) {
   if constexpr (A::kPaged) {
     x.tail = tail_tiles_of<KT>(s.nq, s.nt, a.window, a.sinks, x.rt * R / a.group, last, s.v != nullptr);
     x.holes = false;
+    x.spare = kNoPage;
     tail_tiles = x.tail.count;
   } else {
     tail_tiles = tiles_of<KT>(tail_seen(s, a.causal, last));
@@ -253,7 +255,7 @@ __device__ __forceinline__ void form_again(const A& a, const QuerySeq& s, const 
     if constexpr (A::kPaged) {
       for (int tt = max(x.k0 - x.mem_tiles, 0); tt < x.k1 - x.mem_tiles; ++tt)
         for (int key0 = tail_tile<A>(x, tt) * KT, b = 0; b < KT; b += 16) {
-          const Place at = place_at(a.pool, s, entry_of(a.pool, s, key0 + b), key0 + b);
+          const Place at = place_at(a.pool, s, entry_of(a.pool, s, key0 + b), key0 + b, x.spare);
           const uint32_t seen = at.there ? visible<uint32_t>(a, s, row, key0 + b) : 0u;
           for (int j = 0; j < 16; ++j) {
             const int64_t byte = at.at + x.g * a.pool.head + min(j, at.last) * (int64_t)a.pool.row;
@@ -564,7 +566,7 @@ __global__ __launch_bounds__(256) void attend_f32(A a) {
     } else if constexpr (A::kPaged) {
       if (t - 4 < mem_tiles) look(t);                      // (behind a memory tile)
 #pragma unroll
-      for (int b = 0; b < 2; ++b) place[b] = place_at(a.pool, s, entry[b], tail_tile<A>(x, t - mem_tiles) * KT + b * 16);
+      for (int b = 0; b < 2; ++b) place[b] = place_at(a.pool, s, entry[b], tail_tile<A>(x, t - mem_tiles) * KT + b * 16, x.spare);
       if (t + 4 < x.k1) look(t + 4);
       const char* p = kp + (col < 16 ? place[0].at : place[1].at) + (uint32_t)min(col & 15, col < 16 ? place[0].last : place[1].last) * (int64_t)rsb;
 #pragma unroll
@@ -763,7 +765,7 @@ __global__ __launch_bounds__(256, 2) void attend_f32_many(A a) {
   const auto copy = [&](const char* base, float* to, int t, bool is_k) __attribute__((always_inline)) {
     if constexpr (A::kPaged) {
       if (t == max(x.k0, mem_tiles)) entry[is_k] = entry_of(a.pool, s, group_key(t));
-      const Place at = place_at(a.pool, s, entry[is_k], group_key(t));
+      const Place at = place_at(a.pool, s, entry[is_k], group_key(t), x.spare);
       if (t + 1 < x.k1) entry[is_k] = entry_of(a.pool, s, group_key(t + 1));
 #pragma unroll
       for (int j = 0; j < P::COPIES; ++j) {
@@ -827,7 +829,11 @@ __global__ __launch_bounds__(256, 2) void attend_f32_many(A a) {
     }
     return bits;
   };
-  if constexpr (A::kPaged) x.holes = x.k1 > mem_tiles && holes_of<KT>(a, s, x);
+  if constexpr (A::kPaged) {
+    // (values without a page are multiplied by weights of 0: finite ones, as the last row's are but for those that see it)
+    x.holes = x.k1 > mem_tiles && holes_of<KT>(a, s, x);
+    if (x.holes) x.spare = entry_of(a.pool, s, nt);
+  }
   if (x.k0 < x.k1) {
     fetch(x.k0, 0);
     store(x.k0, 0);
@@ -1160,7 +1166,7 @@ __global__ __launch_bounds__(256, 2) void attend_few(A a) {
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
           const int row0 = at_row(key) + t * 16;
-          const Place at = place_at(a.pool, s, entry[t], row0);
+          const Place at = place_at(a.pool, s, entry[t], row0, x.spare);
           const char* kr = a.pool.k + x.g * a.pool.head + at.at;
           const char* vr = a.pool.v + x.g * a.pool.head + at.at;
           there[t] = at.there;
@@ -1474,7 +1480,7 @@ __global__ __launch_bounds__(512, 2) void attend_many(A a) {
   const auto copy = [&](const char* base, uint16_t* to, int t, bool is_k) __attribute__((always_inline)) {
     if constexpr (A::kPaged) {
       if (t == max(x.k0, mem_tiles)) entry[is_k] = entry_of(a.pool, s, group_key(t));
-      const Place at = place_at(a.pool, s, entry[is_k], group_key(t));
+      const Place at = place_at(a.pool, s, entry[is_k], group_key(t), x.spare);
       if (t + 1 < x.k1) entry[is_k] = entry_of(a.pool, s, group_key(t + 1));
 #pragma unroll
       for (int j = 0; j < P::COPIES; ++j) {
@@ -1549,7 +1555,11 @@ __global__ __launch_bounds__(512, 2) void attend_many(A a) {
     }
     return bits;
   };
-  if constexpr (A::kPaged) x.holes = x.k1 > mem_tiles && holes_of<KT>(a, s, x);
+  if constexpr (A::kPaged) {
+    // (values without a page are multiplied by weights of 0: finite ones, as the last row's are but for those that see it)
+    x.holes = x.k1 > mem_tiles && holes_of<KT>(a, s, x);
+    if (x.holes) x.spare = entry_of(a.pool, s, nt);
+  }
   const auto raise = [&](float top) __attribute__((always_inline)) {                      // largest raw score of the tile to come
     top = max32(top) * scale;
     // A row's sums keep their reference until one of its scores passes it by 8: weights stay below 2^8, few tiles scale

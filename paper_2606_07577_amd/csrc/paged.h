@@ -66,8 +66,10 @@ __host__ __device__ inline int tail_tile(const TailTiles& x, int tt) { return tt
 
 // The 16 rows from `key` (a multiple of 16; behind the last row: those with it):
 // their table entry's index, and with its value where they begin, in bytes from
-// a head's first row on page 0 (no page: on page 0, whose rows are read and not
-// used), and how many rows follow the first that are not behind the last.
+// a head's first row on page 0, and how many rows follow the first that are not
+// behind the last.  Without a page they are read all the same, and not used: as
+// the rows with the last one, whose entry is `spare`, or if that is no page either
+// (or not known) as those of page 0.
 struct Place {
   int64_t at;
   int last;
@@ -77,11 +79,16 @@ __host__ __device__ inline int group_of(int nt, int key) {
   const int top = (nt - 1) & ~15;
   return key < top ? key : top;
 }
-__host__ __device__ inline Place place_of(const PagePool& pool, int nt, uint32_t entry, int key) {
-  const int group = group_of(nt, key);
+constexpr uint32_t kNoPage = UINT32_MAX;
+__host__ __device__ inline Place place_of(const PagePool& pool, int nt, uint32_t entry, int key, uint32_t spare) {
+  int group = group_of(nt, key);
   Place x;
   x.there = entry < pool.n_pages;
-  x.at = (int64_t)(x.there ? entry : 0) * pool.page + (group & ((1 << pool.shift) - 1)) * (int64_t)pool.row;
+  if (!x.there) {
+    entry = spare < pool.n_pages ? spare : 0;
+    if (spare < pool.n_pages) group = group_of(nt, nt);
+  }
+  x.at = (int64_t)entry * pool.page + (group & ((1 << pool.shift) - 1)) * (int64_t)pool.row;
   x.last = nt - 1 - group < 15 ? nt - 1 - group : 15;
   return x;
 }

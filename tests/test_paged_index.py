@@ -35,9 +35,9 @@ extern "C" uint32_t seen32(int nq, int nt, int window, int sinks, int i, int tre
   return visible<uint32_t>(sight_of(nq, nt, window, i, tree != 0, mask), nt - nq, sinks, key0);
 }
 // Byte of the 16 rows from key and their last one; the index of their entry; whether they have a page.
-extern "C" int64_t place(int64_t page, uint32_t row, uint32_t n_pages, int shift, int nt, int32_t entry, int key, int* last, int* index, int* there) {
+extern "C" int64_t place(int64_t page, uint32_t row, uint32_t n_pages, int shift, int nt, int32_t entry, int key, int32_t spare, int* last, int* index, int* there) {
   PagePool pool = {nullptr, nullptr, page, 0, row, n_pages, shift};
-  const Place x = place_of(pool, nt, (uint32_t)entry, key);
+  const Place x = place_of(pool, nt, (uint32_t)entry, key, (uint32_t)spare);
   *last = x.last; *index = group_of(nt, key) >> shift; *there = x.there;
   return x.at;
 }
@@ -59,7 +59,7 @@ def lib(tmp_path_factory):
     lib = ctypes.CDLL(out)
     lib.seen64.restype, lib.seen32.restype, lib.place.restype = ctypes.c_uint64, ctypes.c_uint32, ctypes.c_int64
     lib.seen64.argtypes = lib.seen32.argtypes = [ctypes.c_int] * 6 + [ctypes.c_uint64, ctypes.c_int]
-    lib.place.argtypes = [ctypes.c_int64, ctypes.c_uint32, ctypes.c_uint32, ctypes.c_int, ctypes.c_int, ctypes.c_int32, ctypes.c_int] + [ctypes.c_void_p] * 3
+    lib.place.argtypes = [ctypes.c_int64, ctypes.c_uint32, ctypes.c_uint32, ctypes.c_int, ctypes.c_int, ctypes.c_int32, ctypes.c_int, ctypes.c_int32] + [ctypes.c_void_p] * 3
     return lib
 
 
@@ -134,11 +134,15 @@ def test_places(lib, page_rows):
         entries = -(-nt // page_rows)
         for key in range(0, nt + 256, 16):
             for entry in (0, 3, pages - 1, pages, -1, -2 ** 31, 2 ** 31 - 1):
-                at = lib.place(page, row, pages, shift, nt, entry, key, *(ctypes.byref(x) for x in (last, index, there)))
-                first = min(key, (nt - 1) // 16 * 16)
-                assert 0 <= index.value < entries and index.value == first // page_rows
-                assert there.value == (0 <= entry < pages)
-                assert at == (entry if there.value else 0) * page + first % page_rows * row
-                assert last.value == min(15, nt - 1 - first) and first % page_rows + last.value < page_rows
-    assert lib.place(1 << 40, (1 << 24) - 16, 2 ** 31 - 1, 8, 1 << 30, 50, 240, *(ctypes.byref(x) for x in (last, index, there))) == \
+                for spare in (-1, 5, pages, 0):
+                    at = lib.place(page, row, pages, shift, nt, entry, key, spare, *(ctypes.byref(x) for x in (last, index, there)))
+                    first, end = min(key, (nt - 1) // 16 * 16), (nt - 1) // 16 * 16
+                    assert 0 <= index.value < entries and index.value == first // page_rows
+                    assert there.value == (0 <= entry < pages)
+                    if not there.value and 0 <= spare < pages:           # read as the rows with the last one
+                        assert at == spare * page + end % page_rows * row and last.value == nt - 1 - end
+                        continue
+                    assert at == (entry if there.value else 0) * page + first % page_rows * row
+                    assert last.value == min(15, nt - 1 - first) and first % page_rows + last.value < page_rows
+    assert lib.place(1 << 40, (1 << 24) - 16, 2 ** 31 - 1, 8, 1 << 30, 50, 240, -1, *(ctypes.byref(x) for x in (last, index, there))) == \
         (50 << 40) + 240 * ((1 << 24) - 16)
