@@ -630,13 +630,9 @@ def make_paged_projection(q, k, v, pos, q_out, table, first_row):
     if pos.dtype != torch.int32 or pos.dim() != 2 or pos.shape[1] != n or (pos.stride(1) != 1 and n > 1):
         raise ValueError("pos must be int32 [axes, n], its positions contiguous")
     _one_device(q, k, v, pos, q_out, table)
-    p = PagedProjection()
     rows = _table(table, int(first_row) + n)
-    p.q, p.q_head_stride, p.q_row_stride = _ptr(q), q.stride(0), q.stride(1)
-    p.k, p.v, p.kv_head_stride, p.kv_row_stride = _ptr(k), _ptr(v), k.stride(0), k.stride(1)
-    p.pos, p.pos_stride, p.n_rows = _ptr(pos), pos.stride(0), n
-    p.q_out, p.q_out_head_stride, p.q_out_row_stride = _ptr(q_out), q_out.stride(0), q_out.stride(1)
-    p.table, p.first_row = _ptr(table), int(first_row)
+    p = PagedProjection(_ptr(q), *q.stride()[:2], _ptr(k), _ptr(v), *k.stride()[:2], _ptr(pos), pos.stride(0), n,
+                        _ptr(q_out), *q_out.stride()[:2], _ptr(table), int(first_row))
     p._layout = _Layout(q.shape[0], k.shape[0], q.shape[2], q.dtype, q.device.index, pos.shape[0])
     p._fit = frozenset([("layout", p._layout), ("rows", rows)])
     return p

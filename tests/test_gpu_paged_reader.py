@@ -8,7 +8,7 @@ import torch
 
 from oracle import operators_oracle as orc
 from paper_2606_07577_amd import omnimem as om
-from paper_2606_07577_amd.step import HeldMemory, PagedReader, Reader
+from paper_2606_07577_amd.step import HeldMemory, PagedReader, Reader, StreamRunner
 
 pytestmark = pytest.mark.gpu
 U = 2.0 ** -24
@@ -227,6 +227,42 @@ def test_turns_on_different_streams():
     torch.cuda.synchronize()
     m.step([1, 1], stream=streams[1])
     m.reader.close()
+
+
+def test_a_streams_memory_read_with_drafts():
+    """A stream's chunks compressed, its caches held in 4 bits, an answer drafted over them: what the drafts of a path say is
+    what the same tokens say one after the other."""
+    layers, n = 2, 160
+    g = torch.Generator(device="cuda").manual_seed(6)
+    rnd = lambda *s: torch.randn(*s, generator=g, device="cuda").bfloat16()
+    run = StreamRunner(layers, H_Q, H_KV, D, n, 300)
+    mod = (torch.arange(n, device="cuda") % 4 == 3).to(torch.uint8)
+    for _ in range(3):
+        run.push([dict(q=rnd(H_Q, n, D), k=rnd(H_KV, n, D), v=rnd(H_KV, n, D), modality=mod, sm_scale=D ** -0.5) for _ in range(layers)])
+    held = run.hold()
+    rope = om.make_rope(D, [1000.0 ** (-j / 16) for j in range(16)])
+    drafted, plain = PagedReader([held], H_Q, H_KV, D, rope, 20, 100), Reader([held], H_Q, H_KV, D, rope, 100)
+    parents = [-1, 0, 0, 2, 1, 3]
+    path = [0, 2, 3, 5]
+    depth = [0, 1, 1, 2, 2, 3]
+    q, k, v = ([rnd(h, len(parents), D) for _ in range(layers)] for h in (H_Q, H_KV, H_KV))
+    pos = torch.tensor([depth], dtype=torch.int32, device="cuda")
+    tree = [torch.tensor(om.tree_masks(parents), device="cuda")]
+    outs = [drafted.layer(l, [q[l]], [k[l]], [v[l]], [pos], tree=tree)[0][:, path] for l in range(layers)]
+    drafted.accept([path])
+    for i, x in enumerate(path):
+        for l in range(layers):
+            [out] = plain.layer(l, [q[l][:, x: x + 1]], [k[l][:, x: x + 1]], [v[l][:, x: x + 1]], [pos[:, x: x + 1].contiguous()])
+            torch.cuda.synchronize()
+            # (bounds as below, held values up to 6 times a scale of theirs among them)
+            assert (out[:, 0].float() - outs[l][:, i].float()).abs().max() <= 2 / 16
+        plain.next()
+    assert drafted.tail == plain.tail == [4]
+    for l in range(layers):                                    # and the tails are the same rows
+        page = drafted.tables[0, 0].long()
+        assert torch.equal(drafted.k[l, page, :, :4], plain.k[l, 0, :, :4]) and torch.equal(drafted.v[l, page, :, :4], plain.v[l, 0, :, :4])
+    for x in (run, drafted, plain):
+        x.close()
 
 
 def test_whole_tails_read_as_the_readers():

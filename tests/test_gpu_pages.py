@@ -336,6 +336,26 @@ def test_whole_caches_give_what_contiguous_rows_give(dtype, nq):
     attn.close()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_sequences_that_share_pages_and_fused_rows(dtype):
+    """Two sequences with the same first pages, the same sequence twice, queries and results as parts of fused rows."""
+    h_q, h_kv, d = 6, 2, 64
+    attn = handle(h_q, h_kv, d, dtype)
+    g = torch.Generator(device="cuda").manual_seed(5)
+    store = Store(g, h_kv, d, dtype, 16, [100, 60], "rows")
+    store.device_tables[1][:2] = store.device_tables[0][:2]
+    store.device_tables.append(store.device_tables[0])
+    cases = [Case(attn, g, h_q, h_kv, d, dtype, *s) for s in ((3, 0, 100), (20, 33, 60), (3, 0, 100))]
+    cases[2].q = cases[0].q
+    fused = torch.randn(20, (h_q + 2 * h_kv) * d, generator=g, device="cuda").to(TORCH[dtype])
+    cases[1].q = fused.view(20, h_q + 2 * h_kv, d).transpose(0, 1)[:h_q]
+    rows = torch.full((21, h_q, d + 8), 7.0, device="cuda", dtype=TORCH[dtype])
+    cases[1].out = rows[:, :, :d].transpose(0, 1)
+    attend(attn, store, cases, 50, 3)
+    assert torch.equal(cases[0].out, cases[2].out) and (rows[:, :, d:] == 7).all()
+    attn.close()
+
+
 def test_pages_far_apart():
     """Pages past 2^32 bytes from the first."""
     attn = handle(4, 2, 128, "bf16")
