@@ -61,8 +61,7 @@ struct Unit {
   int slot;                  // partial, or -1: the result is final
   int split, splits;         // its share of the row tile
   TailTiles tail;            // in pages
-  bool holes;                // and some of them without a page,
-  uint32_t spare;            // for which the page with this entry is read
+  bool holes;                // and some of them without a page
 };
 // Row tile's tail key tile tt of those that it takes.
 template <class A>
@@ -113,7 +112,6 @@ __device__ inline Unit unit_of(const A& a, int u) {
   if constexpr (A::kPaged) {
     x.tail = tail_tiles_of<KT>(s.nq, s.nt, a.window, a.sinks, x.rt * R / a.group, last, s.v != nullptr);
     x.holes = false;
-    x.spare = kNoPage;
     tail_tiles = x.tail.count;
   } else {
     tail_tiles = tiles_of<KT>(tail_seen(s, a.causal, last));
@@ -157,18 +155,33 @@ template <typename U, class A>
 __device__ inline U visible(const A& a, const QuerySeq& s, const Row& row, int key0) {
   return visible<U>(row.sight, s.nt - s.nq, a.sinks, key0);
 }
-// Whether some 16 of the unit's tail rows have no page.
+// Whether some 16 of the unit's tail rows have no page: look() asks for the
+// entries of the first 256 sixteens (a lane to each), found() takes them, and
+// those behind, once what was asked for later is here too (with a wait for them
+// before the first rows 4096 queries over a window of 4096 take 272 us, not 270).
 template <int KT, class A>
-__device__ inline bool holes_of(const A& a, const QuerySeq& s, const Unit& x) {
-  constexpr int GROUPS = KT / 16;
-  const int t0 = max(x.k0 - x.mem_tiles, 0), n = (x.k1 - x.mem_tiles - t0) * GROUPS;
-  bool hole = false;
-  for (int i = threadIdx.x & 63; i < n; i += 64) {
+struct Holes {
+  static constexpr int GROUPS = KT / 16, FIRST = 4;
+  int t0, n;
+  uint32_t entry[FIRST];
+  __device__ inline uint32_t at(const A& a, const QuerySeq& s, const Unit& x, int i) const {
     const int key = tail_tile<A>(x, t0 + i / GROUPS) * KT + i % GROUPS * 16;
-    hole |= gload<uint32_t>(static_cast<const uint32_t*>(s.k) + (group_of(s.nt, key) >> a.pool.shift)) >= a.pool.n_pages;
+    return gload<uint32_t>(static_cast<const uint32_t*>(s.k) + (group_of(s.nt, key) >> a.pool.shift));
   }
-  return __any(hole);
-}
+  __device__ inline void look(const A& a, const QuerySeq& s, const Unit& x) {
+    t0 = max(x.k0 - x.mem_tiles, 0);
+    n = (x.k1 - x.mem_tiles - t0) * GROUPS;
+#pragma unroll
+    for (int j = 0; j < FIRST; ++j) entry[j] = n > 0 ? at(a, s, x, min(j * 64 + (int)(threadIdx.x & 63), n - 1)) : 0;
+  }
+  __device__ inline bool found(const A& a, const QuerySeq& s, const Unit& x) const {
+    uint32_t top = 0;
+#pragma unroll
+    for (int j = 0; j < FIRST; ++j) top = max(top, entry[j]);
+    for (int i = FIRST * 64 + (int)(threadIdx.x & 63); i < n; i += 64) top = max(top, at(a, s, x, i));
+    return __any(top >= a.pool.n_pages);
+  }
+};
 // Bits of a tile's rows that have a page.
 template <typename U, class A>
 __device__ inline U paged_bits(const A& a, const QuerySeq& s, int key0) {
@@ -253,9 +266,10 @@ __device__ __forceinline__ void form_again(const A& a, const QuerySeq& s, const 
   // (in pages) the unit's tail rows: f(K row, V row, it is seen)
   const auto each = [&](auto&& f) __attribute__((always_inline)) {
     if constexpr (A::kPaged) {
+      const uint32_t spare = x.holes ? entry_of(a.pool, s, s.nt) : kNoPage;
       for (int tt = max(x.k0 - x.mem_tiles, 0); tt < x.k1 - x.mem_tiles; ++tt)
         for (int key0 = tail_tile<A>(x, tt) * KT, b = 0; b < KT; b += 16) {
-          const Place at = place_at(a.pool, s, entry_of(a.pool, s, key0 + b), key0 + b, x.spare);
+          const Place at = place_at(a.pool, s, entry_of(a.pool, s, key0 + b), key0 + b, spare);
           const uint32_t seen = at.there ? visible<uint32_t>(a, s, row, key0 + b) : 0u;
           for (int j = 0; j < 16; ++j) {
             const int64_t byte = at.at + x.g * a.pool.head + min(j, at.last) * (int64_t)a.pool.row;
@@ -566,7 +580,7 @@ __global__ __launch_bounds__(256) void attend_f32(A a) {
     } else if constexpr (A::kPaged) {
       if (t - 4 < mem_tiles) look(t);                      // (behind a memory tile)
 #pragma unroll
-      for (int b = 0; b < 2; ++b) place[b] = place_at(a.pool, s, entry[b], tail_tile<A>(x, t - mem_tiles) * KT + b * 16, x.spare);
+      for (int b = 0; b < 2; ++b) place[b] = place_at(a.pool, s, entry[b], tail_tile<A>(x, t - mem_tiles) * KT + b * 16, kNoPage);
       if (t + 4 < x.k1) look(t + 4);
       const char* p = kp + (col < 16 ? place[0].at : place[1].at) + (uint32_t)min(col & 15, col < 16 ? place[0].last : place[1].last) * (int64_t)rsb;
 #pragma unroll
@@ -739,6 +753,12 @@ __global__ __launch_bounds__(256, 2) void attend_f32_many(A a) {
   const int tid = threadIdx.x, lane = tid & 63, wave = wave_id(), half = lane >> 5, col = lane & 31;
   const Row row = row_of(a, s, x, x.rt * R + wave * 32 + col);
   const float* qp = static_cast<const float*>(s.q) + row.h * elems(s.q_hs, 4) + row.i * elems(s.q_rs, 4);
+  uint32_t spare = kNoPage;                                // (see attend_many)
+  Holes<KT, A> holes;
+  if constexpr (A::kPaged) {
+    if (s.nt > 0) spare = entry_of(a.pool, s, s.nt);
+    holes.look(a, s, x);
+  }
   floatx4 q[D / 8];                                        // channels 8 j + 4 half ..: one of each half to an MFMA
 #pragma unroll
   for (int j = 0; j < D / 8; ++j) q[j] = row.live ? gload<floatx4>(qp + 8 * j + 4 * half) : floatx4{};
@@ -765,7 +785,7 @@ __global__ __launch_bounds__(256, 2) void attend_f32_many(A a) {
   const auto copy = [&](const char* base, float* to, int t, bool is_k) __attribute__((always_inline)) {
     if constexpr (A::kPaged) {
       if (t == max(x.k0, mem_tiles)) entry[is_k] = entry_of(a.pool, s, group_key(t));
-      const Place at = place_at(a.pool, s, entry[is_k], group_key(t), x.spare);
+      const Place at = place_at(a.pool, s, entry[is_k], group_key(t), spare);
       if (t + 1 < x.k1) entry[is_k] = entry_of(a.pool, s, group_key(t + 1));
 #pragma unroll
       for (int j = 0; j < P::COPIES; ++j) {
@@ -829,17 +849,13 @@ __global__ __launch_bounds__(256, 2) void attend_f32_many(A a) {
     }
     return bits;
   };
-  if constexpr (A::kPaged) {
-    // (values without a page are multiplied by weights of 0: finite ones, as the last row's are but for those that see it)
-    x.holes = x.k1 > mem_tiles && holes_of<KT>(a, s, x);
-    if (x.holes) x.spare = entry_of(a.pool, s, nt);
-  }
   if (x.k0 < x.k1) {
     fetch(x.k0, 0);
     store(x.k0, 0);
   }
   dma_wait();
   __syncthreads();
+  if constexpr (A::kPaged) x.holes = holes.found(a, s, x);
   for (int t = x.k0; t < x.k1; ++t) {
     const int st = (t - x.k0) & 1;
     if (t + 1 < x.k1) fetch(t + 1, st ^ 1);
@@ -1166,7 +1182,7 @@ __global__ __launch_bounds__(256, 2) void attend_few(A a) {
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
           const int row0 = at_row(key) + t * 16;
-          const Place at = place_at(a.pool, s, entry[t], row0, x.spare);
+          const Place at = place_at(a.pool, s, entry[t], row0, kNoPage);
           const char* kr = a.pool.k + x.g * a.pool.head + at.at;
           const char* vr = a.pool.v + x.g * a.pool.head + at.at;
           there[t] = at.there;
@@ -1446,6 +1462,13 @@ __global__ __launch_bounds__(512, 2) void attend_many(A a) {
   const int tid = threadIdx.x, lane = tid & 63, wave = wave_id(), half = lane >> 5, col = lane & 31;
   const float scale = fabsf(s.scale_log2);
   const Row row = row_of(a, s, x, x.rt * R + wave * 32 + col);
+  uint32_t spare = kNoPage;                                // of the rows that are read where there is no page
+  Holes<KT, A> holes;
+  if constexpr (A::kPaged) {
+    // (values without a page are multiplied by weights of 0: finite ones, as the last row's are but for those that see it)
+    if (s.nt > 0) spare = entry_of(a.pool, s, s.nt);
+    holes.look(a, s, x);
+  }
   frag q[NKS];
   {
     const uint16_t* p = static_cast<const uint16_t*>(s.q) + row.h * elems(s.q_hs, 2) + row.i * elems(s.q_rs, 2);
@@ -1480,7 +1503,7 @@ __global__ __launch_bounds__(512, 2) void attend_many(A a) {
   const auto copy = [&](const char* base, uint16_t* to, int t, bool is_k) __attribute__((always_inline)) {
     if constexpr (A::kPaged) {
       if (t == max(x.k0, mem_tiles)) entry[is_k] = entry_of(a.pool, s, group_key(t));
-      const Place at = place_at(a.pool, s, entry[is_k], group_key(t), x.spare);
+      const Place at = place_at(a.pool, s, entry[is_k], group_key(t), spare);
       if (t + 1 < x.k1) entry[is_k] = entry_of(a.pool, s, group_key(t + 1));
 #pragma unroll
       for (int j = 0; j < P::COPIES; ++j) {
@@ -1555,11 +1578,6 @@ __global__ __launch_bounds__(512, 2) void attend_many(A a) {
     }
     return bits;
   };
-  if constexpr (A::kPaged) {
-    // (values without a page are multiplied by weights of 0: finite ones, as the last row's are but for those that see it)
-    x.holes = x.k1 > mem_tiles && holes_of<KT>(a, s, x);
-    if (x.holes) x.spare = entry_of(a.pool, s, nt);
-  }
   const auto raise = [&](float top) __attribute__((always_inline)) {                      // largest raw score of the tile to come
     top = max32(top) * scale;
     // A row's sums keep their reference until one of its scores passes it by 8: weights stay below 2^8, few tiles scale
@@ -1576,6 +1594,7 @@ __global__ __launch_bounds__(512, 2) void attend_many(A a) {
   if (x.k0 < x.k1) {
     floatx16 s0[2], s1[2];
     const auto first = [&](int stage) __attribute__((always_inline)) {       // scores of the first tile
+      if constexpr (A::kPaged) x.holes = holes.found(a, s, x);
       const uint16_t* kd = kbuf + stage * TILE;
       s0[0] = s0[1] = floatx16{};
 #pragma unroll
