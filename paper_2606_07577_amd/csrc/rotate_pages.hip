@@ -141,10 +141,16 @@ void launch(const All& a, int n, int64_t rows, int64_t tokens, hipStream_t st) {
   x.pool = a.pool;
   std::memcpy(x.turns, a.turns, sizeof a - offsetof(All, turns));
   constexpr int U = D / (2 * kRun<T>), TOKENS = 64 / U;
-  if (tokens >= 4096) {                                    // (see rotate.hip)
+  // us, a workgroup to a token and to several: 2000 tokens of 36 heads of width 128 11.4 and 13.1, 4000 17.4 and 16.1; of 12
+  // heads 6.6 and 7.2, 11.1 and 9.2; of 24 heads of width 64 6.5 and 9.1, 10.9 and 10.4; 20 heads of fp32, width 64: 1000 5.2
+  // and 6.9, 2331 9.2 and 8.9, 3500 11.1 and 9.9
+  if (tokens >= 3000) {
     rotate_rows<T, D, PagedRotateArgs<N>><<<dim3((unsigned)((rows + TOKENS - 1) / TOKENS), n), 256, 0, st>>>(x);
   } else {
-    const int waves = std::min((a.h_q + 2 * a.h_kv + TOKENS - 1) / TOKENS, kRowWaves);
+    // wavefronts for all heads of a token, as long as the chip has them side by side; us, 36 heads of width 128, 5 and 4 or 2:
+    // 256 tokens 4.8 and 5.6, 1000 9.0 and 8.1 (2: 8.7), 2000 14.6 and 11.4 (4: 12.7)
+    const int all = (a.h_q + 2 * a.h_kv + TOKENS - 1) / TOKENS;
+    const int waves = std::min({all, kRowWaves, std::max(2, (int)(4096 / tokens))});
     x.waves = waves;
     rotate_row<T, D, PagedRotateArgs<N>><<<dim3((unsigned)rows, n), 64 * waves, 0, st>>>(x);
   }
