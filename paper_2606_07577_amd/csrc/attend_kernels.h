@@ -9,6 +9,7 @@
 // registers have.
 #pragma once
 
+#include <cmath>
 #include <type_traits>
 
 #include "../../include/omnimem.h"
@@ -2024,6 +2025,44 @@ A take_few(A& a, int rows, int cus) {
   return few;
 }
 
+// Whether bf16 rows in pages take less time in units of 32 than in units of 256,
+// where a head has 1024 at least (so that its keys are read by many units).  For
+// the former: rounds of the chip (a single one, whose compute units have a unit
+// each, hides less: 0.6 rounds more) times a unit's key tiles of 32, and the time
+// of `ends` tiles for each round.  For the latter the longest unit's tiles of 64
+// and 3 more, or the average and 11 with a join, or where there are more units than
+// compute units the average and the last ones' difference; a window's borders are 2.  us,
+// they and what they are taken for in brackets, width 128, 28 and 4 heads: a window
+// of 100 over 1200 queries 29 (31) and 23 (19), over 500 14 (14) and 21 (19), of 1500
+// over 300 37 (35) and 33 (33), prompts of 1000 34 (34) and 40 (40), of 2500 116 (112)
+// and 88 (94), 400 queries over 2048 rows 44 (40) and 35 (37); width 64, 16 and 4
+// heads: a prompt of 3000 56 (55) and 72 (66), windows of 100 over 2000 15 (15) and 17
+// (16), over 4096 24 (26) and 18 (16), 400 queries over 8192 rows 64 (53) and 38 (39).
+template <int D, class A>
+bool fewer_rows_pay(const A& a, int cus) {
+  constexpr double kFew = D == 128 ? 0.185 : 0.12, kMany = D == 128 ? 2.03 : 1.36;    // us of a tile
+  constexpr double kEnds = D == 128 ? 24 : 20;
+  double units = 0, keys = 0, blocks = 0, full = 0, half = 0, longest = 0;
+  for (int i = 0; i < a.n_seqs; ++i) {
+    const QuerySeq& s = a.seq[i];
+    const double rows = (double)a.group * s.nq, n = a.h_kv * std::ceil(rows / 32), m = a.h_kv * std::ceil(rows / 256);
+    const int near = tail_rows<32>(a, s);
+    // (without a window a query sees half of its prompt on average; memory tiles of 128 take 2.6 tiles' time)
+    const double seen = near < s.nt || s.v ? near : s.nq <= s.nt ? s.nt - s.nq / 2 : 0.5 * s.nt * s.nt / s.nq;
+    const double held = std::ceil(s.nm / 64.0) + (near < s.nt ? 2 : 0), tiles = held + std::ceil(tail_rows<256>(a, s) / 64.0);
+    units += n;
+    keys += n * (std::ceil(seen / 32) + 2.6 * std::ceil(s.nm / 128.0));
+    blocks += m;
+    full += m * tiles;
+    half += m * (held + std::min(tiles - held, std::ceil((seen + 64) / 64)));
+    longest = std::max(longest, tiles);
+  }
+  const double rounds = std::ceil(units / cus), splits = std::max(1.0, std::floor(cus / units)), mean = keys / units / splits;
+  const double few = (rounds + 0.6) * mean + kEnds * rounds + (splits > 1 ? 16 : 0);
+  const double many = blocks < cus ? std::min(longest + 3, full / cus + 11) : (half + 3 * blocks) / cus + longest - half / blocks + 3;
+  return kFew * few + 3 <= kMany * many + (D == 128 ? 3 : 5);
+}
+
 constexpr int kAlwaysFew = 64;   // query rows of a head that never take a many-row kernel
 template <int D, class A>
 hipError_t attend(const AttnDims& dm, A& a, int cus, void* ws, hipStream_t st) {
@@ -2076,9 +2115,11 @@ hipError_t attend(const AttnDims& dm, A& a, int cus, void* ws, hipStream_t st) {
   // tail rows 31 and 33 (28); 700 rows over 8192 33 and 35 (22), over 32768 73 and 65 (88).  In pages, whose lengths are
   // shared out evenly (plan_lengths), to 28: trees over 500 to 8192 rows, 448 rows of a head 32.0 and 32.0 (28; one
   // sequence), 42 and 38 (37; 2), 27.5 and 29.6 (14; 4 over up to 2048), 88 and 59 (98; 8), 224 rows 28 and 30 (18), 38 and
-  // 35 (29); a window of 512, 7168 rows 47 and 35 (35), 1792 rows 18 and 28 (9).
-  if (rows <= kAlwaysFew || (rows <= 128 && memory >= tail) || memory + 2 * tail <= (A::kPaged ? 28 : 40) * cus)
-    return attend_few_rows<D, 2>(a, cus, ws, st);
+  // 35 (29); from 1024 rows on see fewer_rows_pay.
+  bool is_few = rows <= kAlwaysFew || (rows <= 128 && memory >= tail) || memory + 2 * tail <= (A::kPaged ? 28 : 40) * cus;
+  if constexpr (A::kPaged)
+    if (rows >= 1024) is_few = fewer_rows_pay<D>(a, cus);
+  if (is_few) return attend_few_rows<D, 2>(a, cus, ws, st);
   A few = take_few<Many<D>::R, Many<D>::KT>(a, kAlwaysFew, cus);
   if (few.n_seqs > 0) {
     const hipError_t e = attend<D>(dm, few, cus, ws, st);

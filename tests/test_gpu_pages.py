@@ -121,7 +121,8 @@ class Heavy:
     """A sequence of so much work over a memory that its call takes the kernels of many rows for all of its sequences
     (those of few rows would leave for a launch of their own if they had more keys)."""
 
-    def __init__(self, attn, g, h_q, h_kv, d, dtype, n=2600, held=5000):
+    def __init__(self, attn, g, h_q, h_kv, d, dtype, held=20000):
+        n = 36000 // h_q
         self.q = torch.randn(h_q, n, d, generator=g, device="cuda").to(TORCH[dtype])
         self.out = torch.zeros_like(self.q)
         rows = [torch.randn(h_kv, held, d, generator=g, device="cuda").to(TORCH[dtype]) for _ in range(2)]
@@ -239,7 +240,7 @@ def test_prompts(dtype, window, sinks, tail):
     attn = handle(3, 1, 128, dtype)
     g = torch.Generator(device="cuda").manual_seed(tail)
     store = Store(g, 1, 128, dtype, 64, [tail])
-    beside = Heavy(attn, g, 3, 1, 128, dtype, n=4000, held=8000)
+    beside = Heavy(attn, g, 3, 1, 128, dtype, held=8000)
     c = Case(attn, g, 3, 1, 128, dtype, 1111, 0, tail)
     attend(attn, store, [c], window, sinks, beside)
     attn.close()
@@ -252,7 +253,7 @@ def test_entries_that_are_no_page(dtype, h_q, nq, window, many):
     """Rows on them are not seen, wherever they lie; what no query's window holds is not looked at."""
     attn = handle(h_q, 2, 64, dtype)
     g = torch.Generator(device="cuda").manual_seed(nq)
-    beside = Heavy(attn, g, h_q, 2, 64, dtype, n=16000 // h_q) if many else None
+    beside = Heavy(attn, g, h_q, 2, 64, dtype) if many else None
     nt = 700
     store = Store(g, 2, 64, dtype, 16, [nt])
     table = store.device_tables[0]
@@ -275,7 +276,7 @@ def test_odd_values_that_are_not_seen(dtype, nq, tree, odd, many):
     no part; page 0, that entries without a page are read from, holds them too."""
     attn = handle(4, 2, 64, dtype)
     g = torch.Generator(device="cuda").manual_seed(nq)
-    beside = Heavy(attn, g, 4, 2, 64, dtype, n=4000) if many else None
+    beside = Heavy(attn, g, 4, 2, 64, dtype) if many else None
     nt, window = 411, 100
     store = Store(g, 2, 64, dtype, 16, [nt])
     store.k[0], store.v[0] = odd, odd
