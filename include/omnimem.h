@@ -618,8 +618,8 @@ typedef struct {
 } omnimem_path;
 
 /* Row first_row + path[i] becomes row first_row + i, for i = 0 .. n_kept - 1, of
- * every KV head of each of `n_layers` stores (alike but for k and v), in one
- * launch.  Rows behind the kept ones are left as they are, but for those that
+ * every KV head of each of `n_layers` stores (alike but for k and v, which
+ * share no row), in one launch.  Rows behind the kept ones are left as they are, but for those that
  * are written.  Of a row without a page, and to one, nothing is moved.
  * Errors: INVALID_ARG, UNSUPPORTED (page_rows). */
 omnimem_status omnimem_keep_pages(omnimem_attn* attn, const omnimem_pages* layers, int32_t n_layers,

@@ -7,11 +7,30 @@ using namespace omnimem;
 namespace {
 
 // A store's checks and its part of the kernels' arguments; its K and V as
-// arrays (pages for heads).
+// arrays (pages for heads), and their axes from the innermost out, in bytes.
+struct Axis {
+  int64_t count, stride;
+};
 struct Store {
   PagePool pool;
   Span k, v;
+  Axis axes[3];
+  int64_t width, extent;
 };
+// Whether K or V of two such stores, `off` bytes apart, share a byte.  An axis
+// begins where the one inside it ends, so of its steps only the two next to
+// `off` come near enough.
+bool meet(const Store& x, int64_t off, int n = 3) {
+  if (off < 0) off = -off;
+  if (n == 0) return off < x.width;
+  if (n == 3 && off >= x.extent) return false;
+  const Axis& a = x.axes[n - 1];
+  if (a.count == 1) return meet(x, off, n - 1);
+  for (int64_t i = off / a.stride; i <= off / a.stride + 1 && i < a.count; ++i)
+    if (meet(x, off - i * a.stride, n - 1)) return true;
+  return false;
+}
+int64_t apart_by(const void* a, const void* b) { return static_cast<const char*>(b) - static_cast<const char*>(a); }
 omnimem_status take_pages(omnimem_attn* attn, const omnimem_pages* pages, Store& x) {
   if (!pages) return fail(attn, OMNIMEM_ERR_INVALID_ARG, "null pages");
   const omnimem_pages& p = *pages;
@@ -23,9 +42,7 @@ omnimem_status take_pages(omnimem_attn* attn, const omnimem_pages* pages, Store&
   if (p.n_pages < 1 || !p.k || !p.v || !aligned(p.k, 16) || !aligned(p.v, 16))
     return fail(attn, OMNIMEM_ERR_INVALID_ARG, "pages: need 1 page at least, and k and v, 16-byte aligned");
   // the three axes from the innermost out: each begins where the one inside it ends
-  struct Axis {
-    int64_t count, stride;
-  } axes[3] = {{p.page_rows, p.row_stride}, {attn->cfg.n_kv_heads, p.head_stride}, {p.n_pages, p.page_stride}};
+  Axis axes[3] = {{p.page_rows, p.row_stride}, {attn->cfg.n_kv_heads, p.head_stride}, {p.n_pages, p.page_stride}};
   std::sort(axes, axes + 3, [](const Axis& a, const Axis& b) { return a.stride < b.stride || (a.stride == b.stride && a.count < b.count); });
   int64_t extent = d;
   double bytes = (double)d * e;
@@ -44,7 +61,10 @@ omnimem_status take_pages(omnimem_attn* attn, const omnimem_pages* pages, Store&
             (uint32_t)(p.row_stride * e), (uint32_t)p.n_pages, shift};
   x.k = {reinterpret_cast<uintptr_t>(p.k), p.n_pages, 1, p.page_stride * e, 0, page};
   x.v = {reinterpret_cast<uintptr_t>(p.v), p.n_pages, 1, p.page_stride * e, 0, page};
-  if (overlap(x.k, x.v)) return fail(attn, OMNIMEM_ERR_INVALID_ARG, "pages: k and v overlap");
+  for (int i = 0; i < 3; ++i) x.axes[i] = {axes[i].count, axes[i].stride * e};
+  x.width = d * e;
+  x.extent = extent * e;
+  if (meet(x, apart_by(p.k, p.v))) return fail(attn, OMNIMEM_ERR_INVALID_ARG, "pages: k and v overlap");
   return OMNIMEM_OK;
 }
 bool on(const Store& x, const Span& a) { return overlap(x.k, a) || overlap(x.v, a); }
@@ -190,6 +210,10 @@ omnimem_status omnimem_keep_pages(omnimem_attn* attn, const omnimem_pages* layer
     if (p.page_stride != f.page_stride || p.head_stride != f.head_stride || p.row_stride != f.row_stride ||
         p.n_pages != f.n_pages || p.page_rows != f.page_rows)
       return fail(attn, OMNIMEM_ERR_INVALID_ARG, "layer %d: its pages differ from the first layer's", l);
+    for (int j = 0; j < l; ++j)
+      if (meet(store, apart_by(p.k, layers[j].k)) || meet(store, apart_by(p.v, layers[j].v)) ||
+          meet(store, apart_by(p.k, layers[j].v)) || meet(store, apart_by(p.v, layers[j].k)))
+        return fail(attn, OMNIMEM_ERR_INVALID_ARG, "layer %d: its pages overlap layer %d's", l, j);
   }
   for (int i = 0; i < n; ++i) {
     const omnimem_path& s = seqs[i];

@@ -28,7 +28,7 @@ def handle(h_q, h_kv, d, dtype):
 
 
 class Store:
-    """Pages [pages, h, page_rows, d] in one of three layouts, all rows NaN but those that are filled."""
+    """Pages [pages, h, page_rows, d] in one of four layouts, all rows NaN but those that are filled."""
 
     def __init__(self, g, h_kv, d, dtype, page_rows, lengths, layout="pages"):
         td = TORCH[dtype]
@@ -39,6 +39,9 @@ class Store:
         elif layout == "rows":                   # heads inside rows, K and V of a page side by side, rows with a gap
             both = torch.full((n, 2, page_rows, h_kv, d + 16), float("nan"), device="cuda", dtype=td)
             k, v = (both[:, i, :, :, :d].transpose(1, 2) for i in range(2))
+        elif layout == "beside":                 # heads inside rows, K and V of a head of a row side by side
+            both = torch.full((n, page_rows, h_kv, 2, d), float("nan"), device="cuda", dtype=td)
+            k, v = (both[:, :, :, i].transpose(1, 2) for i in range(2))
         else:                                    # heads outside pages
             k, v = (torch.full((h_kv, n, page_rows, d), float("nan"), device="cuda", dtype=td).transpose(0, 1) for _ in range(2))
         self.k, self.v, self.rows = k, v, page_rows
@@ -234,6 +237,21 @@ def test_small_sequences_in_the_kernels_of_many_rows(dtype, h_q, h_kv, d, window
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("many", [False, True])
+def test_keys_beside_values(dtype, many):
+    """A store whose rows hold a head's key and its value one behind the other."""
+    attn = handle(4, 2, 128, dtype)
+    g = torch.Generator(device="cuda").manual_seed(12)
+    beside = Heavy(attn, g, 4, 2, 128, dtype) if many else None
+    sizes = [(1, 0, 1), (1, 40, 300), (33, 0, 200), (150, 70, 411), (64, 0, 90)]
+    store = Store(g, 2, 128, dtype, 64, [n for _, _, n in sizes], "beside")
+    cases = [Case(attn, g, 4, 2, 128, dtype, *s, masks=tree_of(64, 3) if s[0] == 64 else None) for s in sizes]
+    for window, sinks in ((0, 0), (70, 5)):
+        attend(attn, store, cases, window, sinks, beside)
+    attn.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("window,sinks,tail", [(0, 0, 6100), (700, 20, 9000)])
 def test_prompts(dtype, window, sinks, tail):
     """Enough work for the kernels of many rows by themselves, row tiles split over workgroups."""
@@ -398,7 +416,7 @@ def size_of(x, rot, neighbours):
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("d,rot,neighbours", [(128, 128, False), (128, 96, True), (64, 64, False), (64, 48, True), (64, 0, False)])
 @pytest.mark.parametrize("norm", [False, True])
-@pytest.mark.parametrize("page_rows,layout,lengths", [(16, "pages", [1, 0, 7, 130]), (64, "rows", [1] * 35), (32, "heads", [4000, 300, 1])])
+@pytest.mark.parametrize("page_rows,layout,lengths", [(16, "pages", [1, 0, 7, 130]), (64, "rows", [1] * 35), (32, "heads", [4000, 300, 1]), (128, "beside", [70, 300, 1])])
 def test_rows_go_to_their_pages(dtype, d, rot, neighbours, norm, page_rows, layout, lengths):
     h_q, h_kv, axes = 5, 1, 3
     g = torch.Generator(device="cuda").manual_seed(rot + d)
@@ -492,7 +510,7 @@ def test_rows_without_a_page_are_dropped(rows):
 # --- accepted drafts -----------------------------------------------------------
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("h_kv,d,layout", [(1, 64, "pages"), (4, 128, "rows"), (3, 64, "heads")])
+@pytest.mark.parametrize("h_kv,d,layout", [(1, 64, "pages"), (4, 128, "rows"), (3, 64, "heads"), (2, 128, "beside")])
 @pytest.mark.parametrize("layers", [1, 35])
 def test_accepted_drafts_move_up(dtype, h_kv, d, layout, layers):
     attn = handle(2 * h_kv, h_kv, d, dtype)

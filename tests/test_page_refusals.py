@@ -231,6 +231,43 @@ def test_keep_pages(lib, attn):
         assert b"layer 1" in lib.omnimem_attn_last_error(attn) and lib.standin_launches() == 0
 
 
+def rows_of(start, pool, elt):
+    """The first bytes of a small store's rows, in units of 16."""
+    return {(start + elt * (p * pool["page_stride"] + h * pool["head_stride"] + r * pool["row_stride"])) // 16
+            for p in range(pool["n_pages"]) for h in range(H) for r in range(pool["page_rows"])}
+
+
+def test_stores_inside_one_another(lib, attn):
+    """K and V, and the stores of several layers, may lie between one another's rows, heads and pages, but share no row: against
+    all rows of small stores, at every distance of their width and some others."""
+    e, width, pages = attn.elt, D * attn.elt, 3
+    layouts = [dict(row_stride=2 * H * D, head_stride=D, page_stride=32 * H * D),              # K and V of a row side by side
+               dict(row_stride=2 * H * D, head_stride=2 * D, page_stride=32 * H * D),          # of a head of a row
+               dict(row_stride=D, head_stride=32 * D, page_stride=32 * H * D),                 # of a head
+               dict(row_stride=2 * D, head_stride=16 * 2 * D * pages, page_stride=16 * 2 * D),  # heads outside pages
+               dict(row_stride=D + 16, head_stride=40 * D, page_stride=90 * D)]                # gaps that no row fits
+    lib.standin_launches()
+    met = 0
+    for layout in layouts:
+        pool = dict(k=FAR, v=2 * FAR, n_pages=pages, page_rows=16, **layout)
+        k = rows_of(FAR, pool, e)
+        assert len(k) == pages * H * 16
+        for off in [i * width for i in range(400)] + [i * width + 16 for i in range(0, 400, 7)] + [i * width - 32 for i in range(1, 400, 9)]:
+            share = any(x + j in k for x in rows_of(FAR + off, pool, e) for j in range(1 - width // 16, width // 16))
+            met += share
+            status = om.ERR_INVALID_ARG if share else om.OK
+            assert keep(lib, attn, pools=({**pool, "v": FAR + off},)) == status, (layout, off)
+            if off % (5 * width) == 0:
+                assert keep(lib, attn, pools=({**pool, "v": FAR + off} if not share else pool,)) == om.OK
+                for second in (dict(k=FAR + off, v=3 * FAR), dict(k=3 * FAR, v=FAR + off), dict(k=3 * FAR, v=2 * FAR + off),
+                               dict(k=2 * FAR + off, v=3 * FAR)):
+                    assert keep(lib, attn, pools=(pool, {**pool, "k": 4 * FAR, "v": 5 * FAR}, {**pool, **second})) == status
+                    assert status == om.OK or b"layer 2" in lib.omnimem_attn_last_error(attn)
+    assert met > 500
+    lib.standin_launches()
+    assert keep(lib, attn, pools=(POOL, POOL)) == om.ERR_INVALID_ARG and lib.standin_launches() == 0
+
+
 def test_binding():
     """Tensors that do not fit are refused before the library is called; tables as long as their rows need."""
     assert om.tree_masks([-1, 0, 0, 2, -1]) == [1, 3, 5, 13, 16]
