@@ -640,3 +640,54 @@ def test_calls_on_another_stream():
     stream.wait_stream(torch.cuda.current_stream())
     attend(attn, store, [c], 0, 0, stream=stream)
     attn.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_two_handles_at_once(dtype):
+    """Handles have workspaces of their own: their calls may run side by side, keys split over workgroups in both."""
+    g = torch.Generator(device="cuda").manual_seed(8)
+    store = Store(g, 2, 128, dtype, 64, [4000, 3500])
+    handles, streams = [handle(8, 2, 128, dtype) for _ in range(2)], [torch.cuda.Stream() for _ in range(2)]
+    cases = [[Case(attn, g, 8, 2, 128, dtype, nq, 0, nt) for nq, nt in sizes]
+             for attn, sizes in zip(handles, ([(1, 4000), (3, 3500)], [(40, 4000), (64, 3500)]))]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for attn, stream, cs in zip(handles, streams, cases):
+            attn.omnimem_attend_pages(store.pages(), [c.query(store, b) for b, c in enumerate(cs)], 3000, 7, stream=stream)
+    torch.cuda.synchronize()
+    for cs in cases:
+        for b, c in enumerate(cs):
+            c.check(store, b, 3000, 7)
+    for attn in handles:
+        attn.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("nq,tree", [(1, False), (40, True), (300, False)])
+def test_the_last_rows_of_the_longest_cache(dtype, nq, tree):
+    """2^30 rows on a few pages' repetitions: the last ones are written, seen through a window and moved as those of a short
+    cache on the same pages are (the same key tiles, so the same bits)."""
+    h_q, h_kv, d, rows, short = 4, 2, 64, 256, 1024
+    attn = handle(h_q, h_kv, d, dtype)
+    g = torch.Generator(device="cuda").manual_seed(nq)
+    rope = om.make_rope(d, [0.1 ** j for j in range(d // 2)])
+    table = torch.full((2 ** 30 // rows,), -1, dtype=torch.int32, device="cuda")
+    table[-short // rows:] = torch.arange(short // rows, device="cuda", dtype=torch.int32)
+    q, k, v, start = (torch.randn(h, n, d, generator=g, device="cuda").to(TORCH[dtype])
+                      for h, n in ((h_q, nq), (h_kv, nq), (h_kv, nq), (short // rows * h_kv, rows)))
+    pos = torch.arange(nq, dtype=torch.int32, device="cuda")[None]
+    masks = torch.tensor(om_signed(tree_of(nq, 2)), dtype=torch.int64, device="cuda") if tree else None
+    results = []
+    for t, n in ((table, 2 ** 30), (table[-short // rows:].clone(), short)):
+        kp, vp = (x.clone().view(short // rows, h_kv, rows, d) for x in (start, -start))
+        pages, turned, out = om.make_pages(kp, vp), torch.empty_like(q), torch.zeros_like(q)
+        lse = torch.zeros(h_q, nq, device="cuda")
+        attn.omnimem_rotate_pages(rope, pages, [om.make_paged_projection(q, k, v, pos, turned, t, n - nq)])
+        attn.omnimem_attend_pages(pages, [om.make_paged_query(turned, out, t, n, tree=masks, lse=lse)], 150)
+        attn.omnimem_keep_pages([pages], [om.make_path(t, n - 64, [1, 5, 63])])
+        torch.cuda.synchronize()
+        assert torch.isfinite(out).all() and (out != 0).any(2).all()
+        results.append((turned, out, lse, kp, vp))
+    for long, little in zip(*results):
+        assert torch.equal(long, little)
+    attn.close()
