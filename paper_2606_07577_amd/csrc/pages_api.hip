@@ -30,6 +30,19 @@ bool meet(const Store& x, int64_t off, int n = 3) {
     if (meet(x, off - i * a.stride, n - 1)) return true;
   return false;
 }
+// The bytes from the first to the last of some stores' K or V.
+struct Range {
+  uintptr_t lo = UINTPTR_MAX, hi = 0;
+  bool apart(const void* p, int64_t extent) const {
+    const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+    return at >= hi || at + (uintptr_t)extent <= lo;
+  }
+  void add(const void* p, int64_t extent) {
+    const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+    lo = std::min(lo, at);
+    hi = std::max(hi, at + (uintptr_t)extent);
+  }
+};
 int64_t apart_by(const void* a, const void* b) { return static_cast<const char*>(b) - static_cast<const char*>(a); }
 omnimem_status take_pages(omnimem_attn* attn, const omnimem_pages* pages, Store& x) {
   if (!pages) return fail(attn, OMNIMEM_ERR_INVALID_ARG, "null pages");
@@ -204,13 +217,19 @@ omnimem_status omnimem_keep_pages(omnimem_attn* attn, const omnimem_pages* layer
   if (st != OMNIMEM_OK) return st;
   if (n_layers < 0 || (n_layers > 0 && !layers)) return fail(attn, OMNIMEM_ERR_INVALID_ARG, "null layers, or n_layers < 0");
   Store store;
+  // of the layers so far; one that is outside of both (layers' stores one behind the other) is not compared with each
+  Range keys, values;
   for (int l = 0; l < n_layers; ++l) {
     if ((st = take_pages(attn, layers + l, store)) != OMNIMEM_OK) return st;
     const omnimem_pages &p = layers[l], &f = layers[0];
     if (p.page_stride != f.page_stride || p.head_stride != f.head_stride || p.row_stride != f.row_stride ||
         p.n_pages != f.n_pages || p.page_rows != f.page_rows)
       return fail(attn, OMNIMEM_ERR_INVALID_ARG, "layer %d: its pages differ from the first layer's", l);
-    for (int j = 0; j < l; ++j)
+    const bool outside = keys.apart(p.k, store.extent) && values.apart(p.k, store.extent) &&
+                         keys.apart(p.v, store.extent) && values.apart(p.v, store.extent);
+    keys.add(p.k, store.extent);
+    values.add(p.v, store.extent);
+    for (int j = 0; j < l && !outside; ++j)
       if (meet(store, apart_by(p.k, layers[j].k)) || meet(store, apart_by(p.v, layers[j].v)) ||
           meet(store, apart_by(p.k, layers[j].v)) || meet(store, apart_by(p.v, layers[j].k)))
         return fail(attn, OMNIMEM_ERR_INVALID_ARG, "layer %d: its pages overlap layer %d's", l, j);
