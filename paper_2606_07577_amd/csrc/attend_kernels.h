@@ -643,6 +643,13 @@ __global__ __launch_bounds__(256) void attend_f32(A a) {
     }
     uint32_t seen = ~0u;                                   // in pages: the tile's rows that the query sees
     if constexpr (A::kPaged && !decltype(mem)::value) {
+      // Rows without a page were read from page 0, which may hold an infinity or NaN: their weights of 0 would not take
+      // it away, and rows that see whole tiles are not formed again.
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+        if (!place[b].there)
+#pragma unroll
+          for (int i = 0; i < 8 * NCT; ++i) vr[i / 8 * 16 + b * 8 + i % 8] = 0u;
       const int key0 = tail_tile<A>(x, t - mem_tiles) * KT;
       if (key0 < x.tail.all_from || key0 + KT > x.tail.all_to) seen = visible<uint32_t>(a, s, row, key0);
       if (!place[0].there) seen &= 0xFFFF0000u;

@@ -320,6 +320,38 @@ def test_odd_values_that_are_not_seen(dtype, nq, tree, odd, many):
     attn.close()
 
 
+# queries, memory rows, tail rows (whole key tiles of every kernel, but for the last), page rows, entries without a page
+SEEN_WHOLE = [(1, 0, 64, 16, [1]), (1, 0, 128, 16, [0, 5]), (1, 0, 384, 32, [6]), (1, 70, 384, 16, [13]), (3, 0, 8192, 64, [9, 70, 71]),
+              (1, 4000, 8192, 16, [0, 300]), (20, 0, 640, 128, [2]), (90, 33, 1024, 16, [1, 20, 21]), (300, 0, 2048, 64, [7]),
+              (2, 0, 256, 16, [15]), (1, 0, 32, 16, [0, 1])]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("h_q,h_kv,d", [(4, 2, 64), (7, 1, 128)])
+@pytest.mark.parametrize("nq,nm,nt,page_rows,lost", SEEN_WHOLE)
+@pytest.mark.parametrize("many", [False, True])
+def test_holes_among_rows_that_are_all_seen(dtype, h_q, h_kv, d, nq, nm, nt, page_rows, lost, many):
+    """Rows without a page between rows of whole key tiles that a query sees, in one share and in several: what page 0,
+    another sequence's, holds in their place has no part."""
+    attn = handle(h_q, h_kv, d, dtype)
+    g = torch.Generator(device="cuda").manual_seed(nt + nq)
+    beside = Heavy(attn, g, h_q, h_kv, d, dtype) if many else None
+    store = Store(g, h_kv, d, dtype, page_rows, [nt])
+    table = store.tables[0]
+    if 0 in table:                               # (the sequence's own rows lie elsewhere)
+        i, free = table.index(0), next(p for p in range(len(store.k)) if p not in table)
+        store.k[free], store.v[free] = store.k[0], store.v[0]
+        store.device_tables[0][i] = table[i] = free
+    for i, x in enumerate(lost):
+        store.device_tables[0][x] = ODD[i]
+    c = Case(attn, g, h_q, h_kv, d, dtype, nq, nm, nt)
+    for odd in (float("nan"), float("inf"), -float("inf")):
+        store.k[0], store.v[0] = odd, odd
+        c.out.fill_(7.0)
+        attend(attn, store, [c], beside=beside)
+    attn.close()
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_scores_of_infinities_and_sharp_weights(dtype):
     attn = handle(4, 1, 64, dtype)
