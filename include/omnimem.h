@@ -573,7 +573,8 @@ typedef struct {
 } omnimem_paged_projection;
 
 /* What omnimem_rotate does, its keys and values going to pages.  q_out is q
- * (same pointer and strides) or overlaps no input; neither overlaps the pages.
+ * (same pointer and strides) or overlaps no input, positions and weights among
+ * them; nor do the pages overlap any of these.
  * Errors: INVALID_ARG, UNSUPPORTED (rotary_dim not a multiple of 16, page_rows). */
 omnimem_status omnimem_rotate_pages(omnimem_attn* attn, const omnimem_rope* rope, const omnimem_pages* pages,
                                     const omnimem_paged_projection* seqs, int32_t n, hipStream_t stream);

@@ -136,6 +136,18 @@ omnimem_status take_rope(omnimem_attn* attn, const omnimem_rope* rope, Args& a) 
   return OMNIMEM_OK;
 }
 
+// Whether a sequence's rotation reads positions, or a norm's weights, that are
+// `written`.
+template <class Seq, class Written>
+bool beside_rows(const omnimem_attn* a, const omnimem_rope& r, const Seq& s, Written&& written) {
+  const auto array = [](const void* p, int64_t n, int64_t stride, int64_t bytes) {
+    return Span{reinterpret_cast<uintptr_t>(p), n, 1, stride, 0, bytes};
+  };
+  const int64_t width = a->cfg.head_dim * (int64_t)elt(a);
+  return written(array(s.pos, r.n_axes, s.pos_stride * 4, s.n_rows * 4)) || (r.q_weight && written(array(r.q_weight, 1, 0, width))) ||
+         (r.k_weight && written(array(r.k_weight, 1, 0, width)));
+}
+
 template <class Query>
 float log2_scale(const Query& s, int d) {
   return (float)((s.sm_scale != 0.0f ? (double)s.sm_scale : 1.0 / std::sqrt((double)d)) * 1.4426950408889634);

@@ -126,6 +126,8 @@ omnimem_status omnimem_rotate_pages(omnimem_attn* attn, const omnimem_rope* rope
       return bad(attn, i, "q, k, v, q_out or the table overlaps the pages");
     if ((!same(o, q) && overlap(o, q)) || overlap(o, k) || overlap(o, v) || overlap(o, table))
       return bad(attn, i, "q_out overlaps an input that it is not");
+    if (beside_rows(attn, *rope, s, [&](const Span& x) { return overlap(o, x) || on(store, x); }))
+      return bad(attn, i, "q_out or the pages overlap pos or a norm's weights");
   }
   OnDevice dev(attn->device);
   hipError_t e = dev.err;

@@ -188,6 +188,26 @@ def test_rotate_pages(lib, attn):
     assert rotate(lib, attn, rope=om.Rope(n_axes=1, rotary_dim=8, inv_freq=(ctypes.c_double * 4)())) == om.ERR_UNSUPPORTED
 
 
+def test_rotate_pages_over_its_positions_or_weights(lib, attn):
+    """Rotated queries and the pages share no byte with the positions (of the last axis too) or with a norm's weights."""
+    out, end = BASE + (4 << 20), BASE + (4 << 20) + 4 * N * D * attn.elt          # (q_out is [4][N][D])
+    rope = lambda **weights: om.Rope(n_axes=3, eps=1e-6, **weights)
+    last = 4 * (2 * 1000 + N)                                                   # bytes of three axes, 1000 positions apart
+    lib.standin_launches()
+    for pos in (end, out - last, FAR - last, BASE + (3 << 20)):
+        assert rotate(lib, attn, rope=rope(), pos=pos, pos_stride=1000) == om.OK and lib.standin_launches() == 1
+    pool = FAR + 100 * PAGE * attn.elt
+    refused(lib, attn, rotate, [dict(rope=rope(), pos=p, pos_stride=1000)
+                                for p in (out, end - 4, out - last + 4, FAR - last + 4, pool - 4, 2 * FAR, 2 * FAR + 64)])
+    bytes = D * attn.elt
+    for name in ("q_weight", "k_weight"):
+        for w in (end, out - bytes, pool, FAR - bytes, BASE):
+            assert rotate(lib, attn, rope=rope(**{name: w})) == om.OK and lib.standin_launches() == 1
+        refused(lib, attn, rotate, [dict(rope=rope(**{name: w})) for w in (out, end - 16, out - bytes + 16, FAR, pool - 16, 2 * FAR + 4096)], n=1,
+                text=b"sequence 0")
+    assert rotate(lib, attn, rope=rope(q_weight=out, k_weight=FAR), n_rows=0) == om.OK and lib.standin_launches() == 0
+
+
 def test_attend_pages(lib, attn):
     unit = 16 // attn.elt
     tree = BASE + (6 << 20)
