@@ -453,7 +453,8 @@ typedef struct {
  * (x'_a cos - x'_b sin, x'_a sin + x'_b cos).  Values (and modality, when
  * given) are copied.  Angles are formed and reduced in 64 bits, norms and
  * rotations computed in fp32 and rounded once.  Each output is its own input
- * (same pointer and strides: in place) or overlaps no input.
+ * (same pointer and strides: in place) or overlaps no input, positions and
+ * weights among them.
  * Errors: INVALID_ARG, UNSUPPORTED (rotary_dim not a multiple of 16). */
 omnimem_status omnimem_rotate(omnimem_attn* attn, const omnimem_rope* rope, const omnimem_projection* seqs,
                               int32_t n, hipStream_t stream);

@@ -136,10 +136,14 @@ omnimem_status omnimem_rotate(omnimem_attn* attn, const omnimem_rope* rope, cons
       for (int y = 0; y < 3; ++y)
         if ((x != y && overlap(to[x], to[y])) || (!(x == y && same(to[x], in[y])) && overlap(to[x], in[y])))
           return bad(attn, i, "an output overlaps another, or an input that it is not");
-    if (s.modality && s.modality != s.modality_out) {
-      const uintptr_t m0 = reinterpret_cast<uintptr_t>(s.modality), m1 = reinterpret_cast<uintptr_t>(s.modality_out);
-      if (m0 < m1 + (uintptr_t)s.n_rows && m1 < m0 + (uintptr_t)s.n_rows) return bad(attn, i, "modality_out overlaps modality");
-    }
+    const Span modality = {reinterpret_cast<uintptr_t>(s.modality), 1, 1, 0, 0, s.n_rows};
+    const Span modality_out = {reinterpret_cast<uintptr_t>(s.modality_out), 1, 1, 0, 0, s.n_rows};
+    const auto rows = [](const Span (&x)[3], const Span& y) { return overlap(x[0], y) || overlap(x[1], y) || overlap(x[2], y); };
+    const auto written = [&](const Span& x) { return rows(to, x) || (s.modality && overlap(modality_out, x)); };
+    if (beside_rows(attn, *rope, s, written)) return bad(attn, i, "an output overlaps pos or a norm's weights");
+    if (s.modality && ((s.modality != s.modality_out && overlap(modality, modality_out)) || rows(to, modality) || rows(to, modality_out) ||
+                       rows(in, modality_out)))
+      return bad(attn, i, "modality or modality_out overlaps the other, or rows");
   }
   OnDevice dev(attn->device);
   hipError_t e = dev.err;

@@ -261,6 +261,27 @@ def test_one_row_of_several_heads_needs_a_place_for_each(lib, attn):
     refused(lib, attn, "omnimem_attend", om.Query, dict(query(), n_queries=1), (1,), [dict(out_head_stride=0)])
 
 
+def test_rotate_over_its_positions_weights_or_modalities(lib, attn):
+    f, e = projection(attn.elt), attn.elt
+    mod = dict(modality=BASE + (1 << 31), modality_out=BASE + (1 << 31) + 4096)
+    ends = {"q_out": f["q_out"] + 4 * 6400 * e, "k_out": f["k_out"] + (200 + 100) * 64 * e, "v_out": f["v_out"] + (200 + 100) * 64 * e}
+    for out, end in ends.items():
+        refused(lib, attn, "omnimem_rotate", om.Projection, f, (rope(),), [dict(pos=p) for p in (f[out], end - 4, f[out] - 796)])   # (2 axes of 100)
+        for name in ("q_weight", "k_weight"):
+            for w in (f[out], end - 16, f[out] - 64 * e + 16):
+                refused(lib, attn, "omnimem_rotate", om.Projection, f, (rope(**{name: w}),), [{}])
+            lib.standin_launches()
+            assert call(lib, attn, "omnimem_rotate", om.Projection, f, more=(rope(**{name: end}),)) == om.OK and lib.standin_launches() == 1
+        refused(lib, attn, "omnimem_rotate", om.Projection, f, (rope(),),
+                [dict(mod, modality=f[out]), dict(mod, modality_out=end - 1), dict(mod, modality=end - 1)])
+        for pos in (end, f[out] - 800):
+            assert call(lib, attn, "omnimem_rotate", om.Projection, f, more=(rope(),), pos=pos) == om.OK and lib.standin_launches() == 1
+        assert call(lib, attn, "omnimem_rotate", om.Projection, f, more=(rope(),), **dict(mod, modality=end, modality_out=f[out] - 100)) == om.OK
+        assert lib.standin_launches() == 1
+    refused(lib, attn, "omnimem_rotate", om.Projection, f, (rope(),), [dict(mod, modality_out=f["pos"] + 799), dict(mod, modality_out=f["v"])])
+    refused(lib, attn, "omnimem_rotate", om.Projection, f, (rope(k_weight=mod["modality_out"] + 96),), [mod])
+
+
 def test_strides_that_pass_any_address(lib, attn):
     far = 1 << 34
     refused(lib, attn, "omnimem_rotate", om.Projection, dict(projection(attn.elt), n_rows=1 << 30), (rope(),),
