@@ -143,7 +143,9 @@ void launch(const All& a, int n, int64_t rows, int64_t tokens, hipStream_t st) {
   constexpr int U = D / (2 * kRun<T>), TOKENS = 64 / U;
   // us, a workgroup to a token and to several: 2000 tokens of 36 heads of width 128 11.4 and 13.1, 4000 17.4 and 16.1; of 12
   // heads 6.6 and 7.2, 11.1 and 9.2; of 24 heads of width 64 6.5 and 9.1, 10.9 and 10.4; 20 heads of fp32, width 64: 1000 5.2
-  // and 6.9, 2331 9.2 and 8.9, 3500 11.1 and 9.9
+  // and 6.9, 2331 9.2 and 8.9, 3500 11.1 and 9.9.  The grid is the longest sequence times the sequences: prompts of 1000, 2900
+  // and 4000 (36 heads of width 128, in a graph on one state) 5.7, 12.7 and 14.4, beside 31 tokens of other sequences 11.4, 30.0
+  // and 20.2
   if (tokens >= 3000) {
     rotate_rows<T, D, PagedRotateArgs<N>><<<dim3((unsigned)((rows + TOKENS - 1) / TOKENS), n), 256, 0, st>>>(x);
   } else {
